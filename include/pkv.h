@@ -363,6 +363,42 @@ pkv_status pkv_mixed_attention(const pkv_paged_kv* kv, int32_t num_q_heads, floa
                                int32_t max_seq_len, void* d_out, float* d_lse,
                                void* workspace, size_t workspace_bytes, void* stream);
 
+/* Block tables and slot maps built on the GPU from request lengths: the device counterpart of
+ * pkv_seq_reserve and pkv_fill_block_tables for a step whose lengths are on the GPU (a decode
+ * loop in a captured graph, which a host table cannot grow). Sequence i, with cached_lens[i]
+ * cached and new_lens[i] new tokens (0: none, e.g. a padding sequence), takes the blocks that its
+ * growth needs from free_blocks (int32 [num_free], blocks that the caller has set aside, e.g. the
+ * table row of a sequence that pkv_seq_reserve gave room), in order from entry *free_used on,
+ * sequence 0 first; block_tables (int32 [num_seqs][max_blocks]) receives their ids after the
+ * ceil(cached_lens[i] / block_size) entries that the row holds already, which stay. The blocks
+ * are the ones pkv_seq_reserve would take from such a free list. Blocks that a cached prefix
+ * shares are not looked at: a new token goes into a partly filled last block as it is.
+ *   cu_new_lens [num_seqs + 1], seq_lens [num_seqs]: the new tokens' offsets, and
+ *     cached_lens + new_lens. *free_used_out: *free_used plus the blocks taken.
+ *   For each new token, in the rows cu_new_lens[i] .. of these arrays of max_rows entries (each
+ *     may be NULL): slot_map (int64: block * block_size + slot), row_seq (i), positions (the
+ *     token's position p in its sequence), row_lens (p + 1, the keys it may attend over). The
+ *     rows after the last token are padding: -1, -1, -1 and 0.
+ *   *status: 0, or PKV_EXTEND_* bits; the step is then refused as a whole: no table entry
+ *     changes, *free_used_out = *free_used, seq_lens = cached_lens, cu_new_lens is 0 throughout
+ *     and every row is padding.
+ * seq_lens may be cached_lens and free_used_out may be free_used (a loop's step then leaves
+ * the next one's input); no other arrays may overlap. max_rows <= 2^30. Zero sequences write an
+ * empty step. All arrays are device memory. */
+enum {
+  PKV_EXTEND_OUT_OF_BLOCKS = 1,  /* *free_used is negative, or too few blocks are behind it */
+  PKV_EXTEND_TABLE_FULL = 2,     /* a sequence needs more than max_blocks blocks */
+  PKV_EXTEND_TOO_MANY_ROWS = 4,  /* more than max_rows new tokens */
+  PKV_EXTEND_BAD_LENGTH = 8      /* a negative length, or one past 2^31 - 1 */
+};
+pkv_status pkv_extend_tables(int32_t* block_tables, int32_t max_blocks,
+                             const int32_t* cached_lens, const int32_t* new_lens,
+                             int32_t num_seqs, const int32_t* free_blocks, int32_t num_free,
+                             const int32_t* free_used, int32_t* free_used_out,
+                             int32_t* cu_new_lens, int32_t* seq_lens, int32_t* status,
+                             int32_t max_rows, int64_t* slot_map, int32_t* row_seq,
+                             int32_t* positions, int32_t* row_lens, void* stream);
+
 /* Paged gather (test support): copies the first lens[i] tokens of every sequence out of the
  * pool into contiguous k_out / v_out, bf16 [sum lens][num_kv_heads][head_dim], sequence i
  * starting at row cu_lens[i] (int32 [num_seqs + 1]). Bit-exact. max_len (host) >= every

@@ -458,4 +458,30 @@ pkv_status pkv_copy_blocks(const pkv_paged_kv* kv, const int32_t* pairs, int32_t
                   fn);
 }
 
+pkv_status pkv_extend_tables(int32_t* block_tables, int32_t max_blocks,
+                             const int32_t* cached_lens, const int32_t* new_lens,
+                             int32_t num_seqs, const int32_t* free_blocks, int32_t num_free,
+                             const int32_t* free_used, int32_t* free_used_out,
+                             int32_t* cu_new_lens, int32_t* seq_lens, int32_t* status,
+                             int32_t max_rows, int64_t* slot_map, int32_t* row_seq,
+                             int32_t* positions, int32_t* row_lens, void* stream) {
+  const char* fn = "pkv_extend_tables";
+  if (max_blocks < 0 || num_seqs < 0 || num_free < 0 || max_rows < 0)
+    return fail(PKV_ERR_INVALID_ARG, "pkv_extend_tables: negative size");
+  if (max_rows > kMaxGridX)
+    return fail(PKV_ERR_INVALID_ARG, "pkv_extend_tables: more than 2^30 rows");
+  if (free_used == nullptr || free_used_out == nullptr || cu_new_lens == nullptr ||
+      status == nullptr)
+    return fail(PKV_ERR_INVALID_ARG, "pkv_extend_tables: NULL pointer");
+  if (num_seqs > 0 && (cached_lens == nullptr || new_lens == nullptr || seq_lens == nullptr ||
+                       (block_tables == nullptr && max_blocks > 0)))
+    return fail(PKV_ERR_INVALID_ARG, "pkv_extend_tables: NULL pointer");
+  if (num_free > 0 && free_blocks == nullptr)
+    return fail(PKV_ERR_INVALID_ARG, "pkv_extend_tables: free_blocks is NULL");
+  const ExtendArgs a{block_tables, max_blocks,    cached_lens, new_lens, num_seqs,  free_blocks,
+                     num_free,     free_used,     free_used_out, cu_new_lens, seq_lens, status,
+                     max_rows,     slot_map,      row_seq,     positions, row_lens};
+  return launched(launch_extend_tables(a, static_cast<hipStream_t>(stream)), fn);
+}
+
 }  // extern "C"

@@ -28,6 +28,29 @@ hipError_t launch_gather_kv(const KvView& kv, const int32_t* block_tables, int32
                             int32_t max_len, uint16_t* k_out, uint16_t* v_out,
                             hipStream_t stream);
 
+// A step's block tables and row metadata (pkv_extend_tables). seq_lens may be cached_lens and
+// free_used_out free_used: each is read before it is written.
+struct ExtendArgs {
+  int32_t* tables;
+  int32_t max_blocks;
+  const int32_t* cached_lens;
+  const int32_t* new_lens;
+  int32_t num_seqs;
+  const int32_t* free_blocks;
+  int32_t num_free;
+  const int32_t* free_used;
+  int32_t* free_used_out;
+  int32_t* cu_new_lens;
+  int32_t* seq_lens;
+  int32_t* status;
+  int32_t max_rows;
+  int64_t* slot_map;   // these four: [max_rows], or null
+  int32_t* row_seq;
+  int32_t* positions;
+  int32_t* row_lens;
+};
+hipError_t launch_extend_tables(const ExtendArgs& a, hipStream_t stream);
+
 hipError_t launch_copy_blocks(const KvView& kv, const int32_t* pairs, int32_t num_pairs,
                               hipStream_t stream);
 

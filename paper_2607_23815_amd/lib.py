@@ -37,6 +37,8 @@ PKV_ERR_HIP = 6
 PKV_ERR_KEY_EXISTS = 7
 PKV_ERR_BAD_METADATA = 8
 PKV_EVICT_LRU, PKV_EVICT_MRU = 0, 1
+PKV_EXTEND_OUT_OF_BLOCKS, PKV_EXTEND_TABLE_FULL = 1, 2
+PKV_EXTEND_TOO_MANY_ROWS, PKV_EXTEND_BAD_LENGTH = 4, 8
 PKV_PIN_EXPLICIT, PKV_PIN_VIRTUAL = 0, 1
 
 
@@ -143,6 +145,8 @@ _SIGS = {
                                       c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p,
                                       c_int32, c_void_p, c_int32, c_int32, c_void_p, c_void_p,
                                       c_void_p, c_size_t, c_void_p]),
+    "pkv_extend_tables": (c_int32, [c_void_p, c_int32, c_void_p, c_void_p, c_int32, c_void_p,
+                                    c_int32] + [c_void_p] * 5 + [c_int32] + [c_void_p] * 5),
     "pkv_gather_kv": (c_int32, [ctypes.POINTER(PagedKV), c_void_p, c_int32, c_void_p, c_void_p,
                                 c_int32, c_int32, c_void_p, c_void_p, c_void_p]),
 }
@@ -443,6 +447,26 @@ def _stream(stream):
     return torch.cuda.current_stream().cuda_stream
 
 
+def _device(stream):
+    """The current device's index, which a call launches on; an explicit stream must be its."""
+    torch = _torch or _get_torch()
+    dev = torch.cuda.current_device()
+    if stream is not None and stream.device_index != dev:
+        raise ValueError(f"stream is of device {stream.device_index}, the current device is {dev}")
+    return dev
+
+
+def _ptr(t, name, dtype, dev):
+    """A contiguous tensor of this type on the current device `dev`: its address."""
+    if (isinstance(t, _Tensor) and t.dtype is dtype and t.is_cuda and t.get_device() == dev
+            and t.is_contiguous()):
+        return t.data_ptr()
+    _dev_ptr(t, name, dtype)
+    if t is None:
+        raise TypeError(f"{name} must be a GPU tensor (the library has no CPU path)")
+    raise ValueError(f"{name} is on device {t.get_device()}, the current device is {dev}")
+
+
 def paged_kv(k_cache, v_cache) -> PagedKV:
     """Describe a pool: k_cache bf16 [num_blocks][Hkv][D/8][16][8], v_cache bf16
     [num_blocks][Hkv][D][16]."""
@@ -587,6 +611,43 @@ def pkv_gather_kv(k_cache, v_cache, block_tables, lens, cu_lens, max_len: int, k
                               _dev_ptr(cu_lens, "cu_lens", torch.int32), int(lens.shape[0]),
                               int(max_len), _dev_ptr(k_out, "k_out", torch.bfloat16),
                               _dev_ptr(v_out, "v_out", torch.bfloat16), _stream(stream)))
+
+
+def pkv_extend_tables(block_tables, cached_lens, new_lens, free_blocks, free_used, free_used_out,
+                      cu_new_lens, seq_lens, status, max_rows: int, slot_map=None, row_seq=None,
+                      positions=None, row_lens=None, stream=None) -> None:
+    """Block tables [b][max_blocks] grown in place for a step's new tokens, with blocks of
+    free_blocks from entry free_used [1] on, and the step's offsets, lengths and rows (int32;
+    slot_map int64). status [1] holds PKV_EXTEND_* bits when the step was refused. seq_lens may
+    be cached_lens, and free_used_out free_used."""
+    torch = _torch or _get_torch()
+    i32 = torch.int32
+    dev = _device(stream)
+    if block_tables.dim() != 2:
+        raise ValueError("block_tables must be [num_seqs][max_blocks]")
+    b, max_blocks = block_tables.shape
+    if not (cached_lens.numel() == new_lens.numel() == seq_lens.numel() == b
+            and cu_new_lens.numel() == b + 1):
+        raise ValueError("cached_lens, new_lens and seq_lens must have an entry per sequence, "
+                         "cu_new_lens one more")
+    if not free_used.numel() == free_used_out.numel() == status.numel() == 1:
+        raise ValueError("free_used, free_used_out and status must have one entry")
+    for name, t in (("slot_map", slot_map), ("row_seq", row_seq), ("positions", positions),
+                    ("row_lens", row_lens)):
+        if t is not None and t.numel() != max_rows:
+            raise ValueError(f"{name} must have max_rows entries")
+    _check(_lib.pkv_extend_tables(
+        _ptr(block_tables, "block_tables", i32, dev), max_blocks,
+        _ptr(cached_lens, "cached_lens", i32, dev), _ptr(new_lens, "new_lens", i32, dev), b,
+        _ptr(free_blocks, "free_blocks", i32, dev), free_blocks.numel(),
+        _ptr(free_used, "free_used", i32, dev),
+        _ptr(free_used_out, "free_used_out", i32, dev),
+        _ptr(cu_new_lens, "cu_new_lens", i32, dev), _ptr(seq_lens, "seq_lens", i32, dev),
+        _ptr(status, "status", i32, dev), max_rows,
+        None if slot_map is None else _ptr(slot_map, "slot_map", torch.int64, dev),
+        None if row_seq is None else _ptr(row_seq, "row_seq", i32, dev),
+        None if positions is None else _ptr(positions, "positions", i32, dev),
+        None if row_lens is None else _ptr(row_lens, "row_lens", i32, dev), _stream(stream)))
 
 
 def alloc_workspace(nbytes: int, device="cuda"):
