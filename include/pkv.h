@@ -399,6 +399,40 @@ pkv_status pkv_extend_tables(int32_t* block_tables, int32_t max_blocks,
                              int32_t max_rows, int64_t* slot_map, int32_t* row_seq,
                              int32_t* positions, int32_t* row_lens, void* stream);
 
+/* Rotary positions and KV append: the queries and keys of a step's new tokens are turned by
+ * their positions, and the keys and values go to their slots of the pool. Row t is one token:
+ * q [rows][num_q_heads][head_dim], k_new and v_new [rows][num_kv_heads][head_dim], bf16, each with
+ * its own row stride in elements (e.g. the parts of one fused projection's rows); heads within
+ * a row are contiguous. For pair j < rot_dim / 2 of a head's dims, with
+ * phi = positions[axis_of[j]][t] * inv_freq[j]:
+ *   y[a] = scale * (x[a] cos phi - x[b] sin phi),  y[b] = scale * (x[b] cos phi + x[a] sin phi),
+ * (a, b) = (j, j + rot_dim / 2), or (2 j, 2 j + 1) where interleaved; dims from rot_dim on are
+ * copied. Text has one axis; images and video have three (time, height, width), each turning
+ * its own pairs. Angles are reduced in 64 bits (positions of any size, negative ones
+ * included), products and sums are 32-bit, each output is rounded once to bf16.
+ * positions: int32 [num_axes][rows], an axis every pos_stride elements. slot_map: int64 [rows],
+ * block * block_size + slot as pkv_extend_tables writes it; a row whose slot is outside the pool
+ * (-1: padding) is skipped, in q_out too. Slots must be distinct and their blocks private to
+ * their sequences. No other byte of the pool changes. q_out: bf16 [rows][num_q_heads][head_dim]
+ * with its own row stride; it may be q itself (same address and stride). Addresses are 16-byte
+ * aligned, row strides of q, k_new, v_new and q_out multiples of 8 elements that hold a row. At
+ * most 2^28 rows. */
+#define PKV_ROPE_MAX_AXES 4
+typedef struct {
+  int32_t rot_dim;      /* dims turned: 0 .. head_dim, a multiple of 16 */
+  int32_t num_axes;     /* 1 .. PKV_ROPE_MAX_AXES */
+  int32_t interleaved;  /* 0: dim j pairs with j + rot_dim / 2; 1: neighbours pair */
+  float scale;          /* factor of the turned dims (1: none), finite */
+  uint8_t axis_of[64];  /* [rot_dim / 2], each below num_axes */
+  double inv_freq[64];  /* [rot_dim / 2], radians per position, finite */
+} pkv_rope;
+pkv_status pkv_rope_append(const pkv_paged_kv* kv, const pkv_rope* rope, const void* q,
+                           int64_t q_stride, int32_t num_q_heads, const void* k_new,
+                           int64_t k_stride, const void* v_new, int64_t v_stride,
+                           const int64_t* slot_map, const int32_t* positions,
+                           int64_t pos_stride, int32_t rows, void* q_out, int64_t q_out_stride,
+                           void* stream);
+
 /* Paged gather (test support): copies the first lens[i] tokens of every sequence out of the
  * pool into contiguous k_out / v_out, bf16 [sum lens][num_kv_heads][head_dim], sequence i
  * starting at row cu_lens[i] (int32 [num_seqs + 1]). Bit-exact. max_len (host) >= every

@@ -35,7 +35,8 @@ SANITIZE_FLAGS = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitiz
 ARCH = "gfx950"
 
 SOURCES = ["pool.cpp", "sched.cpp", "api.cpp", "kv_copy.hip", "block_copy.hip", "decode.hip",
-           "prefill.hip", "mixed.hip", "validate.hip", "tables.hip"]
+           "prefill.hip", "mixed.hip", "validate.hip", "tables.hip",
+           "rope.hip"]
 
 
 # compiler flags of the host and the device code

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <atomic>
+#include <cmath>
 #include <cstdlib>
 #include <cstring>
 #include <string>
@@ -89,18 +90,20 @@ pkv_status check_metadata(const char* fn, const MetaCheck* checks, int n, hipStr
   std::string what;
   if (bad & kMetaBadBlockId) what += " a block id outside the pool;";
   if (bad & kMetaBadLength) what += " a length outside its host maximum or the table;";
+  if (bad & kMetaBadSlot) what += " a slot outside the pool;";
   if (bad & kMetaBadOffsets) what += " token offsets not starting at 0, decreasing or not ending at the total;";
   std::string batch;
   if (n > 1) batch = which == 0 ? " of the prefill batch" : " of the decode batch";
   return fail(PKV_ERR_BAD_METADATA, std::string(fn) + ": PKV_DEBUG_VALIDATE refused the call:" +
-                                        what + " first offending sequence " +
+                                        what + " first offending " +
+                                        (checks[0].mode == kMetaSlots ? "row " : "sequence ") +
                                         std::to_string(seq) + batch);
 }
 
 MetaCheck meta(int32_t mode, const KvView& view, const int32_t* tables, int32_t max_blocks,
                const int32_t* lens, const int32_t* cu, int32_t num_seqs, int64_t total,
                int64_t max_len, int64_t max_total) {
-  MetaCheck c;
+  MetaCheck c{};
   c.mode = mode;
   c.tables = tables;
   c.max_blocks = max_blocks;
@@ -482,6 +485,82 @@ pkv_status pkv_extend_tables(int32_t* block_tables, int32_t max_blocks,
                      num_free,     free_used,     free_used_out, cu_new_lens, seq_lens, status,
                      max_rows,     slot_map,      row_seq,     positions, row_lens};
   return launched(launch_extend_tables(a, static_cast<hipStream_t>(stream)), fn);
+}
+
+pkv_status pkv_rope_append(const pkv_paged_kv* kv, const pkv_rope* rope, const void* q,
+                           int64_t q_stride, int32_t num_q_heads, const void* k_new,
+                           int64_t k_stride, const void* v_new, int64_t v_stride,
+                           const int64_t* slot_map, const int32_t* positions,
+                           int64_t pos_stride, int32_t rows, void* q_out, int64_t q_out_stride,
+                           void* stream) {
+  const char* fn = "pkv_rope_append";
+  const std::string f(fn);
+  KvView view;
+  pkv_status st = check_kv(kv, fn, &view);
+  if (st != PKV_OK) return st;
+  if (num_q_heads <= 0 || num_q_heads % view.hkv != 0)
+    return fail(PKV_ERR_UNSUPPORTED_SHAPE,
+                f + ": num_q_heads must be a positive multiple of num_kv_heads");
+  if (rope == nullptr) return fail(PKV_ERR_INVALID_ARG, f + ": rope is NULL");
+  if (rope->rot_dim < 0 || rope->rot_dim > view.head_dim || rope->rot_dim % 16 != 0)
+    return fail(PKV_ERR_UNSUPPORTED_SHAPE,
+                f + ": rot_dim must be a multiple of 16, at most head_dim");
+  if (rope->num_axes < 1 || rope->num_axes > PKV_ROPE_MAX_AXES)
+    return fail(PKV_ERR_INVALID_ARG, f + ": num_axes must be 1 to 4");
+  if (!std::isfinite(rope->scale)) return fail(PKV_ERR_INVALID_ARG, f + ": scale is not finite");
+  for (int j = 0; j < rope->rot_dim / 2; ++j) {
+    if (rope->axis_of[j] >= rope->num_axes)
+      return fail(PKV_ERR_INVALID_ARG, f + ": axis_of names an axis past num_axes");
+    if (!std::isfinite(rope->inv_freq[j]))
+      return fail(PKV_ERR_INVALID_ARG, f + ": inv_freq is not finite");
+  }
+  if (rows < 0) return fail(PKV_ERR_INVALID_ARG, f + ": negative size");
+  if (rows == 0) return ok();
+  if (rows > (1 << 28)) return fail(PKV_ERR_INVALID_ARG, f + ": more than 2^28 rows");
+  if (q == nullptr || k_new == nullptr || v_new == nullptr || slot_map == nullptr ||
+      q_out == nullptr || (positions == nullptr && rope->rot_dim > 0))
+    return fail(PKV_ERR_INVALID_ARG, f + ": NULL pointer");
+  if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(q_out))
+    return fail(PKV_ERR_INVALID_ARG, f + ": q / k_new / v_new / q_out must be 16-byte aligned");
+  const int64_t q_row = (int64_t)num_q_heads * view.head_dim;
+  const int64_t kv_row = (int64_t)view.hkv * view.head_dim;
+  if (q_stride < q_row || q_out_stride < q_row || k_stride < kv_row || v_stride < kv_row ||
+      (q_stride | q_out_stride | k_stride | v_stride) & 7)
+    return fail(PKV_ERR_INVALID_ARG,
+                f + ": row strides must be multiples of 8 elements that hold a row");
+  if (rope->num_axes > 1 && pos_stride < rows)
+    return fail(PKV_ERR_INVALID_ARG, f + ": pos_stride is below rows");
+  {
+    MetaCheck c = meta(kMetaSlots, view, nullptr, 0, nullptr, nullptr, rows, -1, 0, 0);
+    c.slots = slot_map;
+    if ((st = check_metadata(fn, &c, 1, static_cast<hipStream_t>(stream))) != PKV_OK) return st;
+  }
+  RopeArgs a{};
+  a.q = static_cast<const uint16_t*>(q);
+  a.k = static_cast<const uint16_t*>(k_new);
+  a.v = static_cast<const uint16_t*>(v_new);
+  a.q_out = static_cast<uint16_t*>(q_out);
+  a.k_cache = view.k;
+  a.v_cache = view.v;
+  a.slot_map = slot_map;
+  a.positions = positions;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.q_out_stride = q_out_stride;
+  a.pos_stride = pos_stride;
+  a.rows = rows;
+  a.hq = num_q_heads;
+  a.hkv = view.hkv;
+  a.num_blocks = view.num_blocks;
+  a.rot_dim = rope->rot_dim;
+  a.interleaved = rope->interleaved != 0;
+  a.scale = rope->scale;
+  for (int j = 0; j < rope->rot_dim / 2; ++j) {
+    a.axis_of[j] = rope->axis_of[j];
+    a.turns[j] = rope->inv_freq[j] / 6.283185307179586476925;
+  }
+  return launched(launch_rope_append(a, view.head_dim, static_cast<hipStream_t>(stream)), fn);
 }
 
 }  // extern "C"

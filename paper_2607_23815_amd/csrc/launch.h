@@ -51,6 +51,27 @@ struct ExtendArgs {
 };
 hipError_t launch_extend_tables(const ExtendArgs& a, hipStream_t stream);
 
+// Rotary positions and append (pkv_rope_append). Strides are in elements (rows of q, k, v and
+// q_out, axes of positions); turns[j] = inv_freq[j] / (2 pi).
+struct RopeArgs {
+  const uint16_t* q;
+  const uint16_t* k;
+  const uint16_t* v;
+  uint16_t* q_out;
+  uint16_t* k_cache;
+  uint16_t* v_cache;
+  const int64_t* slot_map;
+  const int32_t* positions;
+  int64_t q_stride, k_stride, v_stride, q_out_stride, pos_stride;
+  int64_t rows;
+  int32_t hq, hkv, num_blocks, rot_dim, interleaved;
+  int32_t window;  // rows of a workgroup (set by the launch)
+  float scale;
+  uint8_t axis_of[64];
+  double turns[64];
+};
+hipError_t launch_rope_append(RopeArgs a, int head_dim, hipStream_t stream);
+
 hipError_t launch_copy_blocks(const KvView& kv, const int32_t* pairs, int32_t num_pairs,
                               hipStream_t stream);
 
@@ -121,9 +142,11 @@ hipError_t decode_scratch(void** ptr);
 // `total`), each sequence's new tokens at most `max_len` and cached + new at most
 // `max_total`; for decode, `lens` are the sequence lengths (1 .. max_len); for gather, `lens`
 // the gathered lengths (at most max_len, equal to the cu steps). Every table entry the call
-// reads or writes must name a pool block.
-enum : int32_t { kMetaAppend = 0, kMetaPrefill = 1, kMetaDecode = 2, kMetaGather = 3 };
-enum : uint32_t { kMetaBadBlockId = 1u, kMetaBadLength = 2u, kMetaBadOffsets = 4u };
+// reads or writes must name a pool block. For slots, a row stands where a sequence does.
+enum : int32_t { kMetaAppend = 0, kMetaPrefill = 1, kMetaDecode = 2, kMetaGather = 3,
+                 kMetaSlots = 4 };
+enum : uint32_t { kMetaBadBlockId = 1u, kMetaBadLength = 2u, kMetaBadOffsets = 4u,
+                  kMetaBadSlot = 8u };
 struct MetaCheck {
   int32_t mode;
   const int32_t* tables;
@@ -135,6 +158,7 @@ struct MetaCheck {
   int64_t total;      // cu[num_seqs] must equal it (< 0: not checked)
   int64_t max_len;
   int64_t max_total;
+  const int64_t* slots;  // kMetaSlots: [num_seqs] rows' slots, each -1 or within the pool
 };
 // Runs the checks in order on `stream` and waits for each; *bad = the failed check's bits
 // (0 if all pass), *first_seq its lowest offending sequence, *which its index.

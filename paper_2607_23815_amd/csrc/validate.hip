@@ -18,6 +18,7 @@ namespace pkv {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kBlock = 16;  // tokens per KV block
 
 __global__ __launch_bounds__(64) void validate_reset_kernel(uint32_t* word) {
   if (threadIdx.x == 0) {
@@ -31,6 +32,14 @@ __global__ __launch_bounds__(kThreads) void validate_kernel(MetaCheck c, uint32_
   if (i >= c.num_seqs) return;
   uint32_t bad = 0u;
   int64_t e0 = 0, e1 = 0;  // table entries [e0, e1) the call touches
+  if (c.mode == kMetaSlots) {
+    const int64_t s = c.slots[i];
+    if (s < -1 || s >= (int64_t)c.num_blocks * kBlock) {
+      atomicOr(&word[0], (uint32_t)kMetaBadSlot);
+      atomicMin(reinterpret_cast<int*>(&word[1]), i);
+    }
+    return;
+  }
   if (c.mode == kMetaDecode) {
     const int64_t len = c.lens[i];
     if (len < 1 || len > c.max_len) bad |= kMetaBadLength;

@@ -47,6 +47,15 @@ class PagedKV(ctypes.Structure):
                 ("block_size", c_int32), ("num_kv_heads", c_int32), ("head_dim", c_int32)]
 
 
+PKV_ROPE_MAX_AXES = 4
+
+
+class Rope(ctypes.Structure):
+    _fields_ = [("rot_dim", c_int32), ("num_axes", c_int32), ("interleaved", c_int32),
+                ("scale", c_float), ("axis_of", ctypes.c_uint8 * 64),
+                ("inv_freq", ctypes.c_double * 64)]
+
+
 class PoolStats(ctypes.Structure):
     _fields_ = [("num_free", c_int32), ("num_entries", c_int32), ("cached_blocks", c_int32),
                 ("pinned_entries", c_int32), ("eviction", c_int32), ("pinning", c_int32),
@@ -147,6 +156,9 @@ _SIGS = {
                                       c_void_p, c_size_t, c_void_p]),
     "pkv_extend_tables": (c_int32, [c_void_p, c_int32, c_void_p, c_void_p, c_int32, c_void_p,
                                     c_int32] + [c_void_p] * 5 + [c_int32] + [c_void_p] * 5),
+    "pkv_rope_append": (c_int32, [ctypes.POINTER(PagedKV), ctypes.POINTER(Rope), c_void_p, c_int64,
+                                  c_int32, c_void_p, c_int64, c_void_p, c_int64, c_void_p,
+                                  c_void_p, c_int64, c_int32, c_void_p, c_int64, c_void_p]),
     "pkv_gather_kv": (c_int32, [ctypes.POINTER(PagedKV), c_void_p, c_int32, c_void_p, c_void_p,
                                 c_int32, c_int32, c_void_p, c_void_p, c_void_p]),
 }
@@ -648,6 +660,64 @@ def pkv_extend_tables(block_tables, cached_lens, new_lens, free_blocks, free_use
         None if row_seq is None else _ptr(row_seq, "row_seq", i32, dev),
         None if positions is None else _ptr(positions, "positions", i32, dev),
         None if row_lens is None else _ptr(row_lens, "row_lens", i32, dev), _stream(stream)))
+
+
+def rope_spec(inv_freq, axis_of=None, interleaved=False, scale=1.0, num_axes=None) -> Rope:
+    """How heads are turned: inv_freq[j] radians per position for pair j (2 * len(inv_freq) dims
+    are turned), axis_of[j] the axis of positions that turns it (None: one axis). num_axes: the
+    positions' axes (None: up to the last that axis_of names)."""
+    freqs = [float(f) for f in inv_freq]
+    axes = [0] * len(freqs) if axis_of is None else [int(a) for a in axis_of]
+    if len(freqs) > 64 or len(axes) != len(freqs):
+        raise ValueError("inv_freq and axis_of must have the same length, at most 64")
+    if axes and not (min(axes) >= 0 and max(axes) < PKV_ROPE_MAX_AXES):
+        raise ValueError(f"axis_of must name axes 0 to {PKV_ROPE_MAX_AXES - 1}")
+    r = Rope(2 * len(freqs), num_axes or max(axes, default=0) + 1, int(bool(interleaved)), float(scale))
+    r.axis_of[:len(axes)] = axes
+    r.inv_freq[:len(freqs)] = freqs
+    return r
+
+
+def _rows_ptr(t, name, heads, dim, dev):
+    """bf16 [rows][heads][dim] whose rows may lie apart: address and row stride."""
+    if not isinstance(t, _Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a GPU tensor (the library has no CPU path)")
+    if t.dtype is not _torch.bfloat16:
+        raise TypeError(f"{name} must be {_torch.bfloat16}, got {t.dtype}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on device {t.get_device()}, the current device is {dev}")
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
+        raise ValueError(f"{name} must be [rows][{heads}][{dim}]")
+    s0, s1, s2 = t.stride()
+    if s2 != 1 or (s1 != dim and heads > 1):
+        raise ValueError(f"{name} must have contiguous heads")
+    return t.data_ptr(), s0 if t.shape[0] > 1 else heads * dim
+
+
+def pkv_rope_append(k_cache, v_cache, q, k_new, v_new, slot_map, positions, rope: Rope, q_out,
+                    stream=None) -> None:
+    """q [rows][Hq][D] turned into q_out (which may be q), k_new and v_new [rows][Hkv][D] turned
+    and appended at slot_map (int64 [rows]); their rows may lie apart (views of one fused
+    projection). positions: int32 [rows], or [axes][rows] where rope has several axes."""
+    torch = _torch or _get_torch()
+    dev = _device(stream)
+    kv = paged_kv(k_cache, v_cache)
+    if k_cache.get_device() != dev or v_cache.get_device() != dev:
+        raise ValueError(f"k_cache / v_cache are not on the current device {dev}")
+    hkv, d = kv.num_kv_heads, kv.head_dim
+    n, hq = q.shape[0], q.shape[1]
+    if not (k_new.shape[0] == v_new.shape[0] == q_out.shape[0] == slot_map.numel() == n):
+        raise ValueError("q, k_new, v_new, q_out and slot_map must have the same number of rows")
+    if positions.numel() != rope.num_axes * n or positions.shape[-1] != n:
+        raise ValueError(f"positions must be [{rope.num_axes}][rows]")
+    qp, qs = _rows_ptr(q, "q", hq, d, dev)
+    kp, ks = _rows_ptr(k_new, "k_new", hkv, d, dev)
+    vp, vs = _rows_ptr(v_new, "v_new", hkv, d, dev)
+    op, os_ = _rows_ptr(q_out, "q_out", hq, d, dev)
+    _check(_lib.pkv_rope_append(
+        ctypes.byref(kv), ctypes.byref(rope), qp, qs, hq, kp, ks, vp, vs,
+        _ptr(slot_map, "slot_map", torch.int64, dev),
+        _ptr(positions, "positions", torch.int32, dev), n, n, op, os_, _stream(stream)))
 
 
 def alloc_workspace(nbytes: int, device="cuda"):

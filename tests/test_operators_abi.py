@@ -36,6 +36,52 @@ def test_extend_tables_refuses(lib, bad):
     refused(lib, lib.PKV_ERR_INVALID_ARG, _extend(lib, **bad), "pkv_extend_tables")
 
 
+def _kv(lib, head_dim=128, block_size=16, hkv=2):
+    return lib.PagedKV(0x1000, 0x2000, 10, block_size, hkv, head_dim)
+
+
+def _rope(lib, kv=None, rope=None, **kw):
+    a = dict(q=FAKE, q_stride=512, hq=4, k=FAKE, k_stride=256, v=FAKE, v_stride=256, slots=FAKE,
+             positions=FAKE, pos_stride=5, rows=5, q_out=FAKE, q_out_stride=512)
+    a.update(kw)
+    rope = lib.rope_spec([1.0] * 64, axis_of=[0, 1] * 32) if rope is None else rope
+    return lib._lib.pkv_rope_append(ctypes.byref(kv or _kv(lib)),
+                                    ctypes.byref(rope) if rope else None, *a.values(), None)
+
+
+@pytest.mark.parametrize("bad", [
+    dict(q=None), dict(k=None), dict(v=None), dict(slots=None), dict(positions=None),
+    dict(q_out=None), dict(q=ctypes.c_void_p(0x3008)), dict(k=ctypes.c_void_p(0x3002)),
+    dict(v=ctypes.c_void_p(0x3004)), dict(q_out=ctypes.c_void_p(0x3008)), dict(q_stride=504),
+    dict(q_stride=516), dict(k_stride=248), dict(v_stride=257), dict(q_out_stride=-512),
+    dict(pos_stride=4), dict(rows=-1), dict(rows=2**28 + 1)])
+def test_rope_append_refuses(lib, bad):
+    refused(lib, lib.PKV_ERR_INVALID_ARG, _rope(lib, **bad), "pkv_rope_append")
+
+
+def test_rope_append_refuses_shapes(lib):
+    shape = lib.PKV_ERR_UNSUPPORTED_SHAPE
+    refused(lib, shape, _rope(lib, hq=3), "num_q_heads")
+    refused(lib, shape, _rope(lib, hq=0), "num_q_heads")
+    refused(lib, shape, _rope(lib, kv=_kv(lib, 96)), "head_dim")
+    refused(lib, shape, _rope(lib, kv=_kv(lib, 128, 32)), "block_size")
+    refused(lib, shape, _rope(lib, rope=lib.rope_spec([1.0] * 9)), "rot_dim")
+    refused(lib, shape, _rope(lib, kv=_kv(lib, 64)), "rot_dim")
+    arg = lib.PKV_ERR_INVALID_ARG
+    refused(lib, arg, _rope(lib, rope=False), "rope is NULL")
+    refused(lib, arg, _rope(lib, rope=lib.rope_spec([1.0] * 8, scale=float("nan"))), "scale")
+    refused(lib, arg, _rope(lib, rope=lib.rope_spec([float("inf")] * 8)), "inv_freq")
+    refused(lib, arg, _rope(lib, rope=lib.rope_spec([1.0] * 8, axis_of=[1] * 8, num_axes=1)),
+            "axis_of")
+    refused(lib, arg, _rope(lib, rope=lib.rope_spec([1.0] * 8, num_axes=5)), "num_axes")
+    refused(lib, arg, lib._lib.pkv_rope_append(None, *[None] * 2, 0, 4, None, 0, None, 0, None,
+                                               None, 0, 0, None, 0, None), "kv is NULL")
+    assert _rope(lib, rows=0, q=None, k=None, v=None, slots=None) == lib.PKV_OK
+    for freqs, axes in (([1.0] * 65, None), ([1.0] * 8, [0] * 7), ([1.0], [4]), ([1.0], [-1])):
+        with pytest.raises(ValueError):
+            lib.rope_spec(freqs, axis_of=axes)
+
+
 def test_binding_refuses_host_tensors(lib):
     import torch
     if torch.cuda.is_available():
