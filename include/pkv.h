@@ -433,6 +433,20 @@ pkv_status pkv_rope_append(const pkv_paged_kv* kv, const pkv_rope* rope, const v
                            int64_t pos_stride, int32_t rows, void* q_out, int64_t q_out_stride,
                            void* stream);
 
+/* Key bounds per block, for pkv_select_blocks: bounds is bf16
+ * [num_blocks][num_kv_heads][2][head_dim], caller-allocated and 16-byte aligned like the pool;
+ * [block][h][0][d] is the largest and [block][h][1][d] the smallest value of dim d over the keys
+ * that block holds for kv head h (its filled slots; a NaN among them makes both NaN). The call,
+ * made after a step's append with the append's metadata, recomputes the bounds of every block
+ * that holds new tokens of the step: blocks cached_lens[i] / 16 .. (cached_lens[i] + N_i - 1) / 16
+ * of sequence i, N_i = cu_new_lens[i+1] - cu_new_lens[i]; the others stay. Bounds belong to the
+ * physical block, so sequences that share blocks share their bounds (after pkv_copy_blocks a
+ * copy's bounds come with the append that follows it). max_new_len (host) >= every N_i. */
+pkv_status pkv_block_bounds(const pkv_paged_kv* kv, void* bounds, const int32_t* block_tables,
+                            int32_t max_blocks, const int32_t* cached_lens,
+                            const int32_t* cu_new_lens, int32_t num_seqs, int32_t max_new_len,
+                            void* stream);
+
 /* Paged gather (test support): copies the first lens[i] tokens of every sequence out of the
  * pool into contiguous k_out / v_out, bf16 [sum lens][num_kv_heads][head_dim], sequence i
  * starting at row cu_lens[i] (int32 [num_seqs + 1]). Bit-exact. max_len (host) >= every

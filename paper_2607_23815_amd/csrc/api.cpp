@@ -563,4 +563,34 @@ pkv_status pkv_rope_append(const pkv_paged_kv* kv, const pkv_rope* rope, const v
   return launched(launch_rope_append(a, view.head_dim, static_cast<hipStream_t>(stream)), fn);
 }
 
+pkv_status pkv_block_bounds(const pkv_paged_kv* kv, void* bounds, const int32_t* block_tables,
+                            int32_t max_blocks, const int32_t* cached_lens,
+                            const int32_t* cu_new_lens, int32_t num_seqs, int32_t max_new_len,
+                            void* stream) {
+  const char* fn = "pkv_block_bounds";
+  KvView view;
+  pkv_status st = check_kv(kv, fn, &view);
+  if (st != PKV_OK) return st;
+  if (num_seqs < 0 || max_new_len < 0 || max_blocks < 0)
+    return fail(PKV_ERR_INVALID_ARG, "pkv_block_bounds: negative size");
+  if (num_seqs == 0 || max_new_len == 0 || max_blocks == 0) return ok();
+  if (bounds == nullptr || block_tables == nullptr || cached_lens == nullptr ||
+      cu_new_lens == nullptr)
+    return fail(PKV_ERR_INVALID_ARG, "pkv_block_bounds: NULL pointer");
+  if (!aligned16(bounds))
+    return fail(PKV_ERR_INVALID_ARG, "pkv_block_bounds: bounds must be 16-byte aligned");
+  if (num_seqs > kMaxGridZ)
+    return fail(PKV_ERR_INVALID_ARG, "pkv_block_bounds: more than 65535 sequences per call");
+  {
+    const MetaCheck c = meta(kMetaAppend, view, block_tables, max_blocks, cached_lens,
+                             cu_new_lens, num_seqs, -1, max_new_len,
+                             (int64_t)max_blocks * kSupportedBlockSize);
+    if ((st = check_metadata(fn, &c, 1, static_cast<hipStream_t>(stream))) != PKV_OK) return st;
+  }
+  return launched(launch_block_bounds(view, static_cast<uint16_t*>(bounds), block_tables,
+                                      max_blocks, cached_lens, cu_new_lens, num_seqs,
+                                      max_new_len, static_cast<hipStream_t>(stream)),
+                  fn);
+}
+
 }  // extern "C"

@@ -72,6 +72,12 @@ struct RopeArgs {
 };
 hipError_t launch_rope_append(RopeArgs a, int head_dim, hipStream_t stream);
 
+// Key bounds of the blocks that hold new tokens (pkv_block_bounds).
+hipError_t launch_block_bounds(const KvView& kv, uint16_t* bounds, const int32_t* block_tables,
+                               int32_t max_blocks, const int32_t* cached_lens,
+                               const int32_t* cu_new_lens, int32_t num_seqs, int32_t max_new_len,
+                               hipStream_t stream);
+
 hipError_t launch_copy_blocks(const KvView& kv, const int32_t* pairs, int32_t num_pairs,
                               hipStream_t stream);
 

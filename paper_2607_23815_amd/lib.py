@@ -159,6 +159,8 @@ _SIGS = {
     "pkv_rope_append": (c_int32, [ctypes.POINTER(PagedKV), ctypes.POINTER(Rope), c_void_p, c_int64,
                                   c_int32, c_void_p, c_int64, c_void_p, c_int64, c_void_p,
                                   c_void_p, c_int64, c_int32, c_void_p, c_int64, c_void_p]),
+    "pkv_block_bounds": (c_int32, [ctypes.POINTER(PagedKV), c_void_p, c_void_p, c_int32, c_void_p,
+                                   c_void_p, c_int32, c_int32, c_void_p]),
     "pkv_gather_kv": (c_int32, [ctypes.POINTER(PagedKV), c_void_p, c_int32, c_void_p, c_void_p,
                                 c_int32, c_int32, c_void_p, c_void_p, c_void_p]),
 }
@@ -662,6 +664,13 @@ def pkv_extend_tables(block_tables, cached_lens, new_lens, free_blocks, free_use
         None if row_lens is None else _ptr(row_lens, "row_lens", i32, dev), _stream(stream)))
 
 
+def _paged_kv_on(k_cache, v_cache, dev) -> PagedKV:
+    kv = paged_kv(k_cache, v_cache)
+    if k_cache.get_device() != dev or v_cache.get_device() != dev:
+        raise ValueError(f"k_cache / v_cache are not on the current device {dev}")
+    return kv
+
+
 def rope_spec(inv_freq, axis_of=None, interleaved=False, scale=1.0, num_axes=None) -> Rope:
     """How heads are turned: inv_freq[j] radians per position for pair j (2 * len(inv_freq) dims
     are turned), axis_of[j] the axis of positions that turns it (None: one axis). num_axes: the
@@ -701,9 +710,7 @@ def pkv_rope_append(k_cache, v_cache, q, k_new, v_new, slot_map, positions, rope
     projection). positions: int32 [rows], or [axes][rows] where rope has several axes."""
     torch = _torch or _get_torch()
     dev = _device(stream)
-    kv = paged_kv(k_cache, v_cache)
-    if k_cache.get_device() != dev or v_cache.get_device() != dev:
-        raise ValueError(f"k_cache / v_cache are not on the current device {dev}")
+    kv = _paged_kv_on(k_cache, v_cache, dev)
     hkv, d = kv.num_kv_heads, kv.head_dim
     n, hq = q.shape[0], q.shape[1]
     if not (k_new.shape[0] == v_new.shape[0] == q_out.shape[0] == slot_map.numel() == n):
@@ -718,6 +725,27 @@ def pkv_rope_append(k_cache, v_cache, q, k_new, v_new, slot_map, positions, rope
         ctypes.byref(kv), ctypes.byref(rope), qp, qs, hq, kp, ks, vp, vs,
         _ptr(slot_map, "slot_map", torch.int64, dev),
         _ptr(positions, "positions", torch.int32, dev), n, n, op, os_, _stream(stream)))
+
+
+def pkv_block_bounds(k_cache, v_cache, bounds, block_tables, cached_lens, cu_new_lens,
+                     max_new_len: int, stream=None) -> None:
+    """The key bounds (bf16 [num_blocks][Hkv][2][D], largest then smallest) of the blocks that
+    hold new tokens."""
+    torch = _torch or _get_torch()
+    dev = _device(stream)
+    kv = _paged_kv_on(k_cache, v_cache, dev)
+    if bounds.shape != (kv.num_blocks, kv.num_kv_heads, 2, kv.head_dim):
+        raise ValueError("bounds must be [num_blocks][Hkv][2][D]")
+    b = cached_lens.shape[0]
+    if block_tables.dim() != 2 or block_tables.shape[0] != b or cu_new_lens.numel() != b + 1:
+        raise ValueError("block_tables, cached_lens and cu_new_lens must have a row, an entry and "
+                         "a step per sequence")
+    i32 = torch.int32
+    _check(_lib.pkv_block_bounds(
+        ctypes.byref(kv), _ptr(bounds, "bounds", torch.bfloat16, dev),
+        _ptr(block_tables, "block_tables", i32, dev), block_tables.shape[1],
+        _ptr(cached_lens, "cached_lens", i32, dev), _ptr(cu_new_lens, "cu_new_lens", i32, dev), b,
+        int(max_new_len), _stream(stream)))
 
 
 def alloc_workspace(nbytes: int, device="cuda"):

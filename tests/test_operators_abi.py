@@ -82,6 +82,22 @@ def test_rope_append_refuses_shapes(lib):
             lib.rope_spec(freqs, axis_of=axes)
 
 
+def _bounds(lib, kv=None, **kw):
+    a = dict(bounds=FAKE, tables=FAKE, max_blocks=4, cached=FAKE, cu=FAKE, num_seqs=2, max_new=3)
+    a.update(kw)
+    return lib._lib.pkv_block_bounds(ctypes.byref(kv or _kv(lib)), *a.values(), None)
+
+
+def test_block_bounds_refuses(lib):
+    for bad in (dict(bounds=None), dict(tables=None), dict(cached=None), dict(cu=None),
+                dict(bounds=ctypes.c_void_p(0x3008)), dict(max_blocks=-1), dict(num_seqs=-1),
+                dict(max_new=-1), dict(num_seqs=65536)):
+        refused(lib, lib.PKV_ERR_INVALID_ARG, _bounds(lib, **bad), "pkv_block_bounds")
+    refused(lib, lib.PKV_ERR_UNSUPPORTED_SHAPE, _bounds(lib, kv=_kv(lib, 96)), "head_dim")
+    for empty in (dict(num_seqs=0), dict(max_new=0), dict(max_blocks=0)):
+        assert _bounds(lib, **empty) == lib.PKV_OK
+
+
 def test_binding_refuses_host_tensors(lib):
     import torch
     if torch.cuda.is_available():
