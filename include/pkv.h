@@ -447,6 +447,36 @@ pkv_status pkv_block_bounds(const pkv_paged_kv* kv, void* bounds, const int32_t*
                             const int32_t* cu_new_lens, int32_t num_seqs, int32_t max_new_len,
                             void* stream);
 
+/* Rows of a sparse read. pkv_select_blocks and pkv_sparse_attention work on rows, one query token
+ * each: row t of q (bf16 [rows][num_q_heads][head_dim]) belongs to sequence row_seq[t] (int32
+ * [rows]; NULL: row t is sequence t, rows == num_seqs, a decode step) and sees that sequence's
+ * first row_lens[t] keys (int32 [rows]). A decode step passes seq_lens; rows of longer suffixes
+ * take both arrays from pkv_extend_tables. A row whose row_seq is -1 is padding: nothing of it is
+ * written. num_q_heads / num_kv_heads <= 16; rows * num_kv_heads <= 2^23.
+ *
+ * Choice of blocks: for each row and kv head, the `blocks` of the row's
+ * ceil(row_lens[t] / block_size) blocks that matter most, by the most that any key within a
+ * block's bounds (pkv_block_bounds) could score for any of the group's query heads:
+ *   s[block] = max_h sum_d q[t][h][d] * (q[t][h][d] > 0 ? bounds[block][0][d] : bounds[block][1][d]).
+ * The first sink_blocks and the last recent_blocks (>= 1: the row's own block) are always taken,
+ * the others by falling s, equal ones by rising index; a block whose s is not finite comes first.
+ * The choice is by the exact value of s (its products summed in 64 bits), whatever the order in
+ * which the kernels sum. sel: int32 [rows][num_kv_heads][blocks] receives the chosen logical
+ * block indices in ascending order, then -1 where the row has fewer blocks.
+ * sink_blocks + recent_blocks <= blocks. max_len (host, at most 2^20) >= every row_lens[t];
+ * longer ones are cut to it. workspace: at least pkv_select_workspace_bytes (0 when max_len
+ * has no more than `blocks` blocks), 16-byte aligned, owned by the caller, not read back; calls
+ * that share one must not overlap. */
+pkv_status pkv_select_blocks(const void* bounds, int32_t num_blocks, int32_t num_kv_heads,
+                             int32_t head_dim, const void* q, int32_t num_q_heads,
+                             const int32_t* block_tables, int32_t max_blocks, int32_t num_seqs,
+                             const int32_t* row_seq, const int32_t* row_lens, int32_t rows,
+                             int32_t max_len, int32_t sink_blocks, int32_t recent_blocks,
+                             int32_t blocks, int32_t* sel, void* workspace,
+                             size_t workspace_bytes, void* stream);
+size_t pkv_select_workspace_bytes(int32_t rows, int32_t num_q_heads, int32_t num_kv_heads,
+                                  int32_t head_dim, int32_t max_len, int32_t blocks);
+
 /* Paged gather (test support): copies the first lens[i] tokens of every sequence out of the
  * pool into contiguous k_out / v_out, bf16 [sum lens][num_kv_heads][head_dim], sequence i
  * starting at row cu_lens[i] (int32 [num_seqs + 1]). Bit-exact. max_len (host) >= every

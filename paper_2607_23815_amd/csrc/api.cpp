@@ -96,7 +96,7 @@ pkv_status check_metadata(const char* fn, const MetaCheck* checks, int n, hipStr
   if (n > 1) batch = which == 0 ? " of the prefill batch" : " of the decode batch";
   return fail(PKV_ERR_BAD_METADATA, std::string(fn) + ": PKV_DEBUG_VALIDATE refused the call:" +
                                         what + " first offending " +
-                                        (checks[0].mode == kMetaSlots ? "row " : "sequence ") +
+                                        (checks[0].mode >= kMetaSlots ? "row " : "sequence ") +
                                         std::to_string(seq) + batch);
 }
 
@@ -204,6 +204,36 @@ pkv_status check_decode(const KvView& view, const char* fn, const void* q, int32
                 f + ": workspace missing, too small or not 16-byte aligned "
                     "(see pkv_decode_workspace_bytes)");
   return ok();
+}
+
+constexpr int64_t kMaxRowItems = int64_t(1) << 23;  // (row, kv head) pairs of a sparse read
+
+// Argument checks that both sparse calls make of their rows.
+pkv_status check_rows(const std::string& f, int32_t num_q_heads, int32_t hkv, const void* q,
+                      const int32_t* block_tables, int32_t max_blocks, int32_t num_seqs,
+                      const int32_t* row_seq, const int32_t* row_lens, int32_t rows,
+                      int32_t blocks, const void* sel, bool* empty) {
+  *empty = false;
+  if (num_q_heads <= 0 || num_q_heads % hkv != 0 || num_q_heads / hkv > 16)
+    return fail(PKV_ERR_UNSUPPORTED_SHAPE,
+                f + ": num_q_heads must be a multiple of num_kv_heads, with at most 16 query "
+                    "heads per kv head");
+  if (rows < 0 || num_seqs < 0 || max_blocks < 0 || blocks < 0)
+    return fail(PKV_ERR_INVALID_ARG, f + ": negative size");
+  if (rows == 0) {
+    *empty = true;
+    return ok();
+  }
+  if (row_seq == nullptr && rows != num_seqs)
+    return fail(PKV_ERR_INVALID_ARG, f + ": without row_seq, rows must equal num_seqs");
+  if (blocks == 0) return fail(PKV_ERR_INVALID_ARG, f + ": blocks must be > 0");
+  if (q == nullptr || row_lens == nullptr || sel == nullptr ||
+      (block_tables == nullptr && num_seqs > 0 && max_blocks > 0))
+    return fail(PKV_ERR_INVALID_ARG, f + ": NULL pointer");
+  if (!aligned16(q)) return fail(PKV_ERR_INVALID_ARG, f + ": q must be 16-byte aligned");
+  if ((int64_t)rows * hkv > kMaxRowItems)
+    return fail(PKV_ERR_INVALID_ARG, f + ": more than 2^23 rows x kv heads");
+  return PKV_OK;
 }
 
 }  // namespace
@@ -591,6 +621,76 @@ pkv_status pkv_block_bounds(const pkv_paged_kv* kv, void* bounds, const int32_t*
                                       max_blocks, cached_lens, cu_new_lens, num_seqs,
                                       max_new_len, static_cast<hipStream_t>(stream)),
                   fn);
+}
+
+size_t pkv_select_workspace_bytes(int32_t rows, int32_t num_q_heads, int32_t num_kv_heads,
+                                  int32_t head_dim, int32_t max_len, int32_t blocks) {
+  if (rows <= 0 || num_q_heads <= 0 || num_kv_heads <= 0 || head_dim <= 0 || max_len <= 0 ||
+      blocks <= 0 || (int64_t)rows * num_kv_heads > kMaxRowItems ||
+      max_len > kSelectMaxBlocks * kSupportedBlockSize)
+    return 0;
+  return select_workspace_bytes((int64_t)rows * num_kv_heads, max_len, blocks);
+}
+
+pkv_status pkv_select_blocks(const void* bounds, int32_t num_blocks, int32_t num_kv_heads,
+                             int32_t head_dim, const void* q, int32_t num_q_heads,
+                             const int32_t* block_tables, int32_t max_blocks, int32_t num_seqs,
+                             const int32_t* row_seq, const int32_t* row_lens, int32_t rows,
+                             int32_t max_len, int32_t sink_blocks, int32_t recent_blocks,
+                             int32_t blocks, int32_t* sel, void* workspace,
+                             size_t workspace_bytes, void* stream) {
+  const char* fn = "pkv_select_blocks";
+  const std::string f(fn);
+  if (num_blocks <= 0 || num_kv_heads <= 0)
+    return fail(PKV_ERR_INVALID_ARG, f + ": num_blocks and num_kv_heads must be positive");
+  if (head_dim != 64 && head_dim != 128)
+    return fail(PKV_ERR_UNSUPPORTED_SHAPE, f + ": head_dim must be 64 or 128");
+  bool empty = false;
+  pkv_status st = check_rows(f, num_q_heads, num_kv_heads, q, block_tables, max_blocks, num_seqs,
+                             row_seq, row_lens, rows, blocks, sel, &empty);
+  if (st != PKV_OK || empty) return st;
+  if (bounds == nullptr || !aligned16(bounds))
+    return fail(PKV_ERR_INVALID_ARG, f + ": bounds is NULL or not 16-byte aligned");
+  if (max_len < 0) return fail(PKV_ERR_INVALID_ARG, f + ": negative size");
+  if (max_len > kSelectMaxBlocks * kSupportedBlockSize)
+    return fail(PKV_ERR_INVALID_ARG, f + ": max_len is above 2^20");
+  if ((int64_t)max_blocks * kSupportedBlockSize < max_len)
+    return fail(PKV_ERR_INVALID_ARG, f + ": max_len exceeds max_blocks * block_size");
+  if (sink_blocks < 0 || recent_blocks < 1 || (int64_t)sink_blocks + recent_blocks > blocks)
+    return fail(PKV_ERR_INVALID_ARG,
+                f + ": need sink_blocks >= 0, recent_blocks >= 1 and their sum <= blocks");
+  const size_t need = select_workspace_bytes((int64_t)rows * num_kv_heads, max_len, blocks);
+  if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned16(workspace)))
+    return fail(PKV_ERR_INVALID_ARG,
+                f + ": workspace missing, too small or not 16-byte aligned "
+                    "(see pkv_select_workspace_bytes)");
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  {
+    KvView view{nullptr, nullptr, num_blocks, num_kv_heads, head_dim};
+    MetaCheck c = meta(kMetaRows, view, block_tables, max_blocks, row_lens, nullptr, rows, -1,
+                       max_len, 0);
+    c.row_seq = row_seq;
+    c.table_rows = num_seqs;
+    if ((st = check_metadata(fn, &c, 1, s)) != PKV_OK) return st;
+  }
+  SelectArgs a{};
+  a.bounds = static_cast<const uint16_t*>(bounds);
+  a.q = static_cast<const uint16_t*>(q);
+  a.tables = block_tables;
+  a.row_seq = row_seq;
+  a.row_lens = row_lens;
+  a.sel = sel;
+  a.rows = rows;
+  a.max_blocks = max_blocks;
+  a.num_seqs = num_seqs;
+  a.max_len = max_len;
+  a.hq = num_q_heads;
+  a.hkv = num_kv_heads;
+  a.num_blocks = num_blocks;
+  a.blocks = blocks;
+  a.sink = sink_blocks;
+  a.recent = recent_blocks;
+  return launched(launch_select_blocks(a, head_dim, workspace, s), fn);
 }
 
 }  // extern "C"

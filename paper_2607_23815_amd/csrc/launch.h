@@ -78,6 +78,27 @@ hipError_t launch_block_bounds(const KvView& kv, uint16_t* bounds, const int32_t
                                const int32_t* cu_new_lens, int32_t num_seqs, int32_t max_new_len,
                                hipStream_t stream);
 
+// The choice of blocks (pkv_select_blocks). Workspace, in floats: two halves of a 64-bit key per
+// (row, kv head, block) (the first is the 32-bit score before), then the largest |bound| per 16
+// blocks.
+constexpr int32_t kSelectMaxBlocks = 65536;  // blocks of a row
+struct SelectArgs {
+  const uint16_t* bounds;
+  const uint16_t* q;
+  const int32_t* tables;
+  const int32_t* row_seq;  // null: row i is sequence i
+  const int32_t* row_lens;
+  int32_t* sel;
+  int64_t rows;
+  int32_t max_blocks, num_seqs, max_len, hq, hkv, num_blocks, blocks, sink, recent;
+  int64_t stride;  // of a (row, kv head), in blocks (set by the launch, like the rest)
+  float* scores;
+  float* low;
+  float* tile_most;
+};
+size_t select_workspace_bytes(int64_t items, int32_t max_len, int32_t blocks);
+hipError_t launch_select_blocks(SelectArgs a, int head_dim, void* workspace, hipStream_t stream);
+
 hipError_t launch_copy_blocks(const KvView& kv, const int32_t* pairs, int32_t num_pairs,
                               hipStream_t stream);
 
@@ -148,9 +169,10 @@ hipError_t decode_scratch(void** ptr);
 // `total`), each sequence's new tokens at most `max_len` and cached + new at most
 // `max_total`; for decode, `lens` are the sequence lengths (1 .. max_len); for gather, `lens`
 // the gathered lengths (at most max_len, equal to the cu steps). Every table entry the call
-// reads or writes must name a pool block. For slots, a row stands where a sequence does.
+// reads or writes must name a pool block. For slots and
+// rows, a row stands where a sequence does.
 enum : int32_t { kMetaAppend = 0, kMetaPrefill = 1, kMetaDecode = 2, kMetaGather = 3,
-                 kMetaSlots = 4 };
+                 kMetaSlots = 4, kMetaRows = 5 };
 enum : uint32_t { kMetaBadBlockId = 1u, kMetaBadLength = 2u, kMetaBadOffsets = 4u,
                   kMetaBadSlot = 8u };
 struct MetaCheck {
@@ -165,6 +187,8 @@ struct MetaCheck {
   int64_t max_len;
   int64_t max_total;
   const int64_t* slots;  // kMetaSlots: [num_seqs] rows' slots, each -1 or within the pool
+  const int32_t* row_seq;  // kMetaRows: [num_seqs] rows' sequences, each -1 or below table_rows
+  int32_t table_rows;      // (null: row i is sequence i), lens their visible keys (0 .. max_len)
 };
 // Runs the checks in order on `stream` and waits for each; *bad = the failed check's bits
 // (0 if all pass), *first_seq its lowest offending sequence, *which its index.

@@ -40,7 +40,13 @@ __global__ __launch_bounds__(kThreads) void validate_kernel(MetaCheck c, uint32_
     }
     return;
   }
-  if (c.mode == kMetaDecode) {
+  int64_t seq = i;
+  if (c.mode == kMetaRows) {
+    if (c.row_seq != nullptr) seq = c.row_seq[i];
+    const int64_t len = c.lens[i];
+    if (seq < -1 || seq >= c.table_rows || len < 0 || len > c.max_len) bad |= kMetaBadLength;
+    if (!bad && seq >= 0) e1 = (len + 15) / 16;
+  } else if (c.mode == kMetaDecode) {
     const int64_t len = c.lens[i];
     if (len < 1 || len > c.max_len) bad |= kMetaBadLength;
     e1 = (len + 15) / 16;
@@ -69,7 +75,7 @@ __global__ __launch_bounds__(kThreads) void validate_kernel(MetaCheck c, uint32_
     e1 = c.max_blocks;
   }
   if (e0 < 0) e0 = 0;
-  const int32_t* row = c.tables + (size_t)i * c.max_blocks;
+  const int32_t* row = c.tables + (seq < 0 ? 0 : (size_t)seq * c.max_blocks);
   for (int64_t e = e0; e < e1; ++e) {
     const int32_t t = row[e];
     if (t < 0 || t >= c.num_blocks) {

@@ -161,6 +161,10 @@ _SIGS = {
                                   c_void_p, c_int64, c_int32, c_void_p, c_int64, c_void_p]),
     "pkv_block_bounds": (c_int32, [ctypes.POINTER(PagedKV), c_void_p, c_void_p, c_int32, c_void_p,
                                    c_void_p, c_int32, c_int32, c_void_p]),
+    "pkv_select_blocks": (c_int32, [c_void_p, c_int32, c_int32, c_int32, c_void_p, c_int32, c_void_p,
+                                    c_int32, c_int32, c_void_p, c_void_p] + [c_int32] * 5 +
+                          [c_void_p, c_void_p, c_size_t, c_void_p]),
+    "pkv_select_workspace_bytes": (c_size_t, [c_int32] * 6),
     "pkv_gather_kv": (c_int32, [ctypes.POINTER(PagedKV), c_void_p, c_int32, c_void_p, c_void_p,
                                 c_int32, c_int32, c_void_p, c_void_p, c_void_p]),
 }
@@ -746,6 +750,56 @@ def pkv_block_bounds(k_cache, v_cache, bounds, block_tables, cached_lens, cu_new
         _ptr(block_tables, "block_tables", i32, dev), block_tables.shape[1],
         _ptr(cached_lens, "cached_lens", i32, dev), _ptr(cu_new_lens, "cu_new_lens", i32, dev), b,
         int(max_new_len), _stream(stream)))
+
+
+def _workspace(t, dev):
+    """A call's workspace: its address and bytes (None: none)."""
+    if t is None:
+        return None, 0
+    return _ptr(t, "workspace", t.dtype, dev), t.numel() * t.element_size()
+
+
+def pkv_select_workspace_bytes(rows, num_q_heads, num_kv_heads, head_dim, max_len,
+                               blocks) -> int:
+    return int(_lib.pkv_select_workspace_bytes(rows, num_q_heads, num_kv_heads, head_dim, max_len,
+                                               blocks))
+
+
+def _check_rows(q, block_tables, row_lens, row_seq):
+    n = row_lens.numel()
+    if q.dim() != 3 or q.shape[0] != n or block_tables.dim() != 2:
+        raise ValueError("q must be [rows][Hq][D] with an entry of row_lens per row, block_tables "
+                         "[num_seqs][max_blocks]")
+    if n != (block_tables.shape[0] if row_seq is None else row_seq.numel()):
+        raise ValueError("row_seq must have an entry per row; without it row i is sequence i")
+    return n
+
+
+def pkv_select_blocks(bounds, q, block_tables, row_lens, max_len: int, sink_blocks: int,
+                      recent_blocks: int, sel, row_seq=None, workspace=None, stream=None) -> None:
+    """sel [rows][Hkv][blocks] receives, for each row of q [rows][Hq][D] and kv head, the logical
+    blocks chosen by their key bounds [num_blocks][Hkv][2][D], ascending, then -1."""
+    torch = _torch or _get_torch()
+    bf16, i32 = torch.bfloat16, torch.int32
+    dev = _device(stream)
+    if bounds.dim() != 4 or bounds.shape[2] != 2:
+        raise ValueError("bounds must be [num_blocks][Hkv][2][D]")
+    nb, hkv, _, d = bounds.shape
+    n = _check_rows(q, block_tables, row_lens, row_seq)
+    if sel.dim() != 3 or sel.shape[:2] != (n, hkv) or q.shape[2] != d:
+        raise ValueError("sel must be [rows][Hkv][blocks], and q's head dim the bounds'")
+    b, max_blocks = block_tables.shape
+    hq, blocks = q.shape[1], sel.shape[2]
+    if workspace is None:  # convenience for one-off calls; timed callers pass their own
+        workspace = alloc_workspace(pkv_select_workspace_bytes(n, hq, hkv, d, int(max_len),
+                                                               blocks))
+    ws, ws_bytes = _workspace(workspace, dev)
+    _check(_lib.pkv_select_blocks(
+        _ptr(bounds, "bounds", bf16, dev), nb, hkv, d, _ptr(q, "q", bf16, dev), hq,
+        _ptr(block_tables, "block_tables", i32, dev), max_blocks, b,
+        None if row_seq is None else _ptr(row_seq, "row_seq", i32, dev),
+        _ptr(row_lens, "row_lens", i32, dev), n, int(max_len), sink_blocks, recent_blocks, blocks,
+        _ptr(sel, "sel", i32, dev), ws, ws_bytes, _stream(stream)))
 
 
 def alloc_workspace(nbytes: int, device="cuda"):

@@ -98,6 +98,35 @@ def test_block_bounds_refuses(lib):
         assert _bounds(lib, **empty) == lib.PKV_OK
 
 
+def _select(lib, **kw):
+    a = dict(bounds=FAKE, num_blocks=100, hkv=2, d=128, q=FAKE, hq=8, tables=FAKE, max_blocks=64,
+             num_seqs=3, row_seq=FAKE, row_lens=FAKE, rows=5, max_len=1000, sink=1, recent=2,
+             blocks=8, sel=FAKE, ws=FAKE, ws_bytes=1 << 20)
+    a.update(kw)
+    return lib._lib.pkv_select_blocks(*a.values(), None)
+
+
+def test_select_blocks_refuses(lib):
+    arg, shape = lib.PKV_ERR_INVALID_ARG, lib.PKV_ERR_UNSUPPORTED_SHAPE
+    for bad in (dict(bounds=None), dict(q=None), dict(tables=None), dict(row_lens=None),
+                dict(sel=None), dict(bounds=ctypes.c_void_p(0x3002)),
+                dict(q=ctypes.c_void_p(0x3008)), dict(num_blocks=0), dict(hkv=0), dict(rows=-1),
+                dict(num_seqs=-1), dict(max_blocks=-1), dict(blocks=-1), dict(max_len=-1),
+                dict(blocks=0), dict(sink=-1), dict(recent=0), dict(sink=7), dict(recent=2**31 - 1),
+                dict(row_seq=None), dict(max_len=1025), dict(rows=2**22 + 1),
+                dict(max_len=2**20 + 1, max_blocks=2**17)):
+        refused(lib, arg, _select(lib, **bad), "pkv_select_blocks")
+    for bad in (dict(d=96), dict(hq=7), dict(hq=0), dict(hq=34)):
+        refused(lib, shape, _select(lib, **bad), "pkv_select_blocks")
+    need = lib.pkv_select_workspace_bytes(5, 8, 2, 128, 1000, 8)
+    assert need >= 5 * 2 * 63 * 8
+    for bad in (dict(ws=None), dict(ws_bytes=need - 1), dict(ws=ctypes.c_void_p(0x3004))):
+        refused(lib, arg, _select(lib, **bad), "workspace")
+    assert lib.pkv_select_workspace_bytes(5, 8, 2, 128, 128, 8) == 0  # every block is chosen
+    assert lib.pkv_select_workspace_bytes(5, 8, 2, 128, 2**20 + 1, 8) == 0
+    assert _select(lib, rows=0, q=None, sel=None) == lib.PKV_OK
+
+
 def test_binding_refuses_host_tensors(lib):
     import torch
     if torch.cuda.is_available():
