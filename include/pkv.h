@@ -477,6 +477,30 @@ pkv_status pkv_select_blocks(const void* bounds, int32_t num_blocks, int32_t num
 size_t pkv_select_workspace_bytes(int32_t rows, int32_t num_q_heads, int32_t num_kv_heads,
                                   int32_t head_dim, int32_t max_len, int32_t blocks);
 
+/* Attention over chosen blocks: row t's query heads of kv head h attend over the keys of the
+ * blocks that sel[t][h] (int32 [rows][num_kv_heads][blocks], as pkv_select_blocks writes it, or
+ * the caller's own choice) names, as far as the row sees them:
+ *   out[t][qh] = sum_p softmax_p(scale * <q[t][qh], K[p]>) V[p],
+ *   p < row_lens[t], p / block_size in sel[t][h],   h = qh / (num_q_heads / num_kv_heads),
+ * and lse[t][qh] = ln sum_p exp(scale * <q[t][qh], K[p]>) (float [rows][num_q_heads], or NULL).
+ * Entries of sel that name no block of the row (-1, or past its last) are passed over, as are
+ * table entries outside the pool; the others must differ from one another and may come in any
+ * order. Every block of a row listed, the result is pkv_decode_attention's up to the order of
+ * its sums. A row without a visible key (row_lens[t] 0, nothing listed), or whose scores are all
+ * -infinity, gives zeros and an LSE of -infinity. bf16 inputs, 32-bit sums, weights rounded to
+ * bf16 for the value product (as in decode), bf16 output. At most 65536 blocks are
+ * chosen for a row; row_lens has no such limit. workspace: at least pkv_sparse_workspace_bytes (0 where there are rows
+ * enough to fill the chip), 16-byte aligned, owned by the caller, not read back; calls that
+ * share one must not overlap. */
+pkv_status pkv_sparse_attention(const pkv_paged_kv* kv, const void* q, int32_t num_q_heads,
+                                const int32_t* block_tables, int32_t max_blocks,
+                                int32_t num_seqs, const int32_t* row_seq,
+                                const int32_t* row_lens, int32_t rows, const int32_t* sel,
+                                int32_t blocks, float scale, void* out, float* lse,
+                                void* workspace, size_t workspace_bytes, void* stream);
+size_t pkv_sparse_workspace_bytes(int32_t rows, int32_t num_q_heads, int32_t num_kv_heads,
+                                  int32_t head_dim, int32_t blocks);
+
 /* Paged gather (test support): copies the first lens[i] tokens of every sequence out of the
  * pool into contiguous k_out / v_out, bf16 [sum lens][num_kv_heads][head_dim], sequence i
  * starting at row cu_lens[i] (int32 [num_seqs + 1]). Bit-exact. max_len (host) >= every

@@ -36,7 +36,7 @@ ARCH = "gfx950"
 
 SOURCES = ["pool.cpp", "sched.cpp", "api.cpp", "kv_copy.hip", "block_copy.hip", "decode.hip",
            "prefill.hip", "mixed.hip", "validate.hip", "tables.hip",
-           "rope.hip", "bounds.hip", "select.hip"]
+           "rope.hip", "bounds.hip", "select.hip", "sparse.hip"]
 
 
 # compiler flags of the host and the device code

@@ -693,4 +693,69 @@ pkv_status pkv_select_blocks(const void* bounds, int32_t num_blocks, int32_t num
   return launched(launch_select_blocks(a, head_dim, workspace, s), fn);
 }
 
+size_t pkv_sparse_workspace_bytes(int32_t rows, int32_t num_q_heads, int32_t num_kv_heads,
+                                  int32_t head_dim, int32_t blocks) {
+  if (rows <= 0 || num_q_heads <= 0 || num_kv_heads <= 0 || num_q_heads % num_kv_heads != 0 ||
+      head_dim <= 0 || blocks <= 0 || blocks > kSelectMaxBlocks ||
+      (int64_t)rows * num_kv_heads > kMaxRowItems)
+    return 0;
+  return sparse_workspace_bytes((int64_t)rows * num_kv_heads, num_q_heads / num_kv_heads,
+                                head_dim, blocks);
+}
+
+pkv_status pkv_sparse_attention(const pkv_paged_kv* kv, const void* q, int32_t num_q_heads,
+                                const int32_t* block_tables, int32_t max_blocks,
+                                int32_t num_seqs, const int32_t* row_seq,
+                                const int32_t* row_lens, int32_t rows, const int32_t* sel,
+                                int32_t blocks, float scale, void* out, float* lse,
+                                void* workspace, size_t workspace_bytes, void* stream) {
+  const char* fn = "pkv_sparse_attention";
+  const std::string f(fn);
+  KvView view;
+  pkv_status st = check_kv(kv, fn, &view);
+  if (st != PKV_OK) return st;
+  bool empty = false;
+  st = check_rows(f, num_q_heads, view.hkv, q, block_tables, max_blocks, num_seqs, row_seq,
+                  row_lens, rows, blocks, sel, &empty);
+  if (st != PKV_OK || empty) return st;
+  if (blocks > kSelectMaxBlocks)
+    return fail(PKV_ERR_INVALID_ARG, f + ": more than 65536 blocks of a row");
+  if (out == nullptr || !aligned16(out))
+    return fail(PKV_ERR_INVALID_ARG, f + ": out is NULL or not 16-byte aligned");
+  if (!(scale > 0.f)) return fail(PKV_ERR_INVALID_ARG, f + ": scale <= 0");
+  const size_t need = sparse_workspace_bytes((int64_t)rows * view.hkv, num_q_heads / view.hkv,
+                                             view.head_dim, blocks);
+  if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned16(workspace)))
+    return fail(PKV_ERR_INVALID_ARG,
+                f + ": workspace missing, too small or not 16-byte aligned "
+                    "(see pkv_sparse_workspace_bytes)");
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  {
+    MetaCheck c = meta(kMetaRows, view, block_tables, max_blocks, row_lens, nullptr, rows, -1,
+                       (int64_t)max_blocks * kSupportedBlockSize, 0);
+    c.row_seq = row_seq;
+    c.table_rows = num_seqs;
+    if ((st = check_metadata(fn, &c, 1, s)) != PKV_OK) return st;
+  }
+  SparseArgs a{};
+  a.k_cache = view.k;
+  a.v_cache = view.v;
+  a.q = static_cast<const uint16_t*>(q);
+  a.tables = block_tables;
+  a.row_seq = row_seq;
+  a.row_lens = row_lens;
+  a.sel = sel;
+  a.out = static_cast<uint16_t*>(out);
+  a.lse = lse;
+  a.rows = rows;
+  a.max_blocks = max_blocks;
+  a.num_seqs = num_seqs;
+  a.hq = num_q_heads;
+  a.hkv = view.hkv;
+  a.num_blocks = view.num_blocks;
+  a.blocks = blocks;
+  a.scale_log2 = scale * 1.44269504088896340736f;
+  return launched(launch_sparse_attention(a, view.head_dim, workspace, s), fn);
+}
+
 }  // extern "C"

@@ -99,6 +99,25 @@ struct SelectArgs {
 size_t select_workspace_bytes(int64_t items, int32_t max_len, int32_t blocks);
 hipError_t launch_select_blocks(SelectArgs a, int head_dim, void* workspace, hipStream_t stream);
 
+// Attention over chosen blocks (pkv_sparse_attention).
+struct SparseArgs {
+  const uint16_t* k_cache;
+  const uint16_t* v_cache;
+  const uint16_t* q;
+  const int32_t* tables;
+  const int32_t* row_seq;  // null: row i is sequence i
+  const int32_t* row_lens;
+  const int32_t* sel;
+  uint16_t* out;
+  float* lse;  // or null
+  int64_t rows;
+  int32_t max_blocks, num_seqs, hq, hkv, num_blocks, blocks;
+  float scale_log2;
+};
+size_t sparse_workspace_bytes(int64_t items, int32_t g, int32_t head_dim, int32_t blocks);
+hipError_t launch_sparse_attention(SparseArgs a, int head_dim, void* workspace,
+                                   hipStream_t stream);
+
 hipError_t launch_copy_blocks(const KvView& kv, const int32_t* pairs, int32_t num_pairs,
                               hipStream_t stream);
 

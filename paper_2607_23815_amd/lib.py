@@ -165,6 +165,11 @@ _SIGS = {
                                     c_int32, c_int32, c_void_p, c_void_p] + [c_int32] * 5 +
                           [c_void_p, c_void_p, c_size_t, c_void_p]),
     "pkv_select_workspace_bytes": (c_size_t, [c_int32] * 6),
+    "pkv_sparse_attention": (c_int32, [ctypes.POINTER(PagedKV), c_void_p, c_int32, c_void_p, c_int32,
+                                       c_int32, c_void_p, c_void_p, c_int32, c_void_p, c_int32,
+                                       c_float, c_void_p, c_void_p, c_void_p, c_size_t,
+                                       c_void_p]),
+    "pkv_sparse_workspace_bytes": (c_size_t, [c_int32] * 5),
     "pkv_gather_kv": (c_int32, [ctypes.POINTER(PagedKV), c_void_p, c_int32, c_void_p, c_void_p,
                                 c_int32, c_int32, c_void_p, c_void_p, c_void_p]),
 }
@@ -800,6 +805,40 @@ def pkv_select_blocks(bounds, q, block_tables, row_lens, max_len: int, sink_bloc
         None if row_seq is None else _ptr(row_seq, "row_seq", i32, dev),
         _ptr(row_lens, "row_lens", i32, dev), n, int(max_len), sink_blocks, recent_blocks, blocks,
         _ptr(sel, "sel", i32, dev), ws, ws_bytes, _stream(stream)))
+
+
+def pkv_sparse_workspace_bytes(rows, num_q_heads, num_kv_heads, head_dim, blocks) -> int:
+    return int(_lib.pkv_sparse_workspace_bytes(rows, num_q_heads, num_kv_heads, head_dim, blocks))
+
+
+def pkv_sparse_attention(k_cache, v_cache, q, block_tables, row_lens, sel, scale: float, out,
+                         row_seq=None, lse=None, workspace=None, stream=None) -> None:
+    """Rows q [rows][Hq][D] attend over the first row_lens keys of their sequences, as far as these
+    lie in the logical blocks that sel [rows][Hkv][blocks] names."""
+    torch = _torch or _get_torch()
+    bf16, i32 = torch.bfloat16, torch.int32
+    dev = _device(stream)
+    kv = _paged_kv_on(k_cache, v_cache, dev)
+    n = _check_rows(q, block_tables, row_lens, row_seq)
+    hkv, d, hq = kv.num_kv_heads, kv.head_dim, q.shape[1]
+    if sel.dim() != 3 or sel.shape[:2] != (n, hkv) or q.shape[2] != d or out.shape != q.shape:
+        raise ValueError("sel must be [rows][Hkv][blocks], q and out [rows][Hq][D] of the pool's "
+                         "head dim")
+    if lse is not None and lse.shape != (n, hq):
+        raise ValueError("lse must be [rows][Hq]")
+    b, max_blocks = block_tables.shape
+    blocks = sel.shape[2]
+    if workspace is None:  # convenience for one-off calls; timed callers pass their own
+        workspace = alloc_workspace(pkv_sparse_workspace_bytes(n, hq, hkv, d, blocks))
+    ws, ws_bytes = _workspace(workspace, dev)
+    _check(_lib.pkv_sparse_attention(
+        ctypes.byref(kv), _ptr(q, "q", bf16, dev), hq,
+        _ptr(block_tables, "block_tables", i32, dev), max_blocks, b,
+        None if row_seq is None else _ptr(row_seq, "row_seq", i32, dev),
+        _ptr(row_lens, "row_lens", i32, dev), n, _ptr(sel, "sel", i32, dev), blocks, float(scale),
+        _ptr(out, "out", bf16, dev),
+        None if lse is None else _ptr(lse, "lse", torch.float32, dev), ws, ws_bytes,
+        _stream(stream)))
 
 
 def alloc_workspace(nbytes: int, device="cuda"):

@@ -127,6 +127,30 @@ def test_select_blocks_refuses(lib):
     assert _select(lib, rows=0, q=None, sel=None) == lib.PKV_OK
 
 
+def _sparse(lib, kv=None, **kw):
+    a = dict(q=FAKE, hq=8, tables=FAKE, max_blocks=64, num_seqs=3, row_seq=FAKE, row_lens=FAKE,
+             rows=5, sel=FAKE, blocks=8, scale=0.1, out=FAKE, lse=None, ws=FAKE, ws_bytes=1 << 30)
+    a.update(kw)
+    return lib._lib.pkv_sparse_attention(ctypes.byref(kv or _kv(lib)), *a.values(), None)
+
+
+def test_sparse_attention_refuses(lib):
+    arg, shape = lib.PKV_ERR_INVALID_ARG, lib.PKV_ERR_UNSUPPORTED_SHAPE
+    for bad in (dict(q=None), dict(tables=None), dict(row_lens=None), dict(sel=None),
+                dict(out=None), dict(q=ctypes.c_void_p(0x3008)), dict(out=ctypes.c_void_p(0x3004)),
+                dict(rows=-1), dict(num_seqs=-1), dict(max_blocks=-1), dict(blocks=-1),
+                dict(blocks=0), dict(blocks=65537), dict(scale=0.0), dict(scale=-1.0),
+                dict(scale=float("nan")), dict(row_seq=None), dict(rows=2**22 + 1)):
+        refused(lib, arg, _sparse(lib, **bad), "pkv_sparse_attention")
+    for bad in (dict(hq=7), dict(hq=34), dict(kv=_kv(lib, 32)), dict(kv=_kv(lib, 128, 8))):
+        refused(lib, shape, _sparse(lib, **bad), "pkv_sparse_attention")
+    assert _sparse(lib, rows=0, q=None, sel=None, out=None) == lib.PKV_OK
+    need = lib.pkv_sparse_workspace_bytes(1, 8, 2, 128, 4096)
+    if need:
+        for bad in (dict(ws=None), dict(ws_bytes=need - 1), dict(ws=ctypes.c_void_p(0x3004))):
+            refused(lib, arg, _sparse(lib, rows=1, blocks=4096, **bad), "workspace")
+
+
 def test_binding_refuses_host_tensors(lib):
     import torch
     if torch.cuda.is_available():
