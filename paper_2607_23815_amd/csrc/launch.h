@@ -113,6 +113,11 @@ struct SparseArgs {
   int64_t rows;
   int32_t max_blocks, num_seqs, hq, hkv, num_blocks, blocks;
   float scale_log2;
+  // set by the launch: a list's cut across workgroups, and the splits' partial results
+  int64_t xcd_items;  // items of each XCD's part, or 0: items in order
+  int32_t splits, split_entries;
+  float* ws_o;
+  float* ws_ml;
 };
 size_t sparse_workspace_bytes(int64_t items, int32_t g, int32_t head_dim, int32_t blocks);
 hipError_t launch_sparse_attention(SparseArgs a, int head_dim, void* workspace,
