@@ -77,6 +77,7 @@ def test_matches_a_loop_over_blocks(gpu_lib, hkv, d, seqs):
     args = case(rng, seqs, hkv, d)
     check(call(gpu_lib, *args, seqs), *args, seqs)
     check(call(gpu_lib, *args, seqs, max_new=5000), *args, seqs)
+    check(call(gpu_lib, *args, seqs, max_new=1 << 24), *args, seqs)  # (as keys past the caches)
 
 
 def test_special_values(gpu_lib):
