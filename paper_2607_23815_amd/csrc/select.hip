@@ -12,6 +12,9 @@
 // between are scored again in 64 bits (select_kernel), where the products of bf16 values are exact.
 //
 // One row per sequence is bound by reading the bounds (4 D bytes per block and kv head).
+// One wave takes several tiles of 16 blocks of one row with the next tile's loads in flight. Rows of
+// longer suffixes share their sequence's bounds: a wave then keeps 48 or 64 blocks' bounds in registers
+// and runs the rows of 64 through them, as many rows a product as its 16 lines hold heads.
 #include <math.h>
 
 #include "device_utils.h"
@@ -21,97 +24,305 @@ namespace pkv {
 namespace {
 
 constexpr int kScoreWaves = 4;
-constexpr int kSelThreads = 256;
-constexpr int kSelWaves = kSelThreads / 64;
-constexpr int kBins = 2048;
-constexpr int kCand = 512;  // blocks near the border that are ranked in LDS
+constexpr int kTileBlocks = 16;      // blocks of a product
+constexpr int kMaxTiles = 16;        // tiles of one row that a wave takes at most
+template <int D>
+constexpr int kHeldTiles = D == 128 ? 3 : 4;  // tiles that a wave holds for a group of rows
+constexpr int kGroupRows = 64;       // rows of a group
+constexpr int kCand = 512;           // blocks near the border that are ranked in LDS
 
 // The row's blocks (those with a visible key), as both kernels count them.
 __device__ __forceinline__ int row_blocks(const SelectArgs& a, int64_t row) {
   const int len = min(a.row_lens[row], a.max_len);
-  return len <= 0 ? 0 : min((int)(((int64_t)len + kBlockSize - 1) / kBlockSize), a.max_blocks);
+  return len <= 0 ? 0 : min((len - 1) / kBlockSize + 1, a.max_blocks);
 }
 __device__ __forceinline__ int row_sequence(const SelectArgs& a, int64_t row) {
   const int s = a.row_seq != nullptr ? a.row_seq[row] : (int)row;
   return s >= 0 && s < a.num_seqs ? s : -1;
 }
 
-// A wave per 16 blocks of a (row, kv head), a workgroup per 64: A = q (16 heads x 32 dims), B = bounds (32 dims x 16
-// blocks), so lane (block l % 16, group l / 16) ends with the scores of heads 4 (l / 16) + 0..3.
+template <int kCtrl>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, kCtrl, 0xF, 0xF, true);
+}
+// x and its value in the lane 16 (or 32) away, in some order.
+__device__ __forceinline__ u32x2 with_row(uint32_t x) {
+#if __HIP_DEVICE_COMPILE__
+  const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  return u32x2{r[0], r[1]};
+#else
+  return u32x2{x, x};
+#endif
+}
+__device__ __forceinline__ u32x2 with_half(uint32_t x) {
+#if __HIP_DEVICE_COMPILE__
+  const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return u32x2{r[0], r[1]};
+#else
+  return u32x2{x, x};
+#endif
+}
+// Every lane's value combined, in every lane (32-bit types).
+template <typename T, typename F>
+__device__ __forceinline__ T wave_all(T v, F op) {
+  auto step = [&](uint32_t other) { v = op(v, __builtin_bit_cast(T, other)); };
+  step(dpp<0x128>(__builtin_bit_cast(uint32_t, v)));  // rotations within 16 lanes
+  step(dpp<0x124>(__builtin_bit_cast(uint32_t, v)));
+  step(dpp<0x122>(__builtin_bit_cast(uint32_t, v)));
+  step(dpp<0x121>(__builtin_bit_cast(uint32_t, v)));
+  auto pair = [&](u32x2 r) {  // (elements copied: a bit cast takes whole objects)
+    const uint32_t x = r[0], y = r[1];
+    v = op(__builtin_bit_cast(T, x), __builtin_bit_cast(T, y));
+  };
+  pair(with_row(__builtin_bit_cast(uint32_t, v)));
+  pair(with_half(__builtin_bit_cast(uint32_t, v)));
+  return v;
+}
+struct Max {
+  __device__ float operator()(float x, float y) const { return fmaxf(x, y); }
+  __device__ uint32_t operator()(uint32_t x, uint32_t y) const { return max(x, y); }
+  __device__ int operator()(int x, int y) const { return max(x, y); }
+};
+struct Add {
+  __device__ int operator()(int x, int y) const { return x + y; }
+  __device__ float operator()(float x, float y) const { return x + y; }
+};
+
+// The parts of two bf16 with the sign bit `side`, zeros in the others' place.
+__device__ __forceinline__ uint32_t one_side(uint32_t w, int side) {
+  typedef __attribute__((ext_vector_type(2))) int16_t s16x2;
+  const uint32_t neg = __builtin_bit_cast(uint32_t, (s16x2)(__builtin_bit_cast(s16x2, w) >> 15));
+  return side ? w & neg : w & ~neg;
+}
+// The larger |bf16| of each half of two words, as bits.
+__device__ __forceinline__ uint32_t most_of(uint32_t most, uint32_t w) {
+  typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
+  return __builtin_bit_cast(uint32_t,
+                            __builtin_elementwise_max(__builtin_bit_cast(u16x2, most),
+                                                      __builtin_bit_cast(u16x2, w & 0x7FFF7FFFu)));
+}
+__device__ __forceinline__ float most_value(uint32_t most) {  // over the wave
+  return __uint_as_float(wave_all(max(most & 0xFFFFu, most >> 16), Max()) << 16);
+}
+__device__ __forceinline__ float or_infinity(float s) { return fabsf(s) < INFINITY ? s : INFINITY; }
+
 template <int D>
-__device__ __forceinline__ void score_tile(const SelectArgs& a, int64_t work, int chunks) {
-  constexpr int KK = D / 32;
-  const int64_t item = work / chunks;  // (row, kv head)
-  const int64_t row = item / a.hkv;
-  const int kvh = (int)(item % a.hkv);
-  const int n = row_blocks(a, row);
-  const int seq = row_sequence(a, row);
-  const int tile = (int)(work % chunks) * kScoreWaves + (threadIdx.x >> 6);
-  if (seq < 0 || n <= a.blocks || tile * 16 >= n) return;
-  const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
-  const int g = a.hq / a.hkv;
-  const int b = min(tile * 16 + col, n - 1);
-  const int id = a.tables[(size_t)seq * a.max_blocks + b];
-  const uint16_t* box = a.bounds + ((size_t)(id < 0 || id >= a.num_blocks ? 0 : id) * a.hkv + kvh) * 2 * D;
-  const uint16_t* q = a.q + ((size_t)row * a.hq + kvh * g + col) * D;
-  f32x4 s = {0.f, 0.f, 0.f, 0.f};
-  uint32_t most = 0u;  // the largest |bound| of this lane, as bf16 bits
+struct Box {  // 16 blocks' bounds: lane (block col, chunk group grp)
+  u32x4 v[2][D / 32];
+};
+template <int D>
+__device__ __forceinline__ void load_box(const SelectArgs& a, Box<D>& x, int id, int kvh) {
+  const int grp = (threadIdx.x & 63) >> 4;
+  if (id < 0 || id >= a.num_blocks) id = 0;
+  const uint16_t* box = a.bounds + ((size_t)id * a.hkv + kvh) * 2 * D + grp * 8;
 #pragma unroll
   for (int side = 0; side < 2; ++side) {
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-      const int d = kk * 32 + grp * 8;
-      u32x4 qv = {0u, 0u, 0u, 0u};
-      if (col < g) qv = ld16(q + d);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {  // the positive parts, then the negative ones
-        const uint32_t lo = qv[e] & 0xFFFFu, hi = qv[e] >> 16;
-        const uint32_t keep_lo = (lo >> 15) == (uint32_t)side ? lo : 0u;
-        const uint32_t keep_hi = (hi >> 15) == (uint32_t)side ? hi : 0u;
-        qv[e] = keep_lo | keep_hi << 16;
-      }
-      const u32x4 bv = ld16(box + side * D + d);
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        most = max(most, max(bv[e] & 0x7FFFu, bv[e] >> 16 & 0x7FFFu));
-      s = mfma16(as_bf16x8(qv), as_bf16x8(bv), s);
-    }
+    for (int kk = 0; kk < D / 32; ++kk) x.v[side][kk] = ld16(box + side * D + kk * 32);
   }
-  float best = -INFINITY;
-  bool odd = false;
-#pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    if (4 * grp + r < g) {
-      best = fmaxf(best, s[r]);
-      odd |= !isfinite(s[r]);
-    }
-  }
-  if (odd) best = INFINITY;
-  best = fmaxf(best, __shfl_xor(best, 16));
-  best = fmaxf(best, __shfl_xor(best, 32));
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o));
-  if (grp == 0 && tile * 16 + col < n) a.scores[item * a.stride + tile * 16 + col] = best;
-  if (lane == 0) a.tile_most[item * (a.stride / 16) + tile] = __uint_as_float(most << 16);
 }
-
 template <int D>
-__global__ __launch_bounds__(64 * kScoreWaves) void score_kernel(const SelectArgs a, int chunks,
-                                                                 int64_t total) {
-  for (int64_t work = blockIdx.x; work < total; work += gridDim.x) score_tile<D>(a, work, chunks);
+__device__ __forceinline__ uint32_t box_most(const Box<D>& x) {
+  uint32_t most = 0u;
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+#pragma unroll
+    for (int kk = 0; kk < D / 32; ++kk) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) most = most_of(most, x.v[side][kk][e]);
+    }
+  }
+  return most;
+}
+// q (16 heads x D, lane (head col, chunk group)) split into its positive and negative parts.
+template <int D>
+struct Sides {
+  u32x4 v[2][D / 32];
+};
+template <int D>
+__device__ __forceinline__ void split_q(const u32x4 (&q)[D / 32], Sides<D>& x) {
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+#pragma unroll
+    for (int kk = 0; kk < D / 32; ++kk) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x.v[side][kk][e] = one_side(q[kk][e], side);
+    }
+  }
+}
+// Lane (block col, group grp) receives the sums of heads 4 grp + 0..3.
+template <int D>
+__device__ __forceinline__ f32x4 score(const Sides<D>& q, const Box<D>& b) {
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+#pragma unroll
+    for (int kk = 0; kk < D / 32; ++kk)
+      s = mfma16(as_bf16x8(q.v[side][kk]), as_bf16x8(b.v[side][kk]), s);
+  }
+  return s;
 }
 
-template <typename T, typename F>
-__device__ __forceinline__ T wg_reduce(T v, F op, T* sm) {
+// A wave per (row, kv head, run of tiles).
+template <int D>
+__global__ __launch_bounds__(64 * kScoreWaves) void score_row_kernel(const SelectArgs a, int runs,
+                                                                     int tiles, int64_t total) {
+  const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  for (int64_t work = (int64_t)blockIdx.x * kScoreWaves + wave; work < total;
+       work += (int64_t)gridDim.x * kScoreWaves) {
+    const int64_t item = work / runs;
+    const int64_t row = item / a.hkv;
+    const int kvh = (int)(item % a.hkv);
+    const int t0 = (int)(work % runs) * tiles;
+    const int n = row_blocks(a, row), seq = row_sequence(a, row);
+    if (seq < 0 || n <= a.blocks || t0 * kTileBlocks >= n) continue;
+    const int t1 = min(t0 + tiles, (n + kTileBlocks - 1) / kTileBlocks);
+    const int32_t* table = a.tables + (size_t)seq * a.max_blocks;
+    // the ids of the run's blocks, 64 per register
+    static_assert(kMaxTiles == 16, "four registers of 64 ids");
+    auto ids_of = [&](int k) {
+      return t0 + 4 * k < t1 ? table[min(t0 * kTileBlocks + 64 * k + lane, n - 1)] : 0;
+    };
+    const int ids0 = ids_of(0), ids1 = ids_of(1), ids2 = ids_of(2), ids3 = ids_of(3);
+    const int g = a.hq / a.hkv;
+    u32x4 qv[D / 32];
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v = op(v, (T)__shfl_xor(v, o));
-  __syncthreads();  // (sm's readers of the last call)
-  if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = sm[0];
+    for (int kk = 0; kk < D / 32; ++kk) {
+      qv[kk] = u32x4{0u, 0u, 0u, 0u};
+      if (col < g) qv[kk] = ld16(a.q + ((size_t)row * a.hq + kvh * g + col) * D + kk * 32 + grp * 8);
+    }
+    auto id_of = [=](int j) {  // of block col of the run's tile j
+      const int half = j < 4 ? +ids0 : +ids1, rest = j < 12 ? +ids2 : +ids3;
+      const int x = j < 8 ? +half : +rest;
+      return __builtin_amdgcn_ds_bpermute((j % 4 * 16 + col) * 4, x);
+    };
+    Sides<D> q;
+    Box<D> box[2];
+    load_box<D>(a, box[0], id_of(0), kvh);
+    split_q<D>(qv, q);
+    float* out = a.scores + item * a.stride;
+    float* most = a.tile_most + item * (a.stride / kTileBlocks);
+    auto finish = [&](const Box<D>& b, int t) {
+      const f32x4 s = score<D>(q, b);
+      float best = -INFINITY;
 #pragma unroll
-  for (int k = 1; k < kSelWaves; ++k) v = op(v, sm[k]);
-  return v;
+      for (int r = 0; r < 4; ++r)
+        if (4 * grp + r < g) best = fmaxf(best, or_infinity(s[r]));
+      u32x2 x = with_row(__float_as_uint(best));
+      best = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+      x = with_half(__float_as_uint(best));
+      best = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+      const float top = most_value(box_most<D>(b));
+      if (grp == 0 && t * kTileBlocks + col < n) out[t * kTileBlocks + col] = best;
+      if (lane == 0) most[t] = top;
+    };
+    for (int t = t0; t < t1; t += 2) {
+      if (t + 1 < t1) load_box<D>(a, box[1], id_of(t + 1 - t0), kvh);
+      finish(box[0], t);
+      if (t + 1 >= t1) break;
+      if (t + 2 < t1) load_box<D>(a, box[0], id_of(t + 2 - t0), kvh);
+      finish(box[1], t + 1);
+    }
+  }
+}
+
+// A wave per (64 rows, kv head, held tiles): for each run of rows of one sequence, that sequence's
+// blocks in registers, and the rows' heads through them, 16 / kHeads rows at a time (kHeads: the
+// group's heads rounded up to a power of two).
+template <int D, int kHeads>
+__global__ __launch_bounds__(64 * kScoreWaves) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void score_rows_kernel(const SelectArgs a, int chunks, int64_t total) {
+  constexpr int kRows = kTileBlocks / kHeads;  // rows of a product
+  const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = a.hq / a.hkv;
+  for (int64_t work = (int64_t)blockIdx.x * kScoreWaves + wave; work < total;
+       work += (int64_t)gridDim.x * kScoreWaves) {
+    const int b0 = (int)(work % chunks) * kTileBlocks * kHeldTiles<D>;
+    const int kvh = (int)(work / chunks % a.hkv);
+    const int64_t row0 = work / chunks / a.hkv * kGroupRows;
+    // lane i: row i of the group, its sequence and the blocks to score (0: none)
+    const int64_t mine = row0 + lane;
+    const int seq = mine < a.rows ? row_sequence(a, mine) : -1;
+    int n = seq >= 0 ? row_blocks(a, mine) : 0;
+    if (n <= a.blocks || n <= b0) n = 0;
+    uint64_t todo = __builtin_amdgcn_ballot_w64(n > 0);
+    while (todo != 0) {
+      const int first = __builtin_ctzll(todo);
+      const int s = __builtin_amdgcn_readlane(seq, first);
+      const uint64_t same = __builtin_amdgcn_ballot_w64(seq == s) >> first;
+      const int end = first + (~same == 0 ? 64 : __builtin_ctzll(~same));  // (past the run)
+      const int most_n = wave_all(lane >= first && lane < end ? n : 0, Max());
+      todo &= end >= 64 ? 0 : ~0ull << end;
+      Box<D> box[kHeldTiles<D>];
+      float top[kHeldTiles<D>];
+      const int id = a.tables[(size_t)s * a.max_blocks + min(b0 + lane, most_n - 1)];
+#pragma unroll
+      for (int j = 0; j < kHeldTiles<D>; ++j)
+        load_box<D>(a, box[j], __builtin_amdgcn_ds_bpermute((j * 16 + col) * 4, id), kvh);
+      // lane's line of a product: head col % kHeads of row col / kHeads
+      const int head = col % kHeads;
+      auto load_q = [&](int r, u32x4 (&qv)[D / 32]) {
+        const int at = r + col / kHeads;
+        const uint16_t* from = a.q + ((size_t)(row0 + at) * a.hq + kvh * g + head) * D + grp * 8;
+#pragma unroll
+        for (int kk = 0; kk < D / 32; ++kk) {
+          qv[kk] = u32x4{0u, 0u, 0u, 0u};
+          if (head < g && at < end) qv[kk] = ld16(from + kk * 32);
+        }
+      };
+      u32x4 qv[D / 32];
+      load_q(first, qv);
+#pragma unroll
+      for (int j = 0; j < kHeldTiles<D>; ++j) top[j] = most_value(box_most<D>(box[j]));
+      for (int r = first; r < end; r += kRows) {
+        Sides<D> q;
+        split_q<D>(qv, q);
+        if (r + kRows < end) load_q(r + kRows, qv);
+#pragma unroll
+        for (int j = 0; j < kHeldTiles<D>; ++j) {
+          if (b0 + j * kTileBlocks >= most_n) break;
+          f32x4 sc = score<D>(q, box[j]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {  // heads that pad the group do not count
+            sc[e] = or_infinity(sc[e]);
+            if ((4 * grp + e) % kHeads >= g) sc[e] = -INFINITY;
+          }
+          // value e of lane (block col, grp) is row kRow * grp + e's (or the row is over lanes)
+          constexpr int kMine = kHeads >= 4 ? 1 : 4 / kHeads;  // rows of a lane
+          float best[kMine];
+#pragma unroll
+          for (int e = 0; e < kMine; ++e) {
+            best[e] = sc[e * (4 / kMine)];
+#pragma unroll
+            for (int f = 1; f < 4 / kMine; ++f) best[e] = fmaxf(best[e], sc[e * (4 / kMine) + f]);
+          }
+          if constexpr (kHeads >= 8) {
+            const u32x2 x = with_row(__float_as_uint(best[0]));
+            best[0] = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+          }
+          if constexpr (kHeads == 16) {
+            const u32x2 x = with_half(__float_as_uint(best[0]));
+            best[0] = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+          }
+#pragma unroll
+          for (int e = 0; e < kMine; ++e) {
+            const int at = r + (kHeads >= 4 ? 4 * grp / kHeads : kMine * grp + e);
+            int rn = __builtin_amdgcn_ds_bpermute((at & 63) * 4, n);
+            if (at >= end) rn = 0;
+            const int b = b0 + j * kTileBlocks + col;
+            const int64_t item = (row0 + at) * a.hkv + kvh;
+            const bool writer = kHeads <= 4 || 4 * grp % kHeads == 0;
+            if (writer && b < rn) {
+              a.scores[item * a.stride + b] = best[e];
+              if (col == 0) a.tile_most[(item * a.stride + b) / kTileBlocks] = top[j];
+            }
+          }
+        }
+      }
+    }
+  }
 }
 
 // A score in 64 bits by one wave, as a key whose unsigned order is the scores' order (a score that
@@ -152,17 +363,67 @@ __device__ __forceinline__ uint64_t exact_key(const SelectArgs& a, const uint16_
   return u >> 63 ? ~u : u | 1ull << 63;
 }
 
-// One workgroup per (row, kv head).
-template <int D>
-__global__ __launch_bounds__(kSelThreads) void select_kernel(const SelectArgs a) {
-  __shared__ uint32_t chosen[kSelectMaxBlocks / 32];
+// Several 32-bit values combined over the workgroup at once.
+template <int kThreads, int n, typename T, typename F>
+__device__ __forceinline__ void wg_all(T (&v)[n], F op, T (*sm)[n]) {
+  constexpr int kWaves = kThreads / 64;
+#pragma unroll
+  for (int k = 0; k < n; ++k) v[k] = wave_all(v[k], op);
+  if constexpr (kWaves > 1) {
+    __syncthreads();  // (sm's readers of the last call)
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int k = 0; k < n; ++k) sm[threadIdx.x >> 6][k] = v[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < n; ++k) {
+      v[k] = sm[0][k];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) v[k] = op(v[k], sm[w][k]);
+    }
+  }
+}
+// The sum over the threads before this one, and over all.
+template <int kThreads>
+__device__ __forceinline__ int wg_before(int v, int* total, int* sm) {
+  constexpr int kWaves = kThreads / 64;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  int incl = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int u = __shfl_up(incl, o);
+    if (lane >= o) incl += u;
+  }
+  __syncthreads();
+  if (lane == 63) sm[w] = incl;
+  __syncthreads();
+  int before = incl - v;
+  *total = 0;
+#pragma unroll
+  for (int k = 0; k < kWaves; ++k) {
+    if (k < w) before += sm[k];
+    *total += sm[k];
+  }
+  return before;
+}
+
+// One workgroup per (row, kv head); its scores, at most kThreads * kEach, stay in registers (kEach 0: in
+// memory, any number).
+template <int D, int kThreads, int kEach>
+__global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs a) {
+  constexpr int kWaves = kThreads / 64;
+  constexpr int kPer = kThreads == 1024 ? 2 : 8;  // bins of a thread
+  constexpr int kBins = kPer * kThreads;
+  constexpr int kWords = (kEach > 0 ? kThreads * kEach : kSelectMaxBlocks) / 32;
+  __shared__ uint32_t chosen[kWords];
   __shared__ uint32_t bins[kBins];
   __shared__ uint64_t cand_key[kCand];
   __shared__ int cand_at[kCand];
-  __shared__ float smf[kSelWaves];
-  __shared__ int smi[kSelWaves];
+  __shared__ float sm5[kWaves][5], sm2[kWaves][2];
+  __shared__ int sm1[kWaves][1], sms[kWaves];
   __shared__ int num_cand, pivot;
-  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+  const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
   const int64_t item = blockIdx.x;
   const int64_t row = item / a.hkv;
   const int kvh = (int)(item % a.hkv);
@@ -171,152 +432,151 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(const SelectArgs a)
   const int n = row_blocks(a, row);
   int32_t* sel = a.sel + item * a.blocks;
   if (n <= a.blocks) {  // every block
-    for (int k = t; k < a.blocks; k += kSelThreads) sel[k] = k < n ? k : -1;
+    for (int k = t; k < a.blocks; k += kThreads) sel[k] = k < n ? k : -1;
     return;
   }
   const int first = a.sink, last = n - a.recent;  // [first, last) goes by score
   const int want = a.blocks - a.sink - a.recent;
-  float* score = a.scores + item * a.stride;
+  float* scores = a.scores + item * a.stride;
   float* low = a.low + item * a.stride;
   const int32_t* table = a.tables + (size_t)seq * a.max_blocks;
   const int g = a.hq / a.hkv;
   const uint16_t* q = a.q + ((size_t)row * a.hq + kvh * g) * D;
 
-  for (int k = t; k < (n + 31) / 32; k += kSelThreads) chosen[k] = 0u;
+  float s[kEach > 0 ? kEach : 1];  // of blocks first + t + k kThreads
+  auto each = [&](auto f) {
+    if constexpr (kEach > 0) {
+#pragma unroll
+      for (int k = 0; k < kEach; ++k) {
+        const int b = first + t + k * kThreads;
+        if (b < last) f(b, s[k]);
+      }
+    } else {
+      for (int b = first + t; b < last; b += kThreads) f(b, scores[b]);
+    }
+  };
+  if (want > 0) {
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int b = first + t + k * kThreads;
+      s[k] = b < last ? scores[b] : 0.f;
+    }
+  }
+  for (int k = t; k < (n + 31) / 32; k += kThreads) chosen[k] = 0u;
   if (t == 0) num_cand = 0;
-  for (int k = t; k < kBins; k += kSelThreads) bins[k] = 0u;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) bins[t * kPer + k] = 0u;
   __syncthreads();
   auto choose = [&](int b) { atomicOr(&chosen[b >> 5], 1u << (b & 31)); };
-  for (int k = t; k < a.sink + a.recent; k += kSelThreads)
+  for (int k = t; k < a.sink + a.recent; k += kThreads)
     choose(k < a.sink ? k : n - a.recent + (k - a.sink));
 
   if (want > 0) {
     // the error of a 32-bit score: 2 D products summed in some order, each addition off by at most
     // 2^-23 of the sum of their magnitudes, |q|_1 max |bound|; tiny values may count as zeros
-    float norm = 0.f, qmost = 0.f;
-    for (int h = w; h < g; h += kSelWaves) {
-      float s = 0.f, m = 0.f;
-      for (int d = lane; d < D; d += 64) {
-        const float x = fabsf(__uint_as_float((uint32_t)q[h * D + d] << 16));
-        s += x;
-        m = fmaxf(m, x);
-      }
+    float all[5] = {0.f, 0.f, 0.f, -INFINITY, -INFINITY};  // |q|_1, max |q|, max |bound|, -min s, max s
+    for (int h = w; h < g; h += kWaves) {
+      float norm = 0.f;
 #pragma unroll
-      for (int o = 32; o >= 1; o >>= 1) {
-        s += __shfl_xor(s, o);
-        m = fmaxf(m, __shfl_xor(m, o));
+      for (int e = 0; e < D / 64; ++e) {
+        const float x = fabsf(__uint_as_float((uint32_t)q[h * D + lane * (D / 64) + e] << 16));
+        norm += x;
+        all[1] = fmaxf(all[1], x);
       }
-      norm = fmaxf(norm, s);
-      qmost = fmaxf(qmost, m);
+      all[0] = fmaxf(all[0], wave_all(norm, Add()));
     }
-    auto maxf = [](float x, float y) { return fmaxf(x, y); };
-    auto minf = [](float x, float y) { return fminf(x, y); };
-    auto addi = [](int x, int y) { return x + y; };
-    norm = wg_reduce(norm, maxf, smf);
-    qmost = wg_reduce(qmost, maxf, smf);
-    float most = 0.f;
-    for (int k = t; k < (n + 15) / 16; k += kSelThreads)
-      most = fmaxf(most, a.tile_most[item * (a.stride / 16) + k]);
-    most = wg_reduce(most, maxf, smf);
+    for (int k = t; k < (n + kTileBlocks - 1) / kTileBlocks; k += kThreads)
+      all[2] = fmaxf(all[2], a.tile_most[item * (a.stride / kTileBlocks) + k]);
+    each([&](int, float x) {
+      all[3] = fmaxf(all[3], -x);
+      all[4] = fmaxf(all[4], x);
+    });
+    wg_all<kThreads>(all, Max(), sm5);
     const float tiny = 0x1p-118f;
-    const float err2 = 2.f * (0x1p-15f * 1.01f * norm * most + tiny * (1.f + qmost + most));
+    const float err2 = 2.f * (0x1p-15f * 1.01f * all[0] * all[2] + tiny * (1.f + all[1] + all[2]));
+    const float mn = -all[3], range = all[4] + all[3];
+    const bool odd = !(isfinite(err2) && isfinite(all[4]) && isfinite(mn) && isfinite(range));
 
     // how the scores spread: a histogram between the least and the largest finds the bin of the
     // last chosen one
-    float mn = INFINITY, mx = -INFINITY;
-    for (int b = first + t; b < last; b += kSelThreads) {
-      mn = fminf(mn, score[b]);
-      mx = fmaxf(mx, score[b]);
-    }
-    mn = wg_reduce(mn, minf, smf);
-    mx = wg_reduce(mx, maxf, smf);
-    const float range = mx - mn;
-    bool slow = !(isfinite(err2) && isfinite(mn) && isfinite(mx) && isfinite(range));
+    bool slow = odd;
     const float per = range > 0.f ? (kBins - 1) / range : 0.f;
-    auto bin_of = [&](float s) { return min((int)((s - mn) * per), kBins - 1); };
+    auto bin_of = [&](float x) { return min((int)((x - mn) * per), kBins - 1); };
     float lo = 0.f, hi = 0.f;
     if (!slow) {
-      for (int b = first + t; b < last; b += kSelThreads) atomicAdd(&bins[bin_of(score[b])], 1u);
+      each([&](int, float x) { atomicAdd(&bins[bin_of(x)], 1u); });
       __syncthreads();
-      // thread t counts bins [8 (255 - t), 8 (255 - t) + 8): a scan from the top
-      constexpr int kPer = kBins / kSelThreads;
-      int mine = 0;
-      for (int k = 0; k < kPer; ++k) mine += bins[(kSelThreads - 1 - t) * kPer + k];
-      int incl = mine;
+      // thread t counts bins [kPer (kThreads - 1 - t), + kPer): from the top
+      const uint32_t* mine = &bins[(kThreads - 1 - t) * kPer];
+      int sum = 0;
 #pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const int u = __shfl_up(incl, o);
-        if (lane >= o) incl += u;
-      }
-      if (lane == 63) smi[w] = incl;
-      __syncthreads();
-      for (int k = 0; k < w; ++k) incl += smi[k];
-      if (incl - mine < want && want <= incl) {  // (one thread)
-        int left = want - (incl - mine), k = kPer - 1;
-        while (left > (int)bins[(kSelThreads - 1 - t) * kPer + k])
-          left -= bins[(kSelThreads - 1 - t) * kPer + k--];
-        pivot = (kSelThreads - 1 - t) * kPer + k;
+      for (int k = 0; k < kPer; ++k) sum += mine[k];
+      int total;
+      const int before = wg_before<kThreads>(sum, &total, sms);
+      if (before < want && want <= before + sum) {  // (one thread)
+        int left = want - before, k = kPer - 1;
+        while (left > (int)mine[k]) left -= mine[k--];
+        pivot = (kThreads - 1 - t) * kPer + k;
       }
       __syncthreads();
       // the scores of that bin lie in [lo, hi]: fewer than `want` lie above, at least from lo on
-      lo = INFINITY;
-      hi = -INFINITY;
-      for (int b = first + t; b < last; b += kSelThreads) {
-        if (bin_of(score[b]) == pivot) {
-          lo = fminf(lo, score[b]);
-          hi = fmaxf(hi, score[b]);
+      float edge[2] = {-INFINITY, -INFINITY};
+      each([&](int, float x) {
+        if (bin_of(x) == pivot) {
+          edge[0] = fmaxf(edge[0], -x);
+          edge[1] = fmaxf(edge[1], x);
         }
-      }
-      lo = wg_reduce(lo, minf, smf) - err2;
-      hi = wg_reduce(hi, maxf, smf) + err2;
+      });
+      wg_all<kThreads>(edge, Max(), sm2);
+      lo = -edge[0] - err2;
+      hi = edge[1] + err2;
       // certain ones, and those between
-      int in = 0;
-      for (int b = first + t; b < last; b += kSelThreads) {
-        const float s = score[b];
-        if (s > hi) {
+      int in[1] = {0};
+      each([&](int b, float x) {
+        if (x > hi) {
           choose(b);
-          ++in;
-        } else if (s >= lo) {
+          ++in[0];
+        } else if (x >= lo) {
           const int k = atomicAdd(&num_cand, 1);
           if (k < kCand) cand_at[k] = b;
         }
-      }
-      in = wg_reduce(in, addi, smi);
-      const int left = want - in, cands = num_cand;
+      });
+      wg_all<kThreads>(in, Add(), sm1);
+      __syncthreads();  // (a single wave's candidates too)
+      const int left = want - in[0], cands = num_cand;
       slow = cands > kCand;
       if (!slow && cands == left) {
-        for (int k = t; k < cands; k += kSelThreads) choose(cand_at[k]);
+        for (int k = t; k < cands; k += kThreads) choose(cand_at[k]);
       } else if (!slow) {
-        for (int k = w; k < cands; k += kSelWaves) {
+        for (int k = w; k < cands; k += kWaves) {
           const uint64_t key = exact_key<D>(a, q, g, table, kvh, cand_at[k]);
           if (lane == 0) cand_key[k] = key;
         }
         __syncthreads();
-        for (int k = t; k < cands; k += kSelThreads) {
-          int before = 0;
+        for (int k = t; k < cands; k += kThreads) {
+          int ahead = 0;
           for (int j = 0; j < cands; ++j)
-            before += cand_key[j] > cand_key[k] ||
-                      (cand_key[j] == cand_key[k] && cand_at[j] < cand_at[k]);
-          if (before < left) choose(cand_at[k]);
+            ahead += cand_key[j] > cand_key[k] ||
+                     (cand_key[j] == cand_key[k] && cand_at[j] < cand_at[k]);
+          if (ahead < left) choose(cand_at[k]);
         }
       }
     }
     if (slow) {
       // many blocks at the border (equal ones), or scores that are not finite: every key in 64
       // bits, in the workspace's two halves, and a search for the last chosen key bit by bit
-      uint32_t* kh = reinterpret_cast<uint32_t*>(score);
+      uint32_t* kh = reinterpret_cast<uint32_t*>(scores);
       uint32_t* kl = reinterpret_cast<uint32_t*>(low);
-      const bool all = !(isfinite(err2) && isfinite(mn) && isfinite(mx) && isfinite(range));
-      for (int b0 = first + w * 64; b0 < last; b0 += kSelThreads) {
+      for (int b0 = first + w * 64; b0 < last; b0 += kThreads) {
         const int b = b0 + lane;
-        const float s = b < last ? score[b] : 0.f;
-        uint64_t key = !all && s > hi ? ~0ull : 0ull;
-        uint64_t todo = __builtin_amdgcn_ballot_w64(b < last && (all || (s >= lo && s <= hi)));
+        const float x = b < last ? scores[b] : 0.f;
+        uint64_t key = !odd && x > hi ? ~0ull : 0ull;
+        uint64_t todo = __builtin_amdgcn_ballot_w64(b < last && (odd || (x >= lo && x <= hi)));
         while (todo != 0) {
           const int k = __builtin_ctzll(todo);
           todo &= todo - 1;
-          const uint64_t x = exact_key<D>(a, q, g, table, kvh, b0 + k);
-          if (lane == k) key = x;
+          const uint64_t exact = exact_key<D>(a, q, g, table, kvh, b0 + k);
+          if (lane == k) key = exact;
         }
         if (b < last) {
           kh[b] = (uint32_t)(key >> 32);
@@ -328,20 +588,21 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(const SelectArgs a)
       uint64_t cut = 0;  // the largest key that at least `want` blocks reach
       for (int bit = 63; bit >= 0; --bit) {
         const uint64_t probe = cut | 1ull << bit;
-        int c = 0;
-        for (int b = first + t; b < last; b += kSelThreads) c += key_at(b) >= probe;
-        if (wg_reduce(c, addi, smi) >= want) cut = probe;
+        int c[1] = {0};
+        for (int b = first + t; b < last; b += kThreads) c[0] += key_at(b) >= probe;
+        wg_all<kThreads>(c, Add(), sm1);
+        if (c[0] >= want) cut = probe;
       }
-      int c = 0;
-      for (int b = first + t; b < last; b += kSelThreads) {
+      int c[1] = {0};
+      for (int b = first + t; b < last; b += kThreads) {
         if (key_at(b) > cut) {
           choose(b);
-          ++c;
+          ++c[0];
         }
       }
-      c = wg_reduce(c, addi, smi);
+      wg_all<kThreads>(c, Add(), sm1);
       if (w == 0) {  // the rest from the equal ones, lowest index first
-        int left = want - c;
+        int left = want - c[0];
         for (int b0 = first; b0 < last && left > 0; b0 += 64) {
           const int b = b0 + lane;
           const bool eq = b < last && key_at(b) == cut;
@@ -354,25 +615,13 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(const SelectArgs a)
   }
   __syncthreads();
   // the chosen ones in ascending order
-  int before = 0;
-  for (int k0 = 0; k0 < (n + 31) / 32; k0 += kSelThreads) {
+  int done = 0;
+  for (int k0 = 0; k0 < (n + 31) / 32; k0 += kThreads) {
     const int k = k0 + t;
     uint32_t bits = k < (n + 31) / 32 ? chosen[k] : 0u;
-    const int mine = __builtin_popcount(bits);
-    int incl = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int u = __shfl_up(incl, o);
-      if (lane >= o) incl += u;
-    }
-    __syncthreads();
-    if (lane == 63) smi[w] = incl;
-    __syncthreads();
-    int at = before + incl - mine;
-    for (int j = 0; j < kSelWaves; ++j) {
-      if (j < w) at += smi[j];
-      before += smi[j];
-    }
+    int total;
+    int at = done + wg_before<kThreads>(__builtin_popcount(bits), &total, sms);
+    done += total;
     while (bits != 0u) {
       sel[at++] = k * 32 + __builtin_ctz(bits);
       bits &= bits - 1u;
@@ -385,30 +634,69 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(const SelectArgs a)
 size_t select_workspace_bytes(int64_t items, int32_t max_len, int32_t blocks) {
   const int64_t n = ((int64_t)max_len + kBlockSize - 1) / kBlockSize;
   if (n <= blocks) return 0;  // every block is chosen
-  const int64_t stride = (n + 15) / 16 * 16;
-  return (size_t)(items * (2 * stride + stride / 16)) * sizeof(float);
+  const int64_t stride = (n + kTileBlocks - 1) / kTileBlocks * kTileBlocks;
+  return (size_t)(items * (2 * stride + stride / kTileBlocks)) * sizeof(float);
 }
+
+namespace {
+
+template <int D>
+hipError_t launch_scores(const SelectArgs& a, int64_t items, int64_t n, hipStream_t stream) {
+  constexpr int64_t kMostWorkgroups = 1 << 20;  // (a launch's loop takes the others)
+  const int64_t tiles = (n + kTileBlocks - 1) / kTileBlocks;
+  if (a.row_seq == nullptr) {
+    // Waves enough to fill the chip a few times over, then longer runs of tiles for each.
+    int64_t run = items * tiles / 8192;
+    run = std::min<int64_t>(std::max<int64_t>(run, 1), kMaxTiles);
+    const int64_t runs = (tiles + run - 1) / run, total = items * runs;
+    const int64_t wgs = std::min((total + kScoreWaves - 1) / kScoreWaves, kMostWorkgroups);
+    hipLaunchKernelGGL(score_row_kernel<D>, dim3((unsigned)wgs), dim3(64 * kScoreWaves), 0, stream,
+                       a, (int)runs, (int)run, total);
+    return hipGetLastError();
+  }
+  const int64_t chunks = (tiles + kHeldTiles<D> - 1) / kHeldTiles<D>;
+  const int64_t total = (a.rows + kGroupRows - 1) / kGroupRows * a.hkv * chunks;
+  const int64_t wgs = std::min((total + kScoreWaves - 1) / kScoreWaves, kMostWorkgroups);
+  const int g = a.hq / a.hkv;
+  auto* kern = g == 1   ? score_rows_kernel<D, 1>
+               : g == 2 ? score_rows_kernel<D, 2>
+               : g <= 4 ? score_rows_kernel<D, 4>
+               : g <= 8 ? score_rows_kernel<D, 8>
+                        : score_rows_kernel<D, 16>;
+  hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(64 * kScoreWaves), 0, stream, a, (int)chunks,
+                     total);
+  return hipGetLastError();
+}
+
+template <int D>
+hipError_t launch_select(const SelectArgs& a, int64_t items, int64_t n, hipStream_t stream) {
+  // registers for the longest row the call can have
+  const int threads = n <= 1024 ? 64 : n <= 2048 ? 256 : 1024;
+  auto* kern = n <= 1024   ? select_kernel<D, 64, 16>
+               : n <= 2048 ? select_kernel<D, 256, 8>
+               : n <= 8192 ? select_kernel<D, 1024, 8>
+                           : select_kernel<D, 1024, 0>;
+  hipLaunchKernelGGL(kern, dim3((unsigned)items), dim3(threads), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace
 
 hipError_t launch_select_blocks(SelectArgs a, int head_dim, void* workspace, hipStream_t stream) {
   const int64_t items = a.rows * a.hkv;
-  const int64_t n = std::min<int64_t>(((int64_t)a.max_len + kBlockSize - 1) / kBlockSize, a.max_blocks);
-  a.stride = (((int64_t)a.max_len + kBlockSize - 1) / kBlockSize + 15) / 16 * 16;
+  const int64_t most = ((int64_t)a.max_len + kBlockSize - 1) / kBlockSize;
+  const int64_t n = std::min<int64_t>(most, a.max_blocks);
+  a.stride = (most + kTileBlocks - 1) / kTileBlocks * kTileBlocks;
   a.scores = static_cast<float*>(workspace);
   a.low = a.scores + items * a.stride;
   a.tile_most = a.low + items * a.stride;
   const bool wide = head_dim == 128;
   if (n > a.blocks && a.blocks > a.sink + a.recent) {
-    const int64_t chunks = (n + 16 * kScoreWaves - 1) / (16 * kScoreWaves);
-    const int64_t total = items * chunks;
-    hipLaunchKernelGGL(wide ? score_kernel<128> : score_kernel<64>,
-                       dim3((unsigned)std::min<int64_t>(total, 1 << 20)), dim3(64 * kScoreWaves), 0,
-                       stream, a, (int)chunks, total);
-    const hipError_t err = hipGetLastError();
+    const hipError_t err = wide ? launch_scores<128>(a, items, n, stream)
+                                : launch_scores<64>(a, items, n, stream);
     if (err != hipSuccess) return err;
   }
-  hipLaunchKernelGGL(wide ? select_kernel<128> : select_kernel<64>, dim3((unsigned)items),
-                     dim3(kSelThreads), 0, stream, a);
-  return hipGetLastError();
+  return wide ? launch_select<128>(a, items, n, stream) : launch_select<64>(a, items, n, stream);
 }
 
 }  // namespace pkv
