@@ -17,6 +17,9 @@
 // and runs the rows of 64 through them, as many rows a product as its 16 lines hold heads.
 #include <math.h>
 
+#include <algorithm>
+#include <type_traits>
+
 #include "device_utils.h"
 #include "launch.h"
 
@@ -28,8 +31,6 @@ constexpr int kTileBlocks = 16;      // blocks of a product
 constexpr int kMaxTiles = 16;        // tiles of one row that a wave takes at most
 template <int D>
 constexpr int kHeldTiles = D == 128 ? 3 : 4;  // tiles that a wave holds for a group of rows
-constexpr int kGroupRows = 64;       // rows of a group
-constexpr int kCand = 512;           // blocks near the border that are ranked in LDS
 
 // The row's blocks (those with a visible key), as both kernels count them.
 __device__ __forceinline__ int row_blocks(const SelectArgs& a, int64_t row) {
@@ -62,14 +63,19 @@ __device__ __forceinline__ u32x2 with_half(uint32_t x) {
   return u32x2{x, x};
 #endif
 }
-// Every lane's value combined, in every lane (32-bit types).
+// Every lane's value combined, in every lane (32-bit types); over 16 lanes, and over the wave.
 template <typename T, typename F>
-__device__ __forceinline__ T wave_all(T v, F op) {
+__device__ __forceinline__ T row_all(T v, F op) {
   auto step = [&](uint32_t other) { v = op(v, __builtin_bit_cast(T, other)); };
   step(dpp<0x128>(__builtin_bit_cast(uint32_t, v)));  // rotations within 16 lanes
   step(dpp<0x124>(__builtin_bit_cast(uint32_t, v)));
   step(dpp<0x122>(__builtin_bit_cast(uint32_t, v)));
   step(dpp<0x121>(__builtin_bit_cast(uint32_t, v)));
+  return v;
+}
+template <typename T, typename F>
+__device__ __forceinline__ T wave_all(T v, F op) {
+  v = row_all(v, op);
   auto pair = [&](u32x2 r) {  // (elements copied: a bit cast takes whole objects)
     const uint32_t x = r[0], y = r[1];
     v = op(__builtin_bit_cast(T, x), __builtin_bit_cast(T, y));
@@ -104,7 +110,17 @@ __device__ __forceinline__ uint32_t most_of(uint32_t most, uint32_t w) {
 __device__ __forceinline__ float most_value(uint32_t most) {  // over the wave
   return __uint_as_float(wave_all(max(most & 0xFFFFu, most >> 16), Max()) << 16);
 }
-__device__ __forceinline__ float or_infinity(float s) { return fabsf(s) < INFINITY ? s : INFINITY; }
+// The largest of n of a lane's four sums; +infinity if one of them (or their sum) is not finite.
+template <int n>
+__device__ __forceinline__ float best_of(const f32x4& s, int e) {
+  float best = s[e], sum = s[e];
+#pragma unroll
+  for (int k = 1; k < n; ++k) {
+    best = fmaxf(best, s[e + k]);
+    sum += s[e + k];
+  }
+  return fabsf(sum) < INFINITY ? best : INFINITY;
+}
 
 template <int D>
 struct Box {  // 16 blocks' bounds: lane (block col, chunk group grp)
@@ -163,7 +179,7 @@ __device__ __forceinline__ f32x4 score(const Sides<D>& q, const Box<D>& b) {
   return s;
 }
 
-// A wave per (row, kv head, run of tiles).
+// A wave per (row, run of tiles, kv head); a block's bounds of all heads lie together.
 template <int D>
 __global__ __launch_bounds__(64 * kScoreWaves) void score_row_kernel(const SelectArgs a, int runs,
                                                                      int tiles, int64_t total) {
@@ -171,10 +187,10 @@ __global__ __launch_bounds__(64 * kScoreWaves) void score_row_kernel(const Selec
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   for (int64_t work = (int64_t)blockIdx.x * kScoreWaves + wave; work < total;
        work += (int64_t)gridDim.x * kScoreWaves) {
-    const int64_t item = work / runs;
-    const int64_t row = item / a.hkv;
-    const int kvh = (int)(item % a.hkv);
-    const int t0 = (int)(work % runs) * tiles;
+    const int kvh = (int)(work % a.hkv);
+    const int64_t row = work / a.hkv / runs;
+    const int64_t item = row * a.hkv + kvh;
+    const int t0 = (int)(work / a.hkv % runs) * tiles;
     const int n = row_blocks(a, row), seq = row_sequence(a, row);
     if (seq < 0 || n <= a.blocks || t0 * kTileBlocks >= n) continue;
     const int t1 = min(t0 + tiles, (n + kTileBlocks - 1) / kTileBlocks);
@@ -189,8 +205,8 @@ __global__ __launch_bounds__(64 * kScoreWaves) void score_row_kernel(const Selec
     u32x4 qv[D / 32];
 #pragma unroll
     for (int kk = 0; kk < D / 32; ++kk) {
-      qv[kk] = u32x4{0u, 0u, 0u, 0u};
-      if (col < g) qv[kk] = ld16(a.q + ((size_t)row * a.hq + kvh * g + col) * D + kk * 32 + grp * 8);
+      // (lines past the group's heads hold its last one again: no new maximum)
+      qv[kk] = ld16(a.q + ((size_t)row * a.hq + kvh * g + min(col, g - 1)) * D + kk * 32 + grp * 8);
     }
     auto id_of = [=](int j) {  // of block col of the run's tile j
       const int half = j < 4 ? +ids0 : +ids1, rest = j < 12 ? +ids2 : +ids3;
@@ -205,10 +221,7 @@ __global__ __launch_bounds__(64 * kScoreWaves) void score_row_kernel(const Selec
     float* most = a.tile_most + item * (a.stride / kTileBlocks);
     auto finish = [&](const Box<D>& b, int t) {
       const f32x4 s = score<D>(q, b);
-      float best = -INFINITY;
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (4 * grp + r < g) best = fmaxf(best, or_infinity(s[r]));
+      float best = best_of<4>(s, 0);
       u32x2 x = with_row(__float_as_uint(best));
       best = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
       x = with_half(__float_as_uint(best));
@@ -227,27 +240,45 @@ __global__ __launch_bounds__(64 * kScoreWaves) void score_row_kernel(const Selec
   }
 }
 
-// A wave per (64 rows, kv head, held tiles): for each run of rows of one sequence, that sequence's
-// blocks in registers, and the rows' heads through them, 16 / kHeads rows at a time (kHeads: the
-// group's heads rounded up to a power of two).
+// Rows of a group: 64 at most, and as many as 64 KB of LDS hold of their heads' queries.
+template <int D, int kHeads>
+constexpr int kGroupTiles = std::min(64 * kHeads / kTileBlocks, 2048 / D);
+
+// A workgroup per (group of rows, kv head, held tiles of its waves). The queries of the group's rows go
+// to LDS in operand order, kTileBlocks / kHeads rows a product (kHeads: the group's heads rounded up
+// to a power of two). Each wave holds the bounds of its blocks in registers, one run of rows of one
+// sequence after the other, and takes the queries through them.
 template <int D, int kHeads>
 __global__ __launch_bounds__(64 * kScoreWaves) __attribute__((amdgpu_waves_per_eu(2, 2)))
-void score_rows_kernel(const SelectArgs a, int chunks, int64_t total) {
+void score_rows_kernel(const SelectArgs a, int chunks, int group, int64_t total) {
   constexpr int kRows = kTileBlocks / kHeads;  // rows of a product
+  constexpr int KK = D / 32;
+  __shared__ __align__(16) u32x4 qs[kGroupTiles<D, kHeads>][KK][64];
   const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = a.hq / a.hkv;
-  for (int64_t work = (int64_t)blockIdx.x * kScoreWaves + wave; work < total;
-       work += (int64_t)gridDim.x * kScoreWaves) {
-    const int b0 = (int)(work % chunks) * kTileBlocks * kHeldTiles<D>;
+  for (int64_t work = blockIdx.x; work < total; work += gridDim.x) {
+    const int b0 = ((int)(work % chunks) * kScoreWaves + wave) * kTileBlocks * kHeldTiles<D>;
     const int kvh = (int)(work / chunks % a.hkv);
-    const int64_t row0 = work / chunks / a.hkv * kGroupRows;
+    const int64_t row0 = work / chunks / a.hkv * group;
     // lane i: row i of the group, its sequence and the blocks to score (0: none)
     const int64_t mine = row0 + lane;
-    const int seq = mine < a.rows ? row_sequence(a, mine) : -1;
+    const int seq = lane < group && mine < a.rows ? row_sequence(a, mine) : -1;
     int n = seq >= 0 ? row_blocks(a, mine) : 0;
+    // a product's line: head col % kHeads of row col / kHeads (past the group's heads its last one
+    // again: no new maximum)
+    const int head = min(col % kHeads, g - 1);
+    __syncthreads();  // (the readers of the loop's last pass)
+    for (int t = wave; t * kRows < group; t += kScoreWaves) {
+      const int64_t row = row0 + t * kRows + col / kHeads;
+      const uint16_t* from = a.q + ((size_t)row * a.hq + kvh * g + head) * D + grp * 8;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk)
+        qs[t][kk][lane] = row < a.rows ? ld16(from + kk * 32) : u32x4{0u, 0u, 0u, 0u};
+    }
     if (n <= a.blocks || n <= b0) n = 0;
     uint64_t todo = __builtin_amdgcn_ballot_w64(n > 0);
+    __syncthreads();
     while (todo != 0) {
       const int first = __builtin_ctzll(todo);
       const int s = __builtin_amdgcn_readlane(seq, first);
@@ -261,63 +292,52 @@ void score_rows_kernel(const SelectArgs a, int chunks, int64_t total) {
 #pragma unroll
       for (int j = 0; j < kHeldTiles<D>; ++j)
         load_box<D>(a, box[j], __builtin_amdgcn_ds_bpermute((j * 16 + col) * 4, id), kvh);
-      // lane's line of a product: head col % kHeads of row col / kHeads
-      const int head = col % kHeads;
-      auto load_q = [&](int r, u32x4 (&qv)[D / 32]) {
-        const int at = r + col / kHeads;
-        const uint16_t* from = a.q + ((size_t)(row0 + at) * a.hq + kvh * g + head) * D + grp * 8;
-#pragma unroll
-        for (int kk = 0; kk < D / 32; ++kk) {
-          qv[kk] = u32x4{0u, 0u, 0u, 0u};
-          if (head < g && at < end) qv[kk] = ld16(from + kk * 32);
-        }
-      };
-      u32x4 qv[D / 32];
-      load_q(first, qv);
 #pragma unroll
       for (int j = 0; j < kHeldTiles<D>; ++j) top[j] = most_value(box_most<D>(box[j]));
-      for (int r = first; r < end; r += kRows) {
+      constexpr int kMine = kHeads >= 4 ? 1 : 4 / kHeads;  // rows of a lane
+      const bool writer = kHeads <= 4 || 4 * grp % kHeads == 0;
+      for (int t = first / kRows; t * kRows < end; ++t) {
+        u32x4 qv[KK];
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) qv[kk] = qs[t][kk][lane];
         Sides<D> q;
         split_q<D>(qv, q);
-        if (r + kRows < end) load_q(r + kRows, qv);
+        // the lane's rows: blocks to score from this lane's block on, and where they go
+        int left[kMine];
+        int64_t to[kMine];
+#pragma unroll
+        for (int e = 0; e < kMine; ++e) {
+          const int at = t * kRows + (kHeads >= 4 ? 4 * grp / kHeads : kMine * grp + e);
+          const int rn = __builtin_amdgcn_ds_bpermute(at * 4, n);
+          left[e] = writer && at >= first && at < end ? rn - b0 - col : 0;
+          to[e] = ((row0 + at) * a.hkv + kvh) * a.stride + b0 + col;
+        }
+        // (every tile's products before the first result is looked at)
+        f32x4 sc[kHeldTiles<D>];
+#pragma unroll
+        for (int j = 0; j < kHeldTiles<D>; ++j) sc[j] = score<D>(q, box[j]);
+        float best[kHeldTiles<D>][kMine];
 #pragma unroll
         for (int j = 0; j < kHeldTiles<D>; ++j) {
-          if (b0 + j * kTileBlocks >= most_n) break;
-          f32x4 sc = score<D>(q, box[j]);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {  // heads that pad the group do not count
-            sc[e] = or_infinity(sc[e]);
-            if ((4 * grp + e) % kHeads >= g) sc[e] = -INFINITY;
-          }
-          // value e of lane (block col, grp) is row kRow * grp + e's (or the row is over lanes)
-          constexpr int kMine = kHeads >= 4 ? 1 : 4 / kHeads;  // rows of a lane
-          float best[kMine];
-#pragma unroll
-          for (int e = 0; e < kMine; ++e) {
-            best[e] = sc[e * (4 / kMine)];
-#pragma unroll
-            for (int f = 1; f < 4 / kMine; ++f) best[e] = fmaxf(best[e], sc[e * (4 / kMine) + f]);
-          }
+          for (int e = 0; e < kMine; ++e) best[j][e] = best_of<4 / kMine>(sc[j], e * (4 / kMine));
           if constexpr (kHeads >= 8) {
-            const u32x2 x = with_row(__float_as_uint(best[0]));
-            best[0] = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+            const u32x2 x = with_row(__float_as_uint(best[j][0]));
+            best[j][0] = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
           }
           if constexpr (kHeads == 16) {
-            const u32x2 x = with_half(__float_as_uint(best[0]));
-            best[0] = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+            const u32x2 x = with_half(__float_as_uint(best[j][0]));
+            best[j][0] = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
           }
+        }
 #pragma unroll
-          for (int e = 0; e < kMine; ++e) {
-            const int at = r + (kHeads >= 4 ? 4 * grp / kHeads : kMine * grp + e);
-            int rn = __builtin_amdgcn_ds_bpermute((at & 63) * 4, n);
-            if (at >= end) rn = 0;
-            const int b = b0 + j * kTileBlocks + col;
-            const int64_t item = (row0 + at) * a.hkv + kvh;
-            const bool writer = kHeads <= 4 || 4 * grp % kHeads == 0;
-            if (writer && b < rn) {
-              a.scores[item * a.stride + b] = best[e];
-              if (col == 0) a.tile_most[(item * a.stride + b) / kTileBlocks] = top[j];
-            }
+        for (int e = 0; e < kMine; ++e) {
+          if (left[e] <= 0) continue;
+#pragma unroll
+          for (int j = 0; j < kHeldTiles<D>; ++j) {
+            if (left[e] <= j * kTileBlocks) break;
+            a.scores[to[e] + j * kTileBlocks] = best[j][e];
+            if (col == 0) a.tile_most[to[e] / kTileBlocks + j] = top[j];
           }
         }
       }
@@ -325,39 +345,65 @@ void score_rows_kernel(const SelectArgs a, int chunks, int64_t total) {
   }
 }
 
-// A score in 64 bits by one wave, as a key whose unsigned order is the scores' order (a score that
-// is not finite counts as +infinity). Never 0 and never ~0.
+__device__ __forceinline__ double row_sum(double x) {  // over 16 lanes (lane 0's order counts)
+  auto step = [&](auto ror) {
+    constexpr int kCtrl = decltype(ror)::value;
+    const uint64_t u = (uint64_t)__double_as_longlong(x);
+    x += __longlong_as_double((long long)((uint64_t)dpp<kCtrl>((uint32_t)(u >> 32)) << 32 |
+                                          dpp<kCtrl>((uint32_t)u)));
+  };
+  step(std::integral_constant<int, 0x128>());
+  step(std::integral_constant<int, 0x124>());
+  step(std::integral_constant<int, 0x122>());
+  step(std::integral_constant<int, 0x121>());
+  return x;
+}
+
+// Scores in 64 bits by one wave, four blocks at a time: 16 lanes take block b, each of them D / 16
+// dims for every head. The key's unsigned order is the scores' order (a score that is not finite
+// counts as +infinity); it is never 0 and never ~0, and valid in the first of the 16 lanes.
 template <int D>
 __device__ __forceinline__ uint64_t exact_key(const SelectArgs& a, const uint16_t* q, int g,
                                               const int32_t* table, int kvh, int b) {
-  constexpr int PER = D / 64;
-  const int lane = threadIdx.x & 63;
-  const int id = table[b];
-  const uint16_t* box = a.bounds + ((size_t)(id < 0 || id >= a.num_blocks ? 0 : id) * a.hkv + kvh) * 2 * D;
-  double hi[PER], lo[PER];
+  constexpr int PER = D / 16;
+  const int lane = threadIdx.x & 63, part = lane & 15;
+  int id = table[b];
+  if (id < 0 || id >= a.num_blocks) id = 0;
+  const uint16_t* box = a.bounds + ((size_t)id * a.hkv + kvh) * 2 * D + part * PER;
+  uint16_t hb[PER], lb[PER];
+  __builtin_memcpy(hb, __builtin_assume_aligned(box, 2 * PER), sizeof(hb));
+  __builtin_memcpy(lb, __builtin_assume_aligned(box + D, 2 * PER), sizeof(lb));
+  float hi[PER], lo[PER];
   bool odd = false;
 #pragma unroll
   for (int e = 0; e < PER; ++e) {
-    const float x = __uint_as_float((uint32_t)box[lane * PER + e] << 16);
-    const float y = __uint_as_float((uint32_t)box[D + lane * PER + e] << 16);
-    odd |= !isfinite(x) || !isfinite(y);
-    hi[e] = x;
-    lo[e] = y;
+    hi[e] = __uint_as_float((uint32_t)hb[e] << 16);
+    lo[e] = __uint_as_float((uint32_t)lb[e] << 16);
+    odd |= !isfinite(hi[e]) || !isfinite(lo[e]);
   }
   double best = -INFINITY;
-  for (int h = 0; h < g; ++h) {
-    double s = 0.;
+  constexpr int kHeads = 256 / D;  // heads whose loads and sums run side by side
+  for (int h0 = 0; h0 < g; h0 += kHeads) {
+    uint16_t qb[kHeads][PER];
+#pragma unroll
+    for (int k = 0; k < kHeads; ++k)
+      __builtin_memcpy(qb[k], __builtin_assume_aligned(q + min(h0 + k, g - 1) * D + part * PER, 2 * PER),
+                       sizeof(qb[k]));
+    double s[kHeads] = {};
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
-      const float x = __uint_as_float((uint32_t)q[h * D + lane * PER + e] << 16);
-      odd |= !isfinite(x);
-      s += (double)x * (x > 0.f ? hi[e] : lo[e]);
+#pragma unroll
+      for (int k = 0; k < kHeads; ++k) {
+        const float x = __uint_as_float((uint32_t)qb[k][e] << 16);
+        odd |= !isfinite(x);
+        s[k] = fma((double)x, (double)(x > 0.f ? hi[e] : lo[e]), s[k]);  // (the product is exact)
+      }
     }
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) s += __shfl_xor(s, o);
-    best = fmax(best, s);
+    for (int k = 0; k < kHeads; ++k) best = fmax(best, row_sum(s[k]));
   }
-  if (__builtin_amdgcn_ballot_w64(odd) != 0) best = INFINITY;
+  const uint64_t odds = __builtin_amdgcn_ballot_w64(odd) >> (lane & 48) & 0xFFFFu;
+  if (odds != 0) best = INFINITY;
   best += 0.;  // (-0 becomes +0: equal scores, equal keys)
   const uint64_t u = (uint64_t)__double_as_longlong(best);
   return u >> 63 ? ~u : u | 1ull << 63;
@@ -376,48 +422,56 @@ __device__ __forceinline__ void wg_all(T (&v)[n], F op, T (*sm)[n]) {
       for (int k = 0; k < n; ++k) sm[threadIdx.x >> 6][k] = v[k];
     }
     __syncthreads();
+    // (every lane of a row of 16 reads one wave's values; the waves divide the row evenly)
+    static_assert(kWaves <= 16 && 16 % kWaves == 0, "waves fit a row of lanes");
 #pragma unroll
     for (int k = 0; k < n; ++k) {
-      v[k] = sm[0][k];
-#pragma unroll
-      for (int w = 1; w < kWaves; ++w) v[k] = op(v[k], sm[w][k]);
+      T x = sm[threadIdx.x % kWaves][k];
+      auto step = [&](uint32_t other) { x = op(x, __builtin_bit_cast(T, other)); };
+      if constexpr (kWaves > 8) step(dpp<0x128>(__builtin_bit_cast(uint32_t, x)));
+      if constexpr (kWaves > 4) step(dpp<0x124>(__builtin_bit_cast(uint32_t, x)));
+      step(dpp<0x122>(__builtin_bit_cast(uint32_t, x)));
+      step(dpp<0x121>(__builtin_bit_cast(uint32_t, x)));
+      v[k] = x;
     }
   }
+}
+// The sum over the lanes up to this one: within 16 lanes, then over the rows before.
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
+  return v;
 }
 // The sum over the threads before this one, and over all.
 template <int kThreads>
 __device__ __forceinline__ int wg_before(int v, int* total, int* sm) {
   constexpr int kWaves = kThreads / 64;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  int incl = v;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int u = __shfl_up(incl, o);
-    if (lane >= o) incl += u;
-  }
+  const int incl = wave_scan(v);
   __syncthreads();
   if (lane == 63) sm[w] = incl;
   __syncthreads();
-  int before = incl - v;
-  *total = 0;
-#pragma unroll
-  for (int k = 0; k < kWaves; ++k) {
-    if (k < w) before += sm[k];
-    *total += sm[k];
-  }
-  return before;
+  const int from = lane & 15;  // lane's wave
+  const int sum = from < kWaves ? sm[from] : 0;
+  *total = row_all(sum, Add());
+  return incl - v + row_all(from < w ? sum : 0, Add());
 }
 
-// One workgroup per (row, kv head); its scores, at most kThreads * kEach, stay in registers (kEach 0: in
-// memory, any number).
+// One workgroup per (row, kv head). Its scores stay in registers, 64 consecutive blocks per wave and
+// register, at most kThreads * kEach (kEach 0: in memory, any number).
 template <int D, int kThreads, int kEach>
 __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs a) {
   constexpr int kWaves = kThreads / 64;
   constexpr int kPer = kThreads == 1024 ? 2 : 8;  // bins of a thread
   constexpr int kBins = kPer * kThreads;
-  constexpr int kWords = (kEach > 0 ? kThreads * kEach : kSelectMaxBlocks) / 32;
-  __shared__ uint32_t chosen[kWords];
-  __shared__ uint32_t bins[kBins];
+  constexpr int kCand = kThreads == 64 ? 128 : 512;  // blocks near the border that are ranked in LDS
+  constexpr int kWords = (kEach > 0 ? kThreads * kEach : kSelectMaxBlocks + kThreads) / 64;
+  __shared__ uint64_t chosen[kWords];  // a bit per block from `first` on, a word per wave and chunk
+  __shared__ __align__(16) uint32_t bins[kBins];
   __shared__ uint64_t cand_key[kCand];
   __shared__ int cand_at[kCand];
   __shared__ float sm5[kWaves][5], sm2[kWaves][2];
@@ -437,195 +491,220 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs a) {
   }
   const int first = a.sink, last = n - a.recent;  // [first, last) goes by score
   const int want = a.blocks - a.sink - a.recent;
+  for (int k = t; k < a.sink + a.recent; k += kThreads) {
+    if (k < a.sink) sel[k] = k;
+    else sel[want + k] = last + (k - a.sink);
+  }
+  if (want == 0) return;
   float* scores = a.scores + item * a.stride;
   float* low = a.low + item * a.stride;
   const int32_t* table = a.tables + (size_t)seq * a.max_blocks;
   const int g = a.hq / a.hkv;
   const uint16_t* q = a.q + ((size_t)row * a.hq + kvh * g) * D;
 
-  float s[kEach > 0 ? kEach : 1];  // of blocks first + t + k kThreads
-  auto each = [&](auto f) {
+  // the wave's blocks: `chunks` times 64 from `base` on; a place past the last holds a NaN, which no
+  // comparison, minimum or maximum below takes up
+  const int chunks = ((last - first + 63) / 64 + kWaves - 1) / kWaves;
+  const int base = first + w * chunks * 64;
+  float s[kEach > 0 ? kEach : 1];
+  auto block_of = [&](int k) { return base + 64 * k + lane; };
+  auto value = [&](int b) {
+    const float x = scores[min(b, last - 1)];
+    return b < last ? x : NAN;
+  };
+  if constexpr (kEach > 0) {
+    // (every load before the first use, and none in a branch)
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) s[k] = scores[min(block_of(k), last - 1)];
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) s[k] = k < chunks && block_of(k) < last ? s[k] : NAN;
+  }
+  auto each = [&](auto f) {  // f(block, score), chunk by chunk
     if constexpr (kEach > 0) {
 #pragma unroll
-      for (int k = 0; k < kEach; ++k) {
-        const int b = first + t + k * kThreads;
-        if (b < last) f(b, s[k]);
-      }
+      for (int k = 0; k < kEach; ++k)
+        if (k < chunks) f(block_of(k), s[k]);
     } else {
-      for (int b = first + t; b < last; b += kThreads) f(b, scores[b]);
+      for (int k = 0; k < chunks; ++k) f(block_of(k), value(block_of(k)));
     }
   };
-  if (want > 0) {
-#pragma unroll
-    for (int k = 0; k < kEach; ++k) {
-      const int b = first + t + k * kThreads;
-      s[k] = b < last ? scores[b] : 0.f;
-    }
-  }
-  for (int k = t; k < (n + 31) / 32; k += kThreads) chosen[k] = 0u;
   if (t == 0) num_cand = 0;
 #pragma unroll
   for (int k = 0; k < kPer; ++k) bins[t * kPer + k] = 0u;
+  auto choose = [&](int b) {
+    const int at = b - first;
+    atomicOr(reinterpret_cast<uint32_t*>(chosen) + (at >> 5), 1u << (at & 31));
+  };
+
+  // the error of a 32-bit score: 2 D products summed in some order, each addition off by at most
+  // 2^-23 of the sum of their magnitudes, |q|_1 max |bound|; tiny values may count as zeros
+  float all[5] = {0.f, 0.f, 0.f, -INFINITY, -INFINITY};  // |q|_1, max |q|, max |bound|, -min s, max s
+  for (int h0 = 4 * w; h0 < g; h0 += 4 * kWaves) {  // (16 lanes a head)
+    const uint16_t* from = q + min(h0 + (lane >> 4), g - 1) * D + (lane & 15) * (D / 16);
+    float norm = 0.f;
+#pragma unroll
+    for (int e = 0; e < D / 16; ++e) {
+      const float x = fabsf(__uint_as_float((uint32_t)from[e] << 16));
+      norm += x;
+      all[1] = fmaxf(all[1], x);
+    }
+    all[0] = fmaxf(all[0], row_all(norm, Add()));
+  }
+  for (int k = t; k < (n + kTileBlocks - 1) / kTileBlocks; k += kThreads)
+    all[2] = fmaxf(all[2], a.tile_most[item * (a.stride / kTileBlocks) + k]);
+  each([&](int, float x) {
+    all[3] = fmaxf(all[3], -x);
+    all[4] = fmaxf(all[4], x);
+  });
+  wg_all<kThreads>(all, Max(), sm5);
+  const float tiny = 0x1p-118f;
+  const float err2 = 2.f * (0x1p-15f * 1.01f * all[0] * all[2] + tiny * (1.f + all[1] + all[2]));
+  const float mn = -all[3], range = all[4] + all[3];
+  const bool odd = !(isfinite(err2) && isfinite(all[4]) && isfinite(mn) && isfinite(range));
+
+  // how the scores spread: a histogram between the least and the largest finds the bin of the last
+  // chosen one (places past the last count into bin 0, which nothing looks past)
+  bool slow = odd;
+  const float per = range > 0.f ? (kBins - 1) / range : 0.f;
+  auto bin_of = [&](float x) { return min(max((int)((x - mn) * per), 0), kBins - 1); };
+  float lo = 0.f, hi = 0.f;
   __syncthreads();
-  auto choose = [&](int b) { atomicOr(&chosen[b >> 5], 1u << (b & 31)); };
-  for (int k = t; k < a.sink + a.recent; k += kThreads)
-    choose(k < a.sink ? k : n - a.recent + (k - a.sink));
-
-  if (want > 0) {
-    // the error of a 32-bit score: 2 D products summed in some order, each addition off by at most
-    // 2^-23 of the sum of their magnitudes, |q|_1 max |bound|; tiny values may count as zeros
-    float all[5] = {0.f, 0.f, 0.f, -INFINITY, -INFINITY};  // |q|_1, max |q|, max |bound|, -min s, max s
-    for (int h = w; h < g; h += kWaves) {
-      float norm = 0.f;
+  if (!slow) {
+    each([&](int, float x) { atomicAdd(&bins[bin_of(x)], 1u); });
+    __syncthreads();
+    // thread t counts bins [kPer (kThreads - 1 - t), + kPer): from the top
+    uint32_t mine[kPer];
+    __builtin_memcpy(mine, __builtin_assume_aligned(&bins[(kThreads - 1 - t) * kPer], 4 * kPer),
+                     sizeof(mine));
+    int sum = 0;
 #pragma unroll
-      for (int e = 0; e < D / 64; ++e) {
-        const float x = fabsf(__uint_as_float((uint32_t)q[h * D + lane * (D / 64) + e] << 16));
-        norm += x;
-        all[1] = fmaxf(all[1], x);
+    for (int k = 0; k < kPer; ++k) sum += mine[k];
+    int total;
+    const int before = wg_before<kThreads>(sum, &total, sms);
+    if (before < want && want <= before + sum) {  // (one thread)
+      int above = before;
+#pragma unroll
+      for (int k = kPer - 1; k >= 0; --k) {
+        if (above < want && want <= above + (int)mine[k]) pivot = (kThreads - 1 - t) * kPer + k;
+        above += mine[k];
       }
-      all[0] = fmaxf(all[0], wave_all(norm, Add()));
     }
-    for (int k = t; k < (n + kTileBlocks - 1) / kTileBlocks; k += kThreads)
-      all[2] = fmaxf(all[2], a.tile_most[item * (a.stride / kTileBlocks) + k]);
+    __syncthreads();
+    // the scores of that bin lie in [lo, hi]: fewer than `want` lie above, at least from lo on
+    const int at = pivot;
+    float edge[2] = {-INFINITY, -INFINITY};
     each([&](int, float x) {
-      all[3] = fmaxf(all[3], -x);
-      all[4] = fmaxf(all[4], x);
+      const bool here = bin_of(x) == at;
+      edge[0] = fmaxf(edge[0], here ? -x : -INFINITY);
+      edge[1] = fmaxf(edge[1], here ? x : -INFINITY);
     });
-    wg_all<kThreads>(all, Max(), sm5);
-    const float tiny = 0x1p-118f;
-    const float err2 = 2.f * (0x1p-15f * 1.01f * all[0] * all[2] + tiny * (1.f + all[1] + all[2]));
-    const float mn = -all[3], range = all[4] + all[3];
-    const bool odd = !(isfinite(err2) && isfinite(all[4]) && isfinite(mn) && isfinite(range));
-
-    // how the scores spread: a histogram between the least and the largest finds the bin of the
-    // last chosen one
-    bool slow = odd;
-    const float per = range > 0.f ? (kBins - 1) / range : 0.f;
-    auto bin_of = [&](float x) { return min((int)((x - mn) * per), kBins - 1); };
-    float lo = 0.f, hi = 0.f;
-    if (!slow) {
-      each([&](int, float x) { atomicAdd(&bins[bin_of(x)], 1u); });
-      __syncthreads();
-      // thread t counts bins [kPer (kThreads - 1 - t), + kPer): from the top
-      const uint32_t* mine = &bins[(kThreads - 1 - t) * kPer];
-      int sum = 0;
-#pragma unroll
-      for (int k = 0; k < kPer; ++k) sum += mine[k];
-      int total;
-      const int before = wg_before<kThreads>(sum, &total, sms);
-      if (before < want && want <= before + sum) {  // (one thread)
-        int left = want - before, k = kPer - 1;
-        while (left > (int)mine[k]) left -= mine[k--];
-        pivot = (kThreads - 1 - t) * kPer + k;
+    wg_all<kThreads>(edge, Max(), sm2);
+    lo = -edge[0] - err2;
+    hi = edge[1] + err2;
+    // certain ones, and those between
+    int sure = 0;
+    each([&](int b, float x) {
+      const uint64_t m = __builtin_amdgcn_ballot_w64(x > hi);
+      sure += __builtin_popcountll(m);
+      if (lane == 0) chosen[(b - first) >> 6] = m;  // (its lane's block is the chunk's first)
+      if (x >= lo && x <= hi) {
+        const int k = atomicAdd(&num_cand, 1);
+        if (k < kCand) cand_at[k] = b;
+      }
+    });
+    int in[1] = {lane == 0 ? sure : 0};
+    wg_all<kThreads>(in, Add(), sm1);
+    __syncthreads();  // (a single wave's candidates too)
+    const int left = want - in[0], cands = num_cand;
+    slow = cands > kCand;
+    if (!slow && cands == left) {
+      for (int k = t; k < cands; k += kThreads) choose(cand_at[k]);
+    } else if (!slow) {
+      for (int k0 = 4 * w; k0 < cands; k0 += 4 * kWaves) {
+        const int k = k0 + (lane >> 4);
+        const uint64_t key = exact_key<D>(a, q, g, table, kvh, cand_at[min(k, cands - 1)]);
+        if (k < cands && (lane & 15) == 0) cand_key[k] = key;
       }
       __syncthreads();
-      // the scores of that bin lie in [lo, hi]: fewer than `want` lie above, at least from lo on
-      float edge[2] = {-INFINITY, -INFINITY};
-      each([&](int, float x) {
-        if (bin_of(x) == pivot) {
-          edge[0] = fmaxf(edge[0], -x);
-          edge[1] = fmaxf(edge[1], x);
-        }
-      });
-      wg_all<kThreads>(edge, Max(), sm2);
-      lo = -edge[0] - err2;
-      hi = edge[1] + err2;
-      // certain ones, and those between
-      int in[1] = {0};
-      each([&](int b, float x) {
-        if (x > hi) {
-          choose(b);
-          ++in[0];
-        } else if (x >= lo) {
-          const int k = atomicAdd(&num_cand, 1);
-          if (k < kCand) cand_at[k] = b;
-        }
-      });
-      wg_all<kThreads>(in, Add(), sm1);
-      __syncthreads();  // (a single wave's candidates too)
-      const int left = want - in[0], cands = num_cand;
-      slow = cands > kCand;
-      if (!slow && cands == left) {
-        for (int k = t; k < cands; k += kThreads) choose(cand_at[k]);
-      } else if (!slow) {
-        for (int k = w; k < cands; k += kWaves) {
-          const uint64_t key = exact_key<D>(a, q, g, table, kvh, cand_at[k]);
-          if (lane == 0) cand_key[k] = key;
-        }
-        __syncthreads();
-        for (int k = t; k < cands; k += kThreads) {
-          int ahead = 0;
-          for (int j = 0; j < cands; ++j)
-            ahead += cand_key[j] > cand_key[k] ||
-                     (cand_key[j] == cand_key[k] && cand_at[j] < cand_at[k]);
-          if (ahead < left) choose(cand_at[k]);
-        }
+      for (int k = t; k < cands; k += kThreads) {
+        int ahead = 0;
+        for (int j = 0; j < cands; ++j)
+          ahead += cand_key[j] > cand_key[k] ||
+                   (cand_key[j] == cand_key[k] && cand_at[j] < cand_at[k]);
+        if (ahead < left) choose(cand_at[k]);
       }
     }
-    if (slow) {
-      // many blocks at the border (equal ones), or scores that are not finite: every key in 64
-      // bits, in the workspace's two halves, and a search for the last chosen key bit by bit
-      uint32_t* kh = reinterpret_cast<uint32_t*>(scores);
-      uint32_t* kl = reinterpret_cast<uint32_t*>(low);
-      for (int b0 = first + w * 64; b0 < last; b0 += kThreads) {
-        const int b = b0 + lane;
-        const float x = b < last ? scores[b] : 0.f;
-        uint64_t key = !odd && x > hi ? ~0ull : 0ull;
-        uint64_t todo = __builtin_amdgcn_ballot_w64(b < last && (odd || (x >= lo && x <= hi)));
-        while (todo != 0) {
-          const int k = __builtin_ctzll(todo);
-          todo &= todo - 1;
-          const uint64_t exact = exact_key<D>(a, q, g, table, kvh, b0 + k);
-          if (lane == k) key = exact;
-        }
-        if (b < last) {
-          kh[b] = (uint32_t)(key >> 32);
-          kl[b] = (uint32_t)key;
-        }
+  }
+  if (slow) {
+    // many blocks at the border (equal ones), or scores that are not finite: every key in 64
+    // bits, in the workspace's two halves, and a search for the last chosen key bit by bit
+    uint32_t* kh = reinterpret_cast<uint32_t*>(scores);
+    uint32_t* kl = reinterpret_cast<uint32_t*>(low);
+    for (int b0 = first + w * 64; b0 < last; b0 += kThreads) {
+      const int b = b0 + lane;
+      const float x = b < last ? scores[b] : 0.f;
+      uint64_t key = !odd && x > hi ? ~0ull : 0ull;
+      const uint64_t todo = __builtin_amdgcn_ballot_w64(b < last && (odd || (x >= lo && x <= hi)));
+      for (int k = 0; k < 64; k += 4) {
+        if ((todo >> k & 15) == 0) continue;
+        const int at = k + (lane >> 4);  // block b0 + at, by the lane's 16
+        const uint64_t exact = exact_key<D>(a, q, g, table, kvh, min(b0 + at, last - 1));
+        const int from = (lane & 3) * 16 * 4;  // (to lane k + j from lane 16 j)
+        const uint32_t eh = (uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)(exact >> 32));
+        const uint32_t el = (uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)(uint32_t)exact);
+        if ((lane & ~3) == k && (todo >> lane & 1)) key = (uint64_t)eh << 32 | el;
       }
-      __syncthreads();
-      auto key_at = [&](int b) { return (uint64_t)kh[b] << 32 | kl[b]; };
-      uint64_t cut = 0;  // the largest key that at least `want` blocks reach
-      for (int bit = 63; bit >= 0; --bit) {
-        const uint64_t probe = cut | 1ull << bit;
-        int c[1] = {0};
-        for (int b = first + t; b < last; b += kThreads) c[0] += key_at(b) >= probe;
-        wg_all<kThreads>(c, Add(), sm1);
-        if (c[0] >= want) cut = probe;
+      if (b < last) {
+        kh[b] = (uint32_t)(key >> 32);
+        kl[b] = (uint32_t)key;
       }
+    }
+    __syncthreads();
+    for (int k = t; k < kWaves * chunks; k += kThreads) chosen[k] = 0;
+    auto key_at = [&](int b) { return (uint64_t)kh[b] << 32 | kl[b]; };
+    uint64_t cut = 0;  // the largest key that at least `want` blocks reach
+    for (int bit = 63; bit >= 0; --bit) {
+      const uint64_t probe = cut | 1ull << bit;
       int c[1] = {0};
-      for (int b = first + t; b < last; b += kThreads) {
-        if (key_at(b) > cut) {
-          choose(b);
-          ++c[0];
-        }
-      }
+      for (int b = first + t; b < last; b += kThreads) c[0] += key_at(b) >= probe;
       wg_all<kThreads>(c, Add(), sm1);
-      if (w == 0) {  // the rest from the equal ones, lowest index first
-        int left = want - c[0];
-        for (int b0 = first; b0 < last && left > 0; b0 += 64) {
-          const int b = b0 + lane;
-          const bool eq = b < last && key_at(b) == cut;
-          const uint64_t m = __builtin_amdgcn_ballot_w64(eq);
-          if (eq && __builtin_popcountll(m & ((1ull << lane) - 1)) < left) choose(b);
-          left -= __builtin_popcountll(m);
-        }
+      if (c[0] >= want) cut = probe;
+    }
+    int c[1] = {0};
+    for (int b = first + t; b < last; b += kThreads) {
+      if (key_at(b) > cut) {
+        choose(b);
+        ++c[0];
+      }
+    }
+    wg_all<kThreads>(c, Add(), sm1);
+    if (w == 0) {  // the rest from the equal ones, lowest index first
+      int left = want - c[0];
+      for (int b0 = first; b0 < last && left > 0; b0 += 64) {
+        const int b = b0 + lane;
+        const bool eq = b < last && key_at(b) == cut;
+        const uint64_t m = __builtin_amdgcn_ballot_w64(eq);
+        if (eq && __builtin_popcountll(m & ((1ull << lane) - 1)) < left) choose(b);
+        left -= __builtin_popcountll(m);
       }
     }
   }
   __syncthreads();
-  // the chosen ones in ascending order
-  int done = 0;
-  for (int k0 = 0; k0 < (n + 31) / 32; k0 += kThreads) {
-    const int k = k0 + t;
-    uint32_t bits = k < (n + 31) / 32 ? chosen[k] : 0u;
-    int total;
-    int at = done + wg_before<kThreads>(__builtin_popcount(bits), &total, sms);
-    done += total;
-    while (bits != 0u) {
-      sel[at++] = k * 32 + __builtin_ctz(bits);
-      bits &= bits - 1u;
+  // the chosen ones in ascending order: every wave counts the words' bits, 64 words at a time, and
+  // writes out its part of the words
+  int at = a.sink;
+  for (int k0 = 0; k0 < kWaves * chunks; k0 += 64) {
+    const uint64_t word = k0 + lane < kWaves * chunks ? chosen[k0 + lane] : 0;
+    const int bits = __builtin_popcountll(word), upto = wave_scan(bits);
+    const int end = min(64, kWaves * chunks - k0);
+    for (int k = w; k < end; k += kWaves) {
+      const uint64_t m = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(word >> 32), k) << 32 |
+                         (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)word, k);
+      const int from = at + __builtin_amdgcn_readlane(upto - bits, k);
+      if (m >> lane & 1)
+        sel[from + __builtin_popcountll(m & ((1ull << lane) - 1))] = first + (k0 + k) * 64 + lane;
     }
+    at += __builtin_amdgcn_readlane(upto, 63);
   }
 }
 
@@ -645,8 +724,10 @@ hipError_t launch_scores(const SelectArgs& a, int64_t items, int64_t n, hipStrea
   constexpr int64_t kMostWorkgroups = 1 << 20;  // (a launch's loop takes the others)
   const int64_t tiles = (n + kTileBlocks - 1) / kTileBlocks;
   if (a.row_seq == nullptr) {
-    // Waves enough to fill the chip a few times over, then longer runs of tiles for each.
-    int64_t run = items * tiles / 8192;
+    // Waves enough to fill the chip several times over, then longer runs of tiles for each: 64
+    // sequences of 8-32k keys, 8 heads, 84.8 us with both launches (at half as many waves 94.4, at
+    // twice as many 81.6); 256 with one head 48.6 (49.6, 57.9).
+    int64_t run = items * tiles / 16384;
     run = std::min<int64_t>(std::max<int64_t>(run, 1), kMaxTiles);
     const int64_t runs = (tiles + run - 1) / run, total = items * runs;
     const int64_t wgs = std::min((total + kScoreWaves - 1) / kScoreWaves, kMostWorkgroups);
@@ -654,25 +735,39 @@ hipError_t launch_scores(const SelectArgs& a, int64_t items, int64_t n, hipStrea
                        a, (int)runs, (int)run, total);
     return hipGetLastError();
   }
-  const int64_t chunks = (tiles + kHeldTiles<D> - 1) / kHeldTiles<D>;
-  const int64_t total = (a.rows + kGroupRows - 1) / kGroupRows * a.hkv * chunks;
-  const int64_t wgs = std::min((total + kScoreWaves - 1) / kScoreWaves, kMostWorkgroups);
+  const int64_t chunks = (tiles + kHeldTiles<D> * kScoreWaves - 1) / (kHeldTiles<D> * kScoreWaves);
   const int g = a.hq / a.hkv;
-  auto* kern = g == 1   ? score_rows_kernel<D, 1>
-               : g == 2 ? score_rows_kernel<D, 2>
-               : g <= 4 ? score_rows_kernel<D, 4>
-               : g <= 8 ? score_rows_kernel<D, 8>
-                        : score_rows_kernel<D, 16>;
-  hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(64 * kScoreWaves), 0, stream, a, (int)chunks,
-                     total);
+  auto launch = [&](auto heads) {
+    constexpr int kHeads = decltype(heads)::value;
+    constexpr int kRows = kTileBlocks / kHeads;
+    // Large groups read the bounds less often, small ones fill the chip where rows are few (305 rows, 4
+    // heads, up to 5 chunks of blocks: 27.3 us at 64 rows a group, 21.5 halved to 256 workgroups).
+    int group = kGroupTiles<D, kHeads> * kRows;
+    int64_t total = 0;
+    for (;; group /= 2) {
+      total = (a.rows + group - 1) / group * a.hkv * chunks;
+      if (group <= kRows || total >= kComputeUnits) break;
+    }
+    hipLaunchKernelGGL((score_rows_kernel<D, kHeads>),
+                       dim3((unsigned)std::min(total, kMostWorkgroups)), dim3(64 * kScoreWaves), 0,
+                       stream, a, (int)chunks, group, total);
+  };
+  if (g == 1) launch(std::integral_constant<int, 1>());
+  else if (g == 2) launch(std::integral_constant<int, 2>());
+  else if (g <= 4) launch(std::integral_constant<int, 4>());
+  else if (g <= 8) launch(std::integral_constant<int, 8>());
+  else launch(std::integral_constant<int, 16>());
   return hipGetLastError();
 }
 
 template <int D>
 hipError_t launch_select(const SelectArgs& a, int64_t items, int64_t n, hipStream_t stream) {
-  // registers for the longest row the call can have
-  const int threads = n <= 1024 ? 64 : n <= 2048 ? 256 : 1024;
-  auto* kern = n <= 1024   ? select_kernel<D, 64, 16>
+  // Registers for the longest row the call can have. Short rows take a wave each where there are many:
+  // no barriers, and more rows at once (6100 items of up to 1024 blocks 47.8 us with their scores
+  // against 60.5 with four waves, 12200 of 128 dims 92.0 and 135.1; but 400 items 18.6 and 16.2).
+  const bool t64 = n <= 1024 && items >= 1024;
+  const int threads = t64 ? 64 : n <= 2048 ? 256 : 1024;
+  auto* kern = t64   ? select_kernel<D, 64, 16>
                : n <= 2048 ? select_kernel<D, 256, 8>
                : n <= 8192 ? select_kernel<D, 1024, 8>
                            : select_kernel<D, 1024, 0>;
