@@ -65,7 +65,7 @@ struct RopeArgs {
   int64_t q_stride, k_stride, v_stride, q_out_stride, pos_stride;
   int64_t rows;
   int32_t hq, hkv, num_blocks, rot_dim, interleaved;
-  int32_t window;  // rows of a workgroup (set by the launch)
+  int32_t window;  // log2 of a workgroup's rows (set by the launch)
   float scale;
   uint8_t axis_of[64];
   double turns[64];

@@ -435,13 +435,17 @@ def pkv_sched_run(cfg: SchedConfig, fanout, suffix, out_len, filtered, device=No
 _torch = None
 _Tensor = None
 _raw_stream = None
+_get_device = None
+_bf16 = _i32 = _i64 = _f32 = None
 
 
 def _get_torch():
-    global _torch, _Tensor, _raw_stream
+    global _torch, _Tensor, _raw_stream, _get_device, _bf16, _i32, _i64, _f32
     if _torch is None:
         import torch
         _Tensor = torch.Tensor
+        _bf16, _i32, _i64, _f32 = torch.bfloat16, torch.int32, torch.int64, torch.float32
+        _get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         _torch = torch
     return _torch
@@ -470,24 +474,39 @@ def _stream(stream):
     return torch.cuda.current_stream().cuda_stream
 
 
-def _device(stream):
-    """The current device's index, which a call launches on; an explicit stream must be its."""
-    torch = _torch or _get_torch()
-    dev = torch.cuda.current_device()
-    if stream is not None and stream.device_index != dev:
+def _launch_on(stream):
+    """The current device's index, which a call launches on, and the hipStream_t (the current
+    stream's, or that of an explicit one, which must be of this device)."""
+    if _torch is None:
+        _get_torch()
+    dev = _get_device() if _torch.cuda.is_initialized() else _torch.cuda.current_device()
+    if stream is None:
+        return dev, _raw_stream(dev) if _raw_stream is not None else _stream(None)
+    if stream.device_index != dev:
         raise ValueError(f"stream is of device {stream.device_index}, the current device is {dev}")
-    return dev
+    return dev, stream.cuda_stream
 
 
 def _ptr(t, name, dtype, dev):
     """A contiguous tensor of this type on the current device `dev`: its address."""
-    if (isinstance(t, _Tensor) and t.dtype is dtype and t.is_cuda and t.get_device() == dev
-            and t.is_contiguous()):
+    if isinstance(t, _Tensor) and t.dtype is dtype and t.get_device() == dev and t.is_contiguous():
         return t.data_ptr()
     _dev_ptr(t, name, dtype)
     if t is None:
         raise TypeError(f"{name} must be a GPU tensor (the library has no CPU path)")
     raise ValueError(f"{name} is on device {t.get_device()}, the current device is {dev}")
+
+
+def _paged_kv_on(k_cache, v_cache, dev) -> PagedKV:
+    """paged_kv of a pool on the current device."""
+    k_shape = k_cache.shape
+    if len(k_shape) != 5:
+        raise ValueError("k_cache must be [nb][Hkv][D/8][bs][8] and v_cache [nb][Hkv][D][bs]")
+    nb, hkv, nch, bs, e = k_shape
+    if e != 8 or v_cache.shape != (nb, hkv, nch * 8, bs):
+        raise ValueError("k_cache / v_cache shapes disagree")
+    return PagedKV(_ptr(k_cache, "k_cache", _bf16, dev), _ptr(v_cache, "v_cache", _bf16, dev), nb,
+                   bs, hkv, nch * 8)
 
 
 def paged_kv(k_cache, v_cache) -> PagedKV:
@@ -643,9 +662,7 @@ def pkv_extend_tables(block_tables, cached_lens, new_lens, free_blocks, free_use
     free_blocks from entry free_used [1] on, and the step's offsets, lengths and rows (int32;
     slot_map int64). status [1] holds PKV_EXTEND_* bits when the step was refused. seq_lens may
     be cached_lens, and free_used_out free_used."""
-    torch = _torch or _get_torch()
-    i32 = torch.int32
-    dev = _device(stream)
+    dev, hip_stream = _launch_on(stream)
     if block_tables.dim() != 2:
         raise ValueError("block_tables must be [num_seqs][max_blocks]")
     b, max_blocks = block_tables.shape
@@ -660,24 +677,17 @@ def pkv_extend_tables(block_tables, cached_lens, new_lens, free_blocks, free_use
         if t is not None and t.numel() != max_rows:
             raise ValueError(f"{name} must have max_rows entries")
     _check(_lib.pkv_extend_tables(
-        _ptr(block_tables, "block_tables", i32, dev), max_blocks,
-        _ptr(cached_lens, "cached_lens", i32, dev), _ptr(new_lens, "new_lens", i32, dev), b,
-        _ptr(free_blocks, "free_blocks", i32, dev), free_blocks.numel(),
-        _ptr(free_used, "free_used", i32, dev),
-        _ptr(free_used_out, "free_used_out", i32, dev),
-        _ptr(cu_new_lens, "cu_new_lens", i32, dev), _ptr(seq_lens, "seq_lens", i32, dev),
-        _ptr(status, "status", i32, dev), max_rows,
-        None if slot_map is None else _ptr(slot_map, "slot_map", torch.int64, dev),
-        None if row_seq is None else _ptr(row_seq, "row_seq", i32, dev),
-        None if positions is None else _ptr(positions, "positions", i32, dev),
-        None if row_lens is None else _ptr(row_lens, "row_lens", i32, dev), _stream(stream)))
-
-
-def _paged_kv_on(k_cache, v_cache, dev) -> PagedKV:
-    kv = paged_kv(k_cache, v_cache)
-    if k_cache.get_device() != dev or v_cache.get_device() != dev:
-        raise ValueError(f"k_cache / v_cache are not on the current device {dev}")
-    return kv
+        _ptr(block_tables, "block_tables", _i32, dev), max_blocks,
+        _ptr(cached_lens, "cached_lens", _i32, dev), _ptr(new_lens, "new_lens", _i32, dev), b,
+        _ptr(free_blocks, "free_blocks", _i32, dev), free_blocks.numel(),
+        _ptr(free_used, "free_used", _i32, dev),
+        _ptr(free_used_out, "free_used_out", _i32, dev),
+        _ptr(cu_new_lens, "cu_new_lens", _i32, dev), _ptr(seq_lens, "seq_lens", _i32, dev),
+        _ptr(status, "status", _i32, dev), max_rows,
+        None if slot_map is None else _ptr(slot_map, "slot_map", _i64, dev),
+        None if row_seq is None else _ptr(row_seq, "row_seq", _i32, dev),
+        None if positions is None else _ptr(positions, "positions", _i32, dev),
+        None if row_lens is None else _ptr(row_lens, "row_lens", _i32, dev), hip_stream))
 
 
 def rope_spec(inv_freq, axis_of=None, interleaved=False, scale=1.0, num_axes=None) -> Rope:
@@ -698,18 +708,19 @@ def rope_spec(inv_freq, axis_of=None, interleaved=False, scale=1.0, num_axes=Non
 
 def _rows_ptr(t, name, heads, dim, dev):
     """bf16 [rows][heads][dim] whose rows may lie apart: address and row stride."""
-    if not isinstance(t, _Tensor) or not t.is_cuda:
+    if not isinstance(t, _Tensor) or t.get_device() < 0:
         raise TypeError(f"{name} must be a GPU tensor (the library has no CPU path)")
-    if t.dtype is not _torch.bfloat16:
-        raise TypeError(f"{name} must be {_torch.bfloat16}, got {t.dtype}")
+    if t.dtype is not _bf16:
+        raise TypeError(f"{name} must be {_bf16}, got {t.dtype}")
     if t.get_device() != dev:
         raise ValueError(f"{name} is on device {t.get_device()}, the current device is {dev}")
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
+    shape = t.shape
+    if len(shape) != 3 or shape[1] != heads or shape[2] != dim:
         raise ValueError(f"{name} must be [rows][{heads}][{dim}]")
     s0, s1, s2 = t.stride()
     if s2 != 1 or (s1 != dim and heads > 1):
         raise ValueError(f"{name} must have contiguous heads")
-    return t.data_ptr(), s0 if t.shape[0] > 1 else heads * dim
+    return t.data_ptr(), s0 if shape[0] > 1 else heads * dim
 
 
 def pkv_rope_append(k_cache, v_cache, q, k_new, v_new, slot_map, positions, rope: Rope, q_out,
@@ -717,8 +728,7 @@ def pkv_rope_append(k_cache, v_cache, q, k_new, v_new, slot_map, positions, rope
     """q [rows][Hq][D] turned into q_out (which may be q), k_new and v_new [rows][Hkv][D] turned
     and appended at slot_map (int64 [rows]); their rows may lie apart (views of one fused
     projection). positions: int32 [rows], or [axes][rows] where rope has several axes."""
-    torch = _torch or _get_torch()
-    dev = _device(stream)
+    dev, hip_stream = _launch_on(stream)
     kv = _paged_kv_on(k_cache, v_cache, dev)
     hkv, d = kv.num_kv_heads, kv.head_dim
     n, hq = q.shape[0], q.shape[1]
@@ -732,16 +742,15 @@ def pkv_rope_append(k_cache, v_cache, q, k_new, v_new, slot_map, positions, rope
     op, os_ = _rows_ptr(q_out, "q_out", hq, d, dev)
     _check(_lib.pkv_rope_append(
         ctypes.byref(kv), ctypes.byref(rope), qp, qs, hq, kp, ks, vp, vs,
-        _ptr(slot_map, "slot_map", torch.int64, dev),
-        _ptr(positions, "positions", torch.int32, dev), n, n, op, os_, _stream(stream)))
+        _ptr(slot_map, "slot_map", _i64, dev),
+        _ptr(positions, "positions", _i32, dev), n, n, op, os_, hip_stream))
 
 
 def pkv_block_bounds(k_cache, v_cache, bounds, block_tables, cached_lens, cu_new_lens,
                      max_new_len: int, stream=None) -> None:
     """The key bounds (bf16 [num_blocks][Hkv][2][D], largest then smallest) of the blocks that
     hold new tokens."""
-    torch = _torch or _get_torch()
-    dev = _device(stream)
+    dev, hip_stream = _launch_on(stream)
     kv = _paged_kv_on(k_cache, v_cache, dev)
     if bounds.shape != (kv.num_blocks, kv.num_kv_heads, 2, kv.head_dim):
         raise ValueError("bounds must be [num_blocks][Hkv][2][D]")
@@ -749,12 +758,11 @@ def pkv_block_bounds(k_cache, v_cache, bounds, block_tables, cached_lens, cu_new
     if block_tables.dim() != 2 or block_tables.shape[0] != b or cu_new_lens.numel() != b + 1:
         raise ValueError("block_tables, cached_lens and cu_new_lens must have a row, an entry and "
                          "a step per sequence")
-    i32 = torch.int32
     _check(_lib.pkv_block_bounds(
-        ctypes.byref(kv), _ptr(bounds, "bounds", torch.bfloat16, dev),
-        _ptr(block_tables, "block_tables", i32, dev), block_tables.shape[1],
-        _ptr(cached_lens, "cached_lens", i32, dev), _ptr(cu_new_lens, "cu_new_lens", i32, dev), b,
-        int(max_new_len), _stream(stream)))
+        ctypes.byref(kv), _ptr(bounds, "bounds", _bf16, dev),
+        _ptr(block_tables, "block_tables", _i32, dev), block_tables.shape[1],
+        _ptr(cached_lens, "cached_lens", _i32, dev), _ptr(cu_new_lens, "cu_new_lens", _i32, dev), b,
+        int(max_new_len), hip_stream))
 
 
 def _workspace(t, dev):
@@ -784,9 +792,7 @@ def pkv_select_blocks(bounds, q, block_tables, row_lens, max_len: int, sink_bloc
                       recent_blocks: int, sel, row_seq=None, workspace=None, stream=None) -> None:
     """sel [rows][Hkv][blocks] receives, for each row of q [rows][Hq][D] and kv head, the logical
     blocks chosen by their key bounds [num_blocks][Hkv][2][D], ascending, then -1."""
-    torch = _torch or _get_torch()
-    bf16, i32 = torch.bfloat16, torch.int32
-    dev = _device(stream)
+    dev, hip_stream = _launch_on(stream)
     if bounds.dim() != 4 or bounds.shape[2] != 2:
         raise ValueError("bounds must be [num_blocks][Hkv][2][D]")
     nb, hkv, _, d = bounds.shape
@@ -800,11 +806,11 @@ def pkv_select_blocks(bounds, q, block_tables, row_lens, max_len: int, sink_bloc
                                                                blocks))
     ws, ws_bytes = _workspace(workspace, dev)
     _check(_lib.pkv_select_blocks(
-        _ptr(bounds, "bounds", bf16, dev), nb, hkv, d, _ptr(q, "q", bf16, dev), hq,
-        _ptr(block_tables, "block_tables", i32, dev), max_blocks, b,
-        None if row_seq is None else _ptr(row_seq, "row_seq", i32, dev),
-        _ptr(row_lens, "row_lens", i32, dev), n, int(max_len), sink_blocks, recent_blocks, blocks,
-        _ptr(sel, "sel", i32, dev), ws, ws_bytes, _stream(stream)))
+        _ptr(bounds, "bounds", _bf16, dev), nb, hkv, d, _ptr(q, "q", _bf16, dev), hq,
+        _ptr(block_tables, "block_tables", _i32, dev), max_blocks, b,
+        None if row_seq is None else _ptr(row_seq, "row_seq", _i32, dev),
+        _ptr(row_lens, "row_lens", _i32, dev), n, int(max_len), sink_blocks, recent_blocks, blocks,
+        _ptr(sel, "sel", _i32, dev), ws, ws_bytes, hip_stream))
 
 
 def pkv_sparse_workspace_bytes(rows, num_q_heads, num_kv_heads, head_dim, blocks) -> int:
@@ -815,9 +821,7 @@ def pkv_sparse_attention(k_cache, v_cache, q, block_tables, row_lens, sel, scale
                          row_seq=None, lse=None, workspace=None, stream=None) -> None:
     """Rows q [rows][Hq][D] attend over the first row_lens keys of their sequences, as far as these
     lie in the logical blocks that sel [rows][Hkv][blocks] names."""
-    torch = _torch or _get_torch()
-    bf16, i32 = torch.bfloat16, torch.int32
-    dev = _device(stream)
+    dev, hip_stream = _launch_on(stream)
     kv = _paged_kv_on(k_cache, v_cache, dev)
     n = _check_rows(q, block_tables, row_lens, row_seq)
     hkv, d, hq = kv.num_kv_heads, kv.head_dim, q.shape[1]
@@ -832,13 +836,13 @@ def pkv_sparse_attention(k_cache, v_cache, q, block_tables, row_lens, sel, scale
         workspace = alloc_workspace(pkv_sparse_workspace_bytes(n, hq, hkv, d, blocks))
     ws, ws_bytes = _workspace(workspace, dev)
     _check(_lib.pkv_sparse_attention(
-        ctypes.byref(kv), _ptr(q, "q", bf16, dev), hq,
-        _ptr(block_tables, "block_tables", i32, dev), max_blocks, b,
-        None if row_seq is None else _ptr(row_seq, "row_seq", i32, dev),
-        _ptr(row_lens, "row_lens", i32, dev), n, _ptr(sel, "sel", i32, dev), blocks, float(scale),
-        _ptr(out, "out", bf16, dev),
-        None if lse is None else _ptr(lse, "lse", torch.float32, dev), ws, ws_bytes,
-        _stream(stream)))
+        ctypes.byref(kv), _ptr(q, "q", _bf16, dev), hq,
+        _ptr(block_tables, "block_tables", _i32, dev), max_blocks, b,
+        None if row_seq is None else _ptr(row_seq, "row_seq", _i32, dev),
+        _ptr(row_lens, "row_lens", _i32, dev), n, _ptr(sel, "sel", _i32, dev), blocks, float(scale),
+        _ptr(out, "out", _bf16, dev),
+        None if lse is None else _ptr(lse, "lse", _f32, dev), ws, ws_bytes,
+        hip_stream))
 
 
 def alloc_workspace(nbytes: int, device="cuda"):
