@@ -383,7 +383,8 @@ pkv_status pkv_mixed_attention(const pkv_paged_kv* kv, int32_t num_q_heads, floa
  *     changes, *free_used_out = *free_used, seq_lens = cached_lens, cu_new_lens is 0 throughout
  *     and every row is padding.
  * seq_lens may be cached_lens and free_used_out may be free_used (a loop's step then leaves
- * the next one's input); no other arrays may overlap. max_rows <= 2^30. Zero sequences write an
+ * the next one's input; pkv_block_bounds still needs the old lengths); no other arrays may
+ * overlap. max_rows <= 2^30. Zero sequences write an
  * empty step. All arrays are device memory. */
 enum {
   PKV_EXTEND_OUT_OF_BLOCKS = 1,  /* *free_used is negative, or too few blocks are behind it */
@@ -415,8 +416,8 @@ pkv_status pkv_extend_tables(int32_t* block_tables, int32_t max_blocks,
  * (-1: padding) is skipped, in q_out too. Slots must be distinct and their blocks private to
  * their sequences. No other byte of the pool changes. q_out: bf16 [rows][num_q_heads][head_dim]
  * with its own row stride; it may be q itself (same address and stride). Addresses are 16-byte
- * aligned, row strides of q, k_new, v_new and q_out multiples of 8 elements that hold a row. At
- * most 2^28 rows. */
+ * aligned, row strides of q, k_new, v_new and q_out multiples of 8 elements that hold a row.
+ * rows * num_kv_heads stays below 2^28. */
 #define PKV_ROPE_MAX_AXES 4
 typedef struct {
   int32_t rot_dim;      /* dims turned: 0 .. head_dim, a multiple of 16 */

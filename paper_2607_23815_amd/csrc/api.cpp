@@ -546,7 +546,8 @@ pkv_status pkv_rope_append(const pkv_paged_kv* kv, const pkv_rope* rope, const v
   }
   if (rows < 0) return fail(PKV_ERR_INVALID_ARG, f + ": negative size");
   if (rows == 0) return ok();
-  if (rows > (1 << 28)) return fail(PKV_ERR_INVALID_ARG, f + ": more than 2^28 rows");
+  if (((int64_t)rows + 15) / 16 * view.hkv >= (1 << 24))  // (workgroups of a launch)
+    return fail(PKV_ERR_INVALID_ARG, f + ": 2^28 rows x kv heads or more");
   if (q == nullptr || k_new == nullptr || v_new == nullptr || slot_map == nullptr ||
       q_out == nullptr || (positions == nullptr && rope->rot_dim > 0))
     return fail(PKV_ERR_INVALID_ARG, f + ": NULL pointer");

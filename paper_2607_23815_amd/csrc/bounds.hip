@@ -15,6 +15,7 @@
 // one head 32.5 a block at a time, 25.5 by four).
 #include "device_utils.h"
 #include "launch.h"
+#include "wave_utils.h"
 
 namespace pkv {
 namespace {
@@ -37,11 +38,6 @@ __device__ __forceinline__ uint32_t pk_min(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(s16x2, a),
                                                                 __builtin_bit_cast(s16x2, b)));
 }
-template <int kCtrl>
-__device__ __forceinline__ uint32_t dpp(uint32_t x) {
-  return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, kCtrl, 0xF, 0xF, true);
-}
-
 // Lanes pair up (kCtrl); the one with `upper` set goes on with the upper half of the n words, the
 // other with the lower half, each of both lanes' values.
 template <int kCtrl, int n>

@@ -17,10 +17,10 @@
 // tokens of one dim in 16 bytes, so a run of rows that fills a half-slab is written whole by the
 // workgroup in whose window it begins (it looks up to 7 rows past the window's end); rows of a
 // half-slab only partly covered are written in 2-byte pieces, which need no read and cannot race
-// with another workgroup's. 16-byte stores go past the caches (the rows of a long prompt are more than
-// they hold): 16k rows of 32/8 heads of 128 dims 75.7 us, 5.2 TB/s, against 98.5 with ordinary stores.
-#include <algorithm>
-
+// with another workgroup's. 16-byte stores go past the caches, and a window's heads are neighbouring
+// workgroups, so that its rows are read whole at about the same time. 16k rows of 32/8 heads of 128 dims:
+// 88.8 us, 4.5 TB/s; 64/8 heads 134.9 us, 4.9 TB/s, the rate of a large copy (windows side by side instead
+// of heads 104.6 and 173.6, then with ordinary stores 108.9 and 175.3).
 #include "device_utils.h"
 #include "launch.h"
 
@@ -74,7 +74,7 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(const RopeArgs a)
   __shared__ int num_runs;
 
   const int t = threadIdx.x;
-  const int64_t t0 = (int64_t)blockIdx.x << a.window;
+  const int64_t t0 = (int64_t)(blockIdx.x / a.hkv) << a.window;
   const int n = (int)min((int64_t)1 << a.window, a.rows - t0);    // the window's rows
   const int staged = (int)min((int64_t)n + kAhead, a.rows - t0);  // with those a run can reach
   const int g = a.hq / a.hkv;
@@ -146,7 +146,7 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(const RopeArgs a)
     }
   };
 
-  int h = blockIdx.y;
+  const int h = blockIdx.x % a.hkv;  // (the heads of a window side by side: its rows are read whole)
   load_units(h, 0);
   load_v(h);
   if (t < 64) {  // the slots, and the runs that begin in the window
@@ -180,40 +180,33 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(const RopeArgs a)
     cs[r][j] = make_float2(c * a.scale, s * a.scale);
   }
   const int all = (g + 1) * kUnits << a.window;
-  for (;;) {
 #pragma unroll
-    for (int k = 0; k < kStage; ++k) {
-      const int w = k * kThreads + t;
-      if (w < staged * NCH) st16(&tile[w / NCH * ROW + w % NCH * 8], v[k]);
-    }
-    __syncthreads();
-    store_units(h, 0);
-    for (int w0 = kBatch * kThreads; w0 < all; w0 += kBatch * kThreads) {
-      load_units(h, w0);
-      store_units(h, w0);
-    }
-    // values column by column, neighbouring threads at the runs of one dim
-    for (int w = t; w < num_runs * D; w += kThreads) {
-      const int d = w / num_runs, k = w - d * num_runs;
-      const int r = runs[k][0], len = runs[k][1];
-      const int64_t s = slots[r];
-      uint16_t* dst = a.v_cache + ((s >> 4) * a.hkv + h) * SLAB + d * kBlockSize + (s & 15);
-      if (len == 8) {
-        uint16_t vals[8];
+  for (int k = 0; k < kStage; ++k) {
+    const int w = k * kThreads + t;
+    if (w < staged * NCH) st16(&tile[w / NCH * ROW + w % NCH * 8], v[k]);
+  }
+  __syncthreads();
+  store_units(h, 0);
+  for (int w0 = kBatch * kThreads; w0 < all; w0 += kBatch * kThreads) {
+    load_units(h, w0);
+    store_units(h, w0);
+  }
+  // values column by column, neighbouring threads at the runs of one dim
+  for (int w = t; w < num_runs * D; w += kThreads) {
+    const int d = w / num_runs, k = w - d * num_runs;
+    const int r = runs[k][0], len = runs[k][1];
+    const int64_t s = slots[r];
+    uint16_t* dst = a.v_cache + ((s >> 4) * a.hkv + h) * SLAB + d * kBlockSize + (s & 15);
+    if (len == 8) {
+      uint16_t vals[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) vals[e] = tile[(r + e) * ROW + d];
-        u32x4 packed;
-        __builtin_memcpy(&packed, vals, 16);
-        st16_nt(dst, packed);
-      } else {
-        for (int e = 0; e < len; ++e) dst[e] = tile[(r + e) * ROW + d];
-      }
+      for (int e = 0; e < 8; ++e) vals[e] = tile[(r + e) * ROW + d];
+      u32x4 packed;
+      __builtin_memcpy(&packed, vals, 16);
+      st16_nt(dst, packed);
+    } else {
+      for (int e = 0; e < len; ++e) dst[e] = tile[(r + e) * ROW + d];
     }
-    h += gridDim.y;
-    if (h >= a.hkv) break;
-    load_units(h, 0);
-    load_v(h);
-    __syncthreads();  // (the tile's readers)
   }
 }
 
@@ -234,7 +227,7 @@ hipError_t launch_rope_append(RopeArgs a, int head_dim, hipStream_t stream) {
   // 10.3, 7.6, 7.5, 8.4, 10.8; 100 rows of a prompt 5.2, 4.8, 4.6, 5.1, 6.1; 1344 32.1, 19.3, 13.0, 11.4, 9.4).
   a.window = 4;
   while (a.window > 0 && (((a.rows - 1) >> a.window) + 1) * a.hkv < 384) --a.window;
-  const dim3 grid((unsigned)(((a.rows - 1) >> a.window) + 1), (unsigned)std::min(a.hkv, 1024));
+  const dim3 grid((unsigned)((((a.rows - 1) >> a.window) + 1) * a.hkv));
   return head_dim == 128 ? launch_style<128>(a, grid, stream) : launch_style<64>(a, grid, stream);
 }
 

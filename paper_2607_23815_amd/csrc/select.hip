@@ -22,6 +22,7 @@
 
 #include "device_utils.h"
 #include "launch.h"
+#include "wave_utils.h"
 
 namespace pkv {
 namespace {
@@ -41,58 +42,6 @@ __device__ __forceinline__ int row_sequence(const SelectArgs& a, int64_t row) {
   const int s = a.row_seq != nullptr ? a.row_seq[row] : (int)row;
   return s >= 0 && s < a.num_seqs ? s : -1;
 }
-
-template <int kCtrl>
-__device__ __forceinline__ uint32_t dpp(uint32_t x) {
-  return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, kCtrl, 0xF, 0xF, true);
-}
-// x and its value in the lane 16 (or 32) away, in some order.
-__device__ __forceinline__ u32x2 with_row(uint32_t x) {
-#if __HIP_DEVICE_COMPILE__
-  const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-  return u32x2{r[0], r[1]};
-#else
-  return u32x2{x, x};
-#endif
-}
-__device__ __forceinline__ u32x2 with_half(uint32_t x) {
-#if __HIP_DEVICE_COMPILE__
-  const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
-  return u32x2{r[0], r[1]};
-#else
-  return u32x2{x, x};
-#endif
-}
-// Every lane's value combined, in every lane (32-bit types); over 16 lanes, and over the wave.
-template <typename T, typename F>
-__device__ __forceinline__ T row_all(T v, F op) {
-  auto step = [&](uint32_t other) { v = op(v, __builtin_bit_cast(T, other)); };
-  step(dpp<0x128>(__builtin_bit_cast(uint32_t, v)));  // rotations within 16 lanes
-  step(dpp<0x124>(__builtin_bit_cast(uint32_t, v)));
-  step(dpp<0x122>(__builtin_bit_cast(uint32_t, v)));
-  step(dpp<0x121>(__builtin_bit_cast(uint32_t, v)));
-  return v;
-}
-template <typename T, typename F>
-__device__ __forceinline__ T wave_all(T v, F op) {
-  v = row_all(v, op);
-  auto pair = [&](u32x2 r) {  // (elements copied: a bit cast takes whole objects)
-    const uint32_t x = r[0], y = r[1];
-    v = op(__builtin_bit_cast(T, x), __builtin_bit_cast(T, y));
-  };
-  pair(with_row(__builtin_bit_cast(uint32_t, v)));
-  pair(with_half(__builtin_bit_cast(uint32_t, v)));
-  return v;
-}
-struct Max {
-  __device__ float operator()(float x, float y) const { return fmaxf(x, y); }
-  __device__ uint32_t operator()(uint32_t x, uint32_t y) const { return max(x, y); }
-  __device__ int operator()(int x, int y) const { return max(x, y); }
-};
-struct Add {
-  __device__ int operator()(int x, int y) const { return x + y; }
-  __device__ float operator()(float x, float y) const { return x + y; }
-};
 
 // The parts of two bf16 with the sign bit `side`, zeros in the others' place.
 __device__ __forceinline__ uint32_t one_side(uint32_t w, int side) {
@@ -435,16 +384,6 @@ __device__ __forceinline__ void wg_all(T (&v)[n], F op, T (*sm)[n]) {
       v[k] = x;
     }
   }
-}
-// The sum over the lanes up to this one: within 16 lanes, then over the rows before.
-__device__ __forceinline__ int wave_scan(int v) {
-  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
-  return v;
 }
 // The sum over the threads before this one, and over all.
 template <int kThreads>

@@ -19,6 +19,7 @@
 
 #include "decode_impl.h"
 #include "launch.h"
+#include "wave_utils.h"
 
 namespace pkv {
 namespace {
@@ -32,9 +33,8 @@ constexpr int kParts = 4;        // waves that share an item where items are few
 constexpr int kXcds = 8;         // workgroups go to the chip's XCDs in turn
 
 template <int kCtrl>
-__device__ __forceinline__ float dpp(float x) {
-  return __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(x), kCtrl, 0xF, 0xF,
-                                                            true));
+__device__ __forceinline__ float dpp_f(float x) {
+  return __uint_as_float(dpp<kCtrl>(__float_as_uint(x)));
 }
 constexpr int kRor4 = 0x124, kRor8 = 0x128;  // rotations within 16 lanes
 
@@ -51,14 +51,14 @@ __device__ __forceinline__ u32x2 swap_rows(uint32_t a, uint32_t b) {
 // Sum (or maximum) over the ways, the columns that hold the same head.
 template <int kWays>
 __device__ __forceinline__ float ways_sum(float x) {
-  if constexpr (kWays >= 2) x += dpp<kRor8>(x);
-  if constexpr (kWays >= 4) x += dpp<kRor4>(x);
+  if constexpr (kWays >= 2) x += dpp_f<kRor8>(x);
+  if constexpr (kWays >= 4) x += dpp_f<kRor4>(x);
   return x;
 }
 template <int kWays>
 __device__ __forceinline__ float ways_max(float x) {
-  if constexpr (kWays >= 2) x = fmaxf(x, dpp<kRor8>(x));
-  if constexpr (kWays >= 4) x = fmaxf(x, dpp<kRor4>(x));
+  if constexpr (kWays >= 2) x = fmaxf(x, dpp_f<kRor8>(x));
+  if constexpr (kWays >= 4) x = fmaxf(x, dpp_f<kRor4>(x));
   return x;
 }
 

@@ -54,7 +54,7 @@ def _rope(lib, kv=None, rope=None, **kw):
     dict(q_out=None), dict(q=ctypes.c_void_p(0x3008)), dict(k=ctypes.c_void_p(0x3002)),
     dict(v=ctypes.c_void_p(0x3004)), dict(q_out=ctypes.c_void_p(0x3008)), dict(q_stride=504),
     dict(q_stride=516), dict(k_stride=248), dict(v_stride=257), dict(q_out_stride=-512),
-    dict(pos_stride=4), dict(rows=-1), dict(rows=2**28 + 1)])
+    dict(pos_stride=4), dict(rows=-1), dict(rows=2**27)])
 def test_rope_append_refuses(lib, bad):
     refused(lib, lib.PKV_ERR_INVALID_ARG, _rope(lib, **bad), "pkv_rope_append")
 
