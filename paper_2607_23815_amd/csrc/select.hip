@@ -218,15 +218,24 @@ void score_rows_kernel(const SelectArgs a, int chunks, int group, int64_t total)
     // again: no new maximum)
     const int head = min(col % kHeads, g - 1);
     __syncthreads();  // (the readers of the loop's last pass)
-    for (int t = wave; t * kRows < group; t += kScoreWaves) {
-      const int64_t row = row0 + t * kRows + col / kHeads;
+    constexpr int kMineTiles = (kGroupTiles<D, kHeads> + kScoreWaves - 1) / kScoreWaves;
+    u32x4 qv[kMineTiles][KK];  // (every load before the first is waited for; rows past the last: its)
+#pragma unroll
+    for (int k = 0; k < kMineTiles; ++k) {
+      const int64_t row = min(row0 + (wave + k * kScoreWaves) * kRows + col / kHeads, a.rows - 1);
       const uint16_t* from = a.q + ((size_t)row * a.hq + kvh * g + head) * D + grp * 8;
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk)
-        qs[t][kk][lane] = row < a.rows ? ld16(from + kk * 32) : u32x4{0u, 0u, 0u, 0u};
+        if ((wave + k * kScoreWaves) * kRows < group) qv[k][kk] = ld16(from + kk * 32);
     }
     if (n <= a.blocks || n <= b0) n = 0;
     uint64_t todo = __builtin_amdgcn_ballot_w64(n > 0);
+#pragma unroll
+    for (int k = 0; k < kMineTiles; ++k) {
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk)
+        if ((wave + k * kScoreWaves) * kRows < group) qs[wave + k * kScoreWaves][kk][lane] = qv[k][kk];
+    }
     __syncthreads();
     while (todo != 0) {
       const int first = __builtin_ctzll(todo);
@@ -411,9 +420,10 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs a) {
   constexpr int kWords = (kEach > 0 ? kThreads * kEach : kSelectMaxBlocks + kThreads) / 64;
   __shared__ uint64_t chosen[kWords];  // a bit per block from `first` on, a word per wave and chunk
   __shared__ __align__(16) uint32_t bins[kBins];
+  __shared__ __align__(16) uint16_t heads[16 * D];  // the group's queries
   __shared__ uint64_t cand_key[kCand];
   __shared__ int cand_at[kCand];
-  __shared__ float sm5[kWaves][5], sm2[kWaves][2];
+  __shared__ float sm5[kWaves][5];
   __shared__ int sm1[kWaves][1], sms[kWaves];
   __shared__ int num_cand, pivot;
   const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -452,9 +462,9 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs a) {
     return b < last ? x : NAN;
   };
   if constexpr (kEach > 0) {
-    // (every load before the first use, and none in a branch)
+    // (every load before the first use, and none in a branch; past the last score they read zeros)
 #pragma unroll
-    for (int k = 0; k < kEach; ++k) s[k] = scores[min(block_of(k), last - 1)];
+    for (int k = 0; k < kEach; ++k) s[k] = __uint_as_float(buf_ld4(scores, last * 4, block_of(k) * 4));
 #pragma unroll
     for (int k = 0; k < kEach; ++k) s[k] = k < chunks && block_of(k) < last ? s[k] : NAN;
   }
@@ -479,11 +489,14 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs a) {
   // 2^-23 of the sum of their magnitudes, |q|_1 max |bound|; tiny values may count as zeros
   float all[5] = {0.f, 0.f, 0.f, -INFINITY, -INFINITY};  // |q|_1, max |q|, max |bound|, -min s, max s
   for (int h0 = 4 * w; h0 < g; h0 += 4 * kWaves) {  // (16 lanes a head)
-    const uint16_t* from = q + min(h0 + (lane >> 4), g - 1) * D + (lane & 15) * (D / 16);
+    const int at = min(h0 + (lane >> 4), g - 1) * D + (lane & 15) * (D / 16);
+    uint16_t part[D / 16];
+    __builtin_memcpy(part, __builtin_assume_aligned(q + at, D / 8), sizeof(part));
+    __builtin_memcpy(__builtin_assume_aligned(&heads[at], D / 8), part, sizeof(part));
     float norm = 0.f;
 #pragma unroll
     for (int e = 0; e < D / 16; ++e) {
-      const float x = fabsf(__uint_as_float((uint32_t)from[e] << 16));
+      const float x = fabsf(__uint_as_float((uint32_t)part[e] << 16));
       norm += x;
       all[1] = fmaxf(all[1], x);
     }
@@ -529,17 +542,11 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs a) {
       }
     }
     __syncthreads();
-    // the scores of that bin lie in [lo, hi]: fewer than `want` lie above, at least from lo on
-    const int at = pivot;
-    float edge[2] = {-INFINITY, -INFINITY};
-    each([&](int, float x) {
-      const bool here = bin_of(x) == at;
-      edge[0] = fmaxf(edge[0], here ? -x : -INFINITY);
-      edge[1] = fmaxf(edge[1], here ? x : -INFINITY);
-    });
-    wg_all<kThreads>(edge, Max(), sm2);
-    lo = -edge[0] - err2;
-    hi = edge[1] + err2;
+    // Fewer than `want` scores lie above that bin, at least as many from its lower edge on. A score's
+    // place, (x - mn) * per, is off by less than 2^-22 of itself: 2^-20 of the range covers the edges.
+    const float width = range / (kBins - 1), slack = range * 0x1p-20f;
+    lo = mn + pivot * width - slack - err2;
+    hi = mn + (pivot + 1) * width + slack + err2;
     // certain ones, and those between
     int sure = 0;
     each([&](int b, float x) {
@@ -561,7 +568,7 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs a) {
     } else if (!slow) {
       for (int k0 = 4 * w; k0 < cands; k0 += 4 * kWaves) {
         const int k = k0 + (lane >> 4);
-        const uint64_t key = exact_key<D>(a, q, g, table, kvh, cand_at[min(k, cands - 1)]);
+        const uint64_t key = exact_key<D>(a, heads, g, table, kvh, cand_at[min(k, cands - 1)]);
         if (k < cands && (lane & 15) == 0) cand_key[k] = key;
       }
       __syncthreads();
@@ -587,7 +594,7 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs a) {
       for (int k = 0; k < 64; k += 4) {
         if ((todo >> k & 15) == 0) continue;
         const int at = k + (lane >> 4);  // block b0 + at, by the lane's 16
-        const uint64_t exact = exact_key<D>(a, q, g, table, kvh, min(b0 + at, last - 1));
+        const uint64_t exact = exact_key<D>(a, heads, g, table, kvh, min(b0 + at, last - 1));
         const int from = (lane & 3) * 16 * 4;  // (to lane k + j from lane 16 j)
         const uint32_t eh = (uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)(exact >> 32));
         const uint32_t el = (uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)(uint32_t)exact);
