@@ -79,8 +79,8 @@ hipError_t launch_block_bounds(const KvView& kv, uint16_t* bounds, const int32_t
                                hipStream_t stream);
 
 // The choice of blocks (pkv_select_blocks). Workspace, in floats: two halves of a 64-bit key per
-// (row, kv head, block) (the first is the 32-bit score before), then the largest |bound| per 16
-// blocks.
+// (row, kv head, block) (the first is the 32-bit score before), then the largest |bound| per
+// most_step * 16 blocks.
 constexpr int32_t kSelectMaxBlocks = 65536;  // blocks of a row
 struct SelectArgs {
   const uint16_t* bounds;
@@ -92,6 +92,7 @@ struct SelectArgs {
   int64_t rows;
   int32_t max_blocks, num_seqs, max_len, hq, hkv, num_blocks, blocks, sink, recent;
   int64_t stride;  // of a (row, kv head), in blocks (set by the launch, like the rest)
+  int32_t most_step;  // tiles of 16 blocks that an entry of tile_most speaks for
   float* scores;
   float* low;
   float* tile_most;

@@ -202,12 +202,13 @@ __global__ __launch_bounds__(64 * kScoreWaves) __attribute__((amdgpu_waves_per_e
 void score_rows_kernel(const SelectArgs a, int chunks, int group, int64_t total) {
   constexpr int kRows = kTileBlocks / kHeads;  // rows of a product
   constexpr int KK = D / 32;
+  constexpr int kHeld = kHeldTiles<D>;
   __shared__ __align__(16) u32x4 qs[kGroupTiles<D, kHeads>][KK][64];
   const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = a.hq / a.hkv;
   for (int64_t work = blockIdx.x; work < total; work += gridDim.x) {
-    const int b0 = ((int)(work % chunks) * kScoreWaves + wave) * kTileBlocks * kHeldTiles<D>;
+    const int b0 = ((int)(work % chunks) * kScoreWaves + wave) * kTileBlocks * kHeld;
     const int kvh = (int)(work / chunks % a.hkv);
     const int64_t row0 = work / chunks / a.hkv * group;
     // lane i: row i of the group, its sequence and the blocks to score (0: none)
@@ -244,14 +245,15 @@ void score_rows_kernel(const SelectArgs a, int chunks, int group, int64_t total)
       const int end = first + (~same == 0 ? 64 : __builtin_ctzll(~same));  // (past the run)
       const int most_n = wave_all(lane >= first && lane < end ? n : 0, Max());
       todo &= end >= 64 ? 0 : ~0ull << end;
-      Box<D> box[kHeldTiles<D>];
-      float top[kHeldTiles<D>];
+      Box<D> box[kHeld];
       const int id = a.tables[(size_t)s * a.max_blocks + min(b0 + lane, most_n - 1)];
 #pragma unroll
-      for (int j = 0; j < kHeldTiles<D>; ++j)
-        load_box<D>(a, box[j], __builtin_amdgcn_ds_bpermute((j * 16 + col) * 4, id), kvh);
+      for (int j = 0; j < kHeld; ++j)  // (column col holds neighbours, which are stored together)
+        load_box<D>(a, box[j], __builtin_amdgcn_ds_bpermute((col * kHeld + j) * 4, id), kvh);
+      uint32_t most = 0u;
 #pragma unroll
-      for (int j = 0; j < kHeldTiles<D>; ++j) top[j] = most_value(box_most<D>(box[j]));
+      for (int j = 0; j < kHeld; ++j) most = most_of(most, box_most<D>(box[j]));
+      const float top = most_value(most);
       constexpr int kMine = kHeads >= 4 ? 1 : 4 / kHeads;  // rows of a lane
       const bool writer = kHeads <= 4 || 4 * grp % kHeads == 0;
       for (int t = first / kRows; t * kRows < end; ++t) {
@@ -267,16 +269,16 @@ void score_rows_kernel(const SelectArgs a, int chunks, int group, int64_t total)
         for (int e = 0; e < kMine; ++e) {
           const int at = t * kRows + (kHeads >= 4 ? 4 * grp / kHeads : kMine * grp + e);
           const int rn = __builtin_amdgcn_ds_bpermute(at * 4, n);
-          left[e] = writer && at >= first && at < end ? rn - b0 - col : 0;
-          to[e] = ((row0 + at) * a.hkv + kvh) * a.stride + b0 + col;
+          left[e] = writer && at >= first && at < end ? rn - b0 - col * kHeld : 0;
+          to[e] = ((row0 + at) * a.hkv + kvh) * a.stride + b0;
         }
         // (every tile's products before the first result is looked at)
-        f32x4 sc[kHeldTiles<D>];
+        f32x4 sc[kHeld];
 #pragma unroll
-        for (int j = 0; j < kHeldTiles<D>; ++j) sc[j] = score<D>(q, box[j]);
-        float best[kHeldTiles<D>][kMine];
+        for (int j = 0; j < kHeld; ++j) sc[j] = score<D>(q, box[j]);
+        float best[kHeld][kMine];
 #pragma unroll
-        for (int j = 0; j < kHeldTiles<D>; ++j) {
+        for (int j = 0; j < kHeld; ++j) {
 #pragma unroll
           for (int e = 0; e < kMine; ++e) best[j][e] = best_of<4 / kMine>(sc[j], e * (4 / kMine));
           if constexpr (kHeads >= 8) {
@@ -291,12 +293,10 @@ void score_rows_kernel(const SelectArgs a, int chunks, int group, int64_t total)
 #pragma unroll
         for (int e = 0; e < kMine; ++e) {
           if (left[e] <= 0) continue;
+          float* dst = a.scores + to[e] + col * kHeld;  // (the row's stride holds whole chunks)
 #pragma unroll
-          for (int j = 0; j < kHeldTiles<D>; ++j) {
-            if (left[e] <= j * kTileBlocks) break;
-            a.scores[to[e] + j * kTileBlocks] = best[j][e];
-            if (col == 0) a.tile_most[to[e] / kTileBlocks + j] = top[j];
-          }
+          for (int j = 0; j < kHeld; ++j) dst[j] = best[j][e];
+          if (col == 0) a.tile_most[to[e] / kTileBlocks] = top;
         }
       }
     }
@@ -502,8 +502,8 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs a) {
     }
     all[0] = fmaxf(all[0], row_all(norm, Add()));
   }
-  for (int k = t; k < (n + kTileBlocks - 1) / kTileBlocks; k += kThreads)
-    all[2] = fmaxf(all[2], a.tile_most[item * (a.stride / kTileBlocks) + k]);
+  for (int k = t; k * a.most_step * kTileBlocks < n; k += kThreads)
+    all[2] = fmaxf(all[2], a.tile_most[item * (a.stride / kTileBlocks) + k * a.most_step]);
   each([&](int, float x) {
     all[3] = fmaxf(all[3], -x);
     all[4] = fmaxf(all[4], x);
@@ -656,10 +656,13 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs a) {
 
 }  // namespace
 
+// A row's scores in the workspace: whole chunks of both head dims' score_rows_kernel.
+static int64_t select_stride(int64_t n) { return (n + 191) / 192 * 192; }
+
 size_t select_workspace_bytes(int64_t items, int32_t max_len, int32_t blocks) {
   const int64_t n = ((int64_t)max_len + kBlockSize - 1) / kBlockSize;
   if (n <= blocks) return 0;  // every block is chosen
-  const int64_t stride = (n + kTileBlocks - 1) / kTileBlocks * kTileBlocks;
+  const int64_t stride = select_stride(n);
   return (size_t)(items * (2 * stride + stride / kTileBlocks)) * sizeof(float);
 }
 
@@ -727,7 +730,8 @@ hipError_t launch_select_blocks(SelectArgs a, int head_dim, void* workspace, hip
   const int64_t items = a.rows * a.hkv;
   const int64_t most = ((int64_t)a.max_len + kBlockSize - 1) / kBlockSize;
   const int64_t n = std::min<int64_t>(most, a.max_blocks);
-  a.stride = (most + kTileBlocks - 1) / kTileBlocks * kTileBlocks;
+  a.stride = select_stride(most);
+  a.most_step = a.row_seq == nullptr ? 1 : head_dim == 128 ? kHeldTiles<128> : kHeldTiles<64>;
   a.scores = static_cast<float*>(workspace);
   a.low = a.scores + items * a.stride;
   a.tile_most = a.low + items * a.stride;
