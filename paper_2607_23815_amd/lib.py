@@ -479,7 +479,7 @@ def _launch_on(stream):
     stream's, or that of an explicit one, which must be of this device)."""
     if _torch is None:
         _get_torch()
-    dev = _get_device() if _torch.cuda.is_initialized() else _torch.cuda.current_device()
+    dev = _get_device()
     if stream is None:
         return dev, _raw_stream(dev) if _raw_stream is not None else _stream(None)
     if stream.device_index != dev:
@@ -497,16 +497,17 @@ def _ptr(t, name, dtype, dev):
     raise ValueError(f"{name} is on device {t.get_device()}, the current device is {dev}")
 
 
-def _paged_kv_on(k_cache, v_cache, dev) -> PagedKV:
-    """paged_kv of a pool on the current device."""
+def _paged_kv_on(k_cache, v_cache, dev):
+    """paged_kv of a pool on the current device, its blocks, kv heads and head dim."""
     k_shape = k_cache.shape
     if len(k_shape) != 5:
         raise ValueError("k_cache must be [nb][Hkv][D/8][bs][8] and v_cache [nb][Hkv][D][bs]")
     nb, hkv, nch, bs, e = k_shape
-    if e != 8 or v_cache.shape != (nb, hkv, nch * 8, bs):
+    d = nch * 8
+    if e != 8 or v_cache.shape != (nb, hkv, d, bs):
         raise ValueError("k_cache / v_cache shapes disagree")
     return PagedKV(_ptr(k_cache, "k_cache", _bf16, dev), _ptr(v_cache, "v_cache", _bf16, dev), nb,
-                   bs, hkv, nch * 8)
+                   bs, hkv, d), nb, hkv, d
 
 
 def paged_kv(k_cache, v_cache) -> PagedKV:
@@ -663,9 +664,10 @@ def pkv_extend_tables(block_tables, cached_lens, new_lens, free_blocks, free_use
     slot_map int64). status [1] holds PKV_EXTEND_* bits when the step was refused. seq_lens may
     be cached_lens, and free_used_out free_used."""
     dev, hip_stream = _launch_on(stream)
-    if block_tables.dim() != 2:
+    tables = block_tables.shape
+    if len(tables) != 2:
         raise ValueError("block_tables must be [num_seqs][max_blocks]")
-    b, max_blocks = block_tables.shape
+    b, max_blocks = tables
     if not (cached_lens.numel() == new_lens.numel() == seq_lens.numel() == b
             and cu_new_lens.numel() == b + 1):
         raise ValueError("cached_lens, new_lens and seq_lens must have an entry per sequence, "
@@ -706,21 +708,16 @@ def rope_spec(inv_freq, axis_of=None, interleaved=False, scale=1.0, num_axes=Non
     return r
 
 
-def _rows_ptr(t, name, heads, dim, dev):
+def _rows_ptr(t, name, rows, heads, dim, dev):
     """bf16 [rows][heads][dim] whose rows may lie apart: address and row stride."""
-    if not isinstance(t, _Tensor) or t.get_device() < 0:
-        raise TypeError(f"{name} must be a GPU tensor (the library has no CPU path)")
-    if t.dtype is not _bf16:
-        raise TypeError(f"{name} must be {_bf16}, got {t.dtype}")
-    if t.get_device() != dev:
-        raise ValueError(f"{name} is on device {t.get_device()}, the current device is {dev}")
-    shape = t.shape
-    if len(shape) != 3 or shape[1] != heads or shape[2] != dim:
-        raise ValueError(f"{name} must be [rows][{heads}][{dim}]")
+    if not (isinstance(t, _Tensor) and t.dtype is _bf16 and t.get_device() == dev):
+        _ptr(t, name, _bf16, dev)  # (raises)
+    if t.shape != (rows, heads, dim):
+        raise ValueError(f"{name} must be [{rows}][{heads}][{dim}], a row per entry of slot_map")
     s0, s1, s2 = t.stride()
     if s2 != 1 or (s1 != dim and heads > 1):
         raise ValueError(f"{name} must have contiguous heads")
-    return t.data_ptr(), s0 if shape[0] > 1 else heads * dim
+    return t.data_ptr(), s0 if rows > 1 else heads * dim
 
 
 def pkv_rope_append(k_cache, v_cache, q, k_new, v_new, slot_map, positions, rope: Rope, q_out,
@@ -729,17 +726,18 @@ def pkv_rope_append(k_cache, v_cache, q, k_new, v_new, slot_map, positions, rope
     and appended at slot_map (int64 [rows]); their rows may lie apart (views of one fused
     projection). positions: int32 [rows], or [axes][rows] where rope has several axes."""
     dev, hip_stream = _launch_on(stream)
-    kv = _paged_kv_on(k_cache, v_cache, dev)
-    hkv, d = kv.num_kv_heads, kv.head_dim
-    n, hq = q.shape[0], q.shape[1]
-    if not (k_new.shape[0] == v_new.shape[0] == q_out.shape[0] == slot_map.numel() == n):
-        raise ValueError("q, k_new, v_new, q_out and slot_map must have the same number of rows")
-    if positions.numel() != rope.num_axes * n or positions.shape[-1] != n:
+    kv, _, hkv, d = _paged_kv_on(k_cache, v_cache, dev)
+    n = slot_map.numel()
+    if q.dim() != 3:
+        raise ValueError("q must be [rows][Hq][D]")
+    hq = q.shape[1]
+    if positions.shape != (n,) and positions.shape != (rope.num_axes, n) or \
+            positions.dim() == 1 and rope.num_axes != 1:
         raise ValueError(f"positions must be [{rope.num_axes}][rows]")
-    qp, qs = _rows_ptr(q, "q", hq, d, dev)
-    kp, ks = _rows_ptr(k_new, "k_new", hkv, d, dev)
-    vp, vs = _rows_ptr(v_new, "v_new", hkv, d, dev)
-    op, os_ = _rows_ptr(q_out, "q_out", hq, d, dev)
+    qp, qs = _rows_ptr(q, "q", n, hq, d, dev)
+    kp, ks = _rows_ptr(k_new, "k_new", n, hkv, d, dev)
+    vp, vs = _rows_ptr(v_new, "v_new", n, hkv, d, dev)
+    op, os_ = _rows_ptr(q_out, "q_out", n, hq, d, dev)
     _check(_lib.pkv_rope_append(
         ctypes.byref(kv), ctypes.byref(rope), qp, qs, hq, kp, ks, vp, vs,
         _ptr(slot_map, "slot_map", _i64, dev),
@@ -751,16 +749,17 @@ def pkv_block_bounds(k_cache, v_cache, bounds, block_tables, cached_lens, cu_new
     """The key bounds (bf16 [num_blocks][Hkv][2][D], largest then smallest) of the blocks that
     hold new tokens."""
     dev, hip_stream = _launch_on(stream)
-    kv = _paged_kv_on(k_cache, v_cache, dev)
-    if bounds.shape != (kv.num_blocks, kv.num_kv_heads, 2, kv.head_dim):
+    kv, nb, hkv, d = _paged_kv_on(k_cache, v_cache, dev)
+    if bounds.shape != (nb, hkv, 2, d):
         raise ValueError("bounds must be [num_blocks][Hkv][2][D]")
-    b = cached_lens.shape[0]
-    if block_tables.dim() != 2 or block_tables.shape[0] != b or cu_new_lens.numel() != b + 1:
+    b = cached_lens.numel()
+    tables = block_tables.shape
+    if len(tables) != 2 or tables[0] != b or cu_new_lens.numel() != b + 1:
         raise ValueError("block_tables, cached_lens and cu_new_lens must have a row, an entry and "
                          "a step per sequence")
     _check(_lib.pkv_block_bounds(
         ctypes.byref(kv), _ptr(bounds, "bounds", _bf16, dev),
-        _ptr(block_tables, "block_tables", _i32, dev), block_tables.shape[1],
+        _ptr(block_tables, "block_tables", _i32, dev), tables[1],
         _ptr(cached_lens, "cached_lens", _i32, dev), _ptr(cu_new_lens, "cu_new_lens", _i32, dev), b,
         int(max_new_len), hip_stream))
 
@@ -778,14 +777,18 @@ def pkv_select_workspace_bytes(rows, num_q_heads, num_kv_heads, head_dim, max_le
                                                blocks))
 
 
-def _check_rows(q, block_tables, row_lens, row_seq):
+def _row_sizes(q, block_tables, row_lens, row_seq, sel, hkv, d):
+    """Rows, query heads, sequences, table width and blocks of a sparse read's arrays."""
     n = row_lens.numel()
-    if q.dim() != 3 or q.shape[0] != n or block_tables.dim() != 2:
-        raise ValueError("q must be [rows][Hq][D] with an entry of row_lens per row, block_tables "
-                         "[num_seqs][max_blocks]")
-    if n != (block_tables.shape[0] if row_seq is None else row_seq.numel()):
+    q_shape, tables, chosen = q.shape, block_tables.shape, sel.shape
+    if len(q_shape) != 3 or q_shape[0] != n or q_shape[2] != d or len(tables) != 2:
+        raise ValueError("q must be [rows][Hq][D] of the pool's head dim with an entry of row_lens "
+                         "per row, block_tables [num_seqs][max_blocks]")
+    if n != (tables[0] if row_seq is None else row_seq.numel()):
         raise ValueError("row_seq must have an entry per row; without it row i is sequence i")
-    return n
+    if len(chosen) != 3 or chosen[0] != n or chosen[1] != hkv:
+        raise ValueError("sel must be [rows][Hkv][blocks]")
+    return n, q_shape[1], tables[0], tables[1], chosen[2]
 
 
 def pkv_select_blocks(bounds, q, block_tables, row_lens, max_len: int, sink_blocks: int,
@@ -793,14 +796,11 @@ def pkv_select_blocks(bounds, q, block_tables, row_lens, max_len: int, sink_bloc
     """sel [rows][Hkv][blocks] receives, for each row of q [rows][Hq][D] and kv head, the logical
     blocks chosen by their key bounds [num_blocks][Hkv][2][D], ascending, then -1."""
     dev, hip_stream = _launch_on(stream)
-    if bounds.dim() != 4 or bounds.shape[2] != 2:
+    box = bounds.shape
+    if len(box) != 4 or box[2] != 2:
         raise ValueError("bounds must be [num_blocks][Hkv][2][D]")
-    nb, hkv, _, d = bounds.shape
-    n = _check_rows(q, block_tables, row_lens, row_seq)
-    if sel.dim() != 3 or sel.shape[:2] != (n, hkv) or q.shape[2] != d:
-        raise ValueError("sel must be [rows][Hkv][blocks], and q's head dim the bounds'")
-    b, max_blocks = block_tables.shape
-    hq, blocks = q.shape[1], sel.shape[2]
+    nb, hkv, _, d = box
+    n, hq, b, max_blocks, blocks = _row_sizes(q, block_tables, row_lens, row_seq, sel, hkv, d)
     if workspace is None:  # convenience for one-off calls; timed callers pass their own
         workspace = alloc_workspace(pkv_select_workspace_bytes(n, hq, hkv, d, int(max_len),
                                                                blocks))
@@ -822,16 +822,12 @@ def pkv_sparse_attention(k_cache, v_cache, q, block_tables, row_lens, sel, scale
     """Rows q [rows][Hq][D] attend over the first row_lens keys of their sequences, as far as these
     lie in the logical blocks that sel [rows][Hkv][blocks] names."""
     dev, hip_stream = _launch_on(stream)
-    kv = _paged_kv_on(k_cache, v_cache, dev)
-    n = _check_rows(q, block_tables, row_lens, row_seq)
-    hkv, d, hq = kv.num_kv_heads, kv.head_dim, q.shape[1]
-    if sel.dim() != 3 or sel.shape[:2] != (n, hkv) or q.shape[2] != d or out.shape != q.shape:
-        raise ValueError("sel must be [rows][Hkv][blocks], q and out [rows][Hq][D] of the pool's "
-                         "head dim")
+    kv, _, hkv, d = _paged_kv_on(k_cache, v_cache, dev)
+    n, hq, b, max_blocks, blocks = _row_sizes(q, block_tables, row_lens, row_seq, sel, hkv, d)
+    if out.shape != (n, hq, d):
+        raise ValueError("out must be [rows][Hq][D]")
     if lse is not None and lse.shape != (n, hq):
         raise ValueError("lse must be [rows][Hq]")
-    b, max_blocks = block_tables.shape
-    blocks = sel.shape[2]
     if workspace is None:  # convenience for one-off calls; timed callers pass their own
         workspace = alloc_workspace(pkv_sparse_workspace_bytes(n, hq, hkv, d, blocks))
     ws, ws_bytes = _workspace(workspace, dev)

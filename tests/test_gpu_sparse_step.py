@@ -194,3 +194,40 @@ def test_sparse_rows_of_a_decode_step_without_row_seq(gpu_lib):
     torch.cuda.synchronize()
     assert torch.equal(sel, loop.sel) and torch.equal(out.view(torch.int16),
                                                       loop.out.view(torch.int16))
+
+
+def test_the_binding_refuses_wrong_tensors(gpu_lib):
+    """Shapes, types, strides and devices that do not fit are refused before any launch."""
+    import torch
+    lib = gpu_lib
+    loop = Loop(lib, (8, 2, 64), seqs=4, rows=4, num_blocks=8, width=4, sizes=(1, 2, 3), max_len=64,
+                seed=1)
+    q, k, v = loop.qkv.split([8, 2, 2], dim=1)
+    rope = (loop.k_cache, loop.v_cache, q, k, v, loop.slots, loop.positions, loop.rope, loop.q)
+    attend = (loop.k_cache, loop.v_cache, loop.q, loop.tables, loop.row_lens, loop.sel, 0.1, loop.out)
+    select = (loop.bounds, loop.q, loop.tables, loop.row_lens, 64, 1, 2, loop.sel)
+    bounds = (loop.k_cache, loop.v_cache, loop.bounds, loop.tables, loop.cached, loop.cu, 1)
+    tables = (loop.tables, loop.cached, loop.new, loop.free, loop.used, loop.used, loop.cu, loop.lens,
+              loop.status, 4)
+    for call, args, which in (
+            (lib.pkv_rope_append, rope, (0, 1, 2, 3, 4, 5, 6, 8)),
+            (lib.pkv_sparse_attention, attend, (0, 1, 2, 3, 4, 5, 7)),
+            (lib.pkv_select_blocks, select, (0, 1, 2, 3, 7)),
+            (lib.pkv_block_bounds, bounds, (0, 1, 2, 3, 4, 5)),
+            (lib.pkv_extend_tables, tables, (0, 1, 2, 3, 4, 5, 6, 7, 8))):
+        for i in which:
+            t = args[i]
+            wide = torch.zeros(tuple(t.shape) + (2,), dtype=t.dtype, device="cuda")[..., 0]
+            bads = [t.cpu(), t.float()]
+            if t.numel() > 1:
+                bads.append(wide)
+            if t.dim() > 1:
+                bads.append(t[None])
+            if t.dtype == torch.bfloat16:
+                bads.append(t[..., :-1].contiguous())
+            for bad in bads:
+                with pytest.raises((TypeError, ValueError)):
+                    call(*args[:i], bad, *args[i + 1:])
+                    say(f"  taken: {call.__name__} argument {i} as {bad.dtype} {tuple(bad.shape)}")
+    with pytest.raises(ValueError):
+        lib.pkv_rope_append(*rope[:6], loop.positions[0], *rope[7:])  # three axes are needed
