@@ -29,7 +29,7 @@ namespace {
 
 constexpr int kScoreWaves = 4;
 constexpr int kTileBlocks = 16;      // blocks of a product
-constexpr int kMaxTiles = 16;        // tiles of one row that a wave takes at most
+constexpr int kMaxTiles = 3;         // tiles of one row that a wave takes at most
 template <int D>
 constexpr int kHeldTiles = D == 128 ? 3 : 4;  // tiles that a wave holds for a group of rows
 
@@ -144,12 +144,9 @@ __global__ __launch_bounds__(64 * kScoreWaves) void score_row_kernel(const Selec
     if (seq < 0 || n <= a.blocks || t0 * kTileBlocks >= n) continue;
     const int t1 = min(t0 + tiles, (n + kTileBlocks - 1) / kTileBlocks);
     const int32_t* table = a.tables + (size_t)seq * a.max_blocks;
-    // the ids of the run's blocks, 64 per register
-    static_assert(kMaxTiles == 16, "four registers of 64 ids");
-    auto ids_of = [&](int k) {
-      return t0 + 4 * k < t1 ? table[min(t0 * kTileBlocks + 64 * k + lane, n - 1)] : 0;
-    };
-    const int ids0 = ids_of(0), ids1 = ids_of(1), ids2 = ids_of(2), ids3 = ids_of(3);
+    // the ids of the run's blocks
+    static_assert(kMaxTiles * kTileBlocks <= 64, "one of each lane");
+    const int ids = table[min(t0 * kTileBlocks + lane, n - 1)];
     const int g = a.hq / a.hkv;
     u32x4 qv[D / 32];
 #pragma unroll
@@ -158,9 +155,7 @@ __global__ __launch_bounds__(64 * kScoreWaves) void score_row_kernel(const Selec
       qv[kk] = ld16(a.q + ((size_t)row * a.hq + kvh * g + min(col, g - 1)) * D + kk * 32 + grp * 8);
     }
     auto id_of = [=](int j) {  // of block col of the run's tile j
-      const int half = j < 4 ? +ids0 : +ids1, rest = j < 12 ? +ids2 : +ids3;
-      const int x = j < 8 ? +half : +rest;
-      return __builtin_amdgcn_ds_bpermute((j % 4 * 16 + col) * 4, x);
+      return __builtin_amdgcn_ds_bpermute((j * kTileBlocks + col) * 4, ids);
     };
     Sides<D> q;
     Box<D> box[2];
@@ -673,11 +668,11 @@ hipError_t launch_scores(const SelectArgs& a, int64_t items, int64_t n, hipStrea
   constexpr int64_t kMostWorkgroups = 1 << 20;  // (a launch's loop takes the others)
   const int64_t tiles = (n + kTileBlocks - 1) / kTileBlocks;
   if (a.row_seq == nullptr) {
-    // Waves enough to fill the chip several times over, then longer runs of tiles for each: 64
-    // sequences of 8-32k keys, 8 heads, 84.8 us with both launches (at half as many waves 94.4, at
-    // twice as many 81.6); 256 with one head 48.6 (49.6, 57.9).
-    int64_t run = items * tiles / 16384;
-    run = std::min<int64_t>(std::max<int64_t>(run, 1), kMaxTiles);
+    // Short runs of tiles: waves of a few microseconds keep a row's heads, whose bounds lie together in
+    // memory, side by side in time. 256 sequences of 8-32k keys, 8 heads (us, both launches, at 1, 2, 3, 4,
+    // 6, 8, 16 tiles): 336, 271, 261, 281, 264, 346, 350; with one head 66, 54, 49, 55, 51, 56, 56; 64 with
+    // 8 heads 94, 79, 79, 85, 81, 94, 97; but 16 33.9, 31.1, 31.7, one of 120k 20.7, 20.2, 22.2.
+    const int64_t run = items * tiles >= 32768 ? kMaxTiles : 2;
     const int64_t runs = (tiles + run - 1) / run, total = items * runs;
     const int64_t wgs = std::min((total + kScoreWaves - 1) / kScoreWaves, kMostWorkgroups);
     hipLaunchKernelGGL(score_row_kernel<D>, dim3((unsigned)wgs), dim3(64 * kScoreWaves), 0, stream,
