@@ -6,6 +6,9 @@
  *   - a downstream operator's prefill, which reuses the KV cache a tuple's cached prompt
  *     prefix already holds and computes only the new suffix tokens, and
  *   - decode, one new token per sequence attending over the whole cached context.
+ * Beside the two stand the calls of a step that reads a long cache sparsely, without the host in
+ * between: tables grown on the GPU, rotary positions with the append, key bounds per block, the
+ * choice of blocks by these bounds, and attention over the chosen ones.
  * This is the KV-cache reuse that pipelining semantic operators relies on: the filter -> map
  * example of Section 2.1 ("Prefix sharing in semantic operators") has prompts
  * [S | C(t) | I_filter] and [S | C(t) | I_map] whose shared prefix [S | C(t)] is cached once
@@ -385,7 +388,8 @@ pkv_status pkv_mixed_attention(const pkv_paged_kv* kv, int32_t num_q_heads, floa
  * seq_lens may be cached_lens and free_used_out may be free_used (a loop's step then leaves
  * the next one's input; pkv_block_bounds still needs the old lengths); no other arrays may
  * overlap. max_rows <= 2^30. Zero sequences write an
- * empty step. All arrays are device memory. */
+ * empty step. All arrays are device memory. (PKV_DEBUG_VALIDATE adds nothing here: *status says
+ * what a step was refused for.) */
 enum {
   PKV_EXTEND_OUT_OF_BLOCKS = 1,  /* *free_used is negative, or too few blocks are behind it */
   PKV_EXTEND_TABLE_FULL = 2,     /* a sequence needs more than max_blocks blocks */
@@ -453,7 +457,7 @@ pkv_status pkv_block_bounds(const pkv_paged_kv* kv, void* bounds, const int32_t*
  * [rows]; NULL: row t is sequence t, rows == num_seqs, a decode step) and sees that sequence's
  * first row_lens[t] keys (int32 [rows]). A decode step passes seq_lens; rows of longer suffixes
  * take both arrays from pkv_extend_tables. A row whose row_seq is -1 is padding: nothing of it is
- * written. num_q_heads / num_kv_heads <= 16; rows * num_kv_heads <= 2^23.
+ * written. num_q_heads / num_kv_heads <= 16; rows * num_kv_heads < 2^22.
  *
  * Choice of blocks: for each row and kv head, the `blocks` of the row's
  * ceil(row_lens[t] / block_size) blocks that matter most, by the most that any key within a

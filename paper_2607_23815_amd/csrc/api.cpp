@@ -206,7 +206,7 @@ pkv_status check_decode(const KvView& view, const char* fn, const void* q, int32
   return ok();
 }
 
-constexpr int64_t kMaxRowItems = int64_t(1) << 23;  // (row, kv head) pairs of a sparse read
+constexpr int64_t kMaxRowItems = (int64_t(1) << 22) - 1;  // (row, kv head) pairs of a sparse read
 
 // Argument checks that both sparse calls make of their rows.
 pkv_status check_rows(const std::string& f, int32_t num_q_heads, int32_t hkv, const void* q,
@@ -232,7 +232,7 @@ pkv_status check_rows(const std::string& f, int32_t num_q_heads, int32_t hkv, co
     return fail(PKV_ERR_INVALID_ARG, f + ": NULL pointer");
   if (!aligned16(q)) return fail(PKV_ERR_INVALID_ARG, f + ": q must be 16-byte aligned");
   if ((int64_t)rows * hkv > kMaxRowItems)
-    return fail(PKV_ERR_INVALID_ARG, f + ": more than 2^23 rows x kv heads");
+    return fail(PKV_ERR_INVALID_ARG, f + ": 2^22 rows x kv heads or more");
   return PKV_OK;
 }
 
@@ -612,6 +612,8 @@ pkv_status pkv_block_bounds(const pkv_paged_kv* kv, void* bounds, const int32_t*
     return fail(PKV_ERR_INVALID_ARG, "pkv_block_bounds: bounds must be 16-byte aligned");
   if (num_seqs > kMaxGridZ)
     return fail(PKV_ERR_INVALID_ARG, "pkv_block_bounds: more than 65535 sequences per call");
+  if (max_blocks >= (1 << 24))  // (workgroups of a launch)
+    return fail(PKV_ERR_INVALID_ARG, "pkv_block_bounds: 2^24 blocks of a sequence or more");
   {
     const MetaCheck c = meta(kMetaAppend, view, block_tables, max_blocks, cached_lens,
                              cu_new_lens, num_seqs, -1, max_new_len,

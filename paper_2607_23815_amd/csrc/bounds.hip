@@ -157,8 +157,9 @@ hipError_t launch_block_bounds(const KvView& kv, uint16_t* bounds, const int32_t
                                int32_t max_blocks, const int32_t* cached_lens,
                                const int32_t* cu_new_lens, int32_t num_seqs, int32_t max_new_len,
                                hipStream_t stream) {
-  // blocks that max_new_len tokens can touch, wherever the first one falls
-  const int64_t blocks = ((int64_t)max_new_len + kBlockSize - 2) / kBlockSize + 1;
+  // blocks that max_new_len tokens can touch, wherever the first one falls in the table
+  const int64_t blocks = std::min<int64_t>(((int64_t)max_new_len + kBlockSize - 2) / kBlockSize + 1,
+                                           max_blocks);
   const int run = (kWaves + kv.hkv - 1) / kv.hkv;  // (at least a slab for every wave)
   const dim3 grid((unsigned)((blocks + run - 1) / run), (unsigned)num_seqs);
   // Keys beyond what the last-level cache (256 MB) can still hold of their append are read past the

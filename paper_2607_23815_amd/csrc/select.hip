@@ -513,7 +513,9 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs a) {
   // chosen one (places past the last count into bin 0, which nothing looks past)
   bool slow = odd;
   const float per = range > 0.f ? (kBins - 1) / range : 0.f;
-  auto bin_of = [&](float x) { return min(max((int)((x - mn) * per), 0), kBins - 1); };
+  auto bin_of = [&](float x) {  // (a NaN's is 0)
+    return (int)fminf(fmaxf((x - mn) * per, 0.f), kBins - 1.f);
+  };
   float lo = 0.f, hi = 0.f;
   __syncthreads();
   if (!slow) {

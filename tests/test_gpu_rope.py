@@ -138,6 +138,9 @@ CASES = [
     dict(heads=(32, 8, 128), seqs=RAGGED, order="reversed"),
     dict(heads=(4, 2, 64), seqs=RAGGED, order="padded", axes=3),
     dict(heads=(40, 20, 128), seqs=RAGGED, order="padded"),
+    dict(heads=(32, 8, 128), seqs=[(5, 500), (0, 333), (11, 64)]),  # (windows of 16 rows)
+    dict(heads=(8, 8, 64), seqs=[(5, 500), (0, 333), (11, 64)], order="padded", interleaved=True),
+    dict(heads=(17, 17, 64), seqs=[(5, 300), (0, 133)], order="reversed", rot=32),
     dict(heads=(4, 2, 64), seqs=[(0, 40)], far=True),
     dict(heads=(4, 2, 128), seqs=[(0, 40)], far=True, axes=3, interleaved=True),
 ]

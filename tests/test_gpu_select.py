@@ -270,3 +270,45 @@ def test_validation_names_a_bad_row(gpu_lib):
                     max_len=80)
     finally:
         lib.pkv_set_debug_validate(False)
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(32, 8, 128), (16, 4, 64), (16, 1, 128), (4, 4, 64)])
+def test_many_rows_of_few_sequences(gpu_lib, hq, hkv, d):
+    """Rows enough for whole groups, which end inside sequences: 60 rows of them checked."""
+    rng = np.random.default_rng(d)
+    lens = [2500, 1700, 900, 2100]
+    tables, bounds = pool(rng, lens, hkv, d)
+    seq = np.repeat(np.arange(4), [1500, 701, 400, 1100])
+    seen = np.concatenate([np.arange(n - m + 1, n + 1) for n, m in
+                           zip(lens, (1500, 701, 400, 1100))])
+    seq[rng.integers(0, len(seq), 40)] = -1
+    q = rand_bf16(rng, (len(seq), hq, d))
+    got = run(gpu_lib, tables, bounds, q, seen, 1, 2, 9, row_seq=seq)
+    rows = np.sort(rng.permutation(len(seq))[:60])
+    check(got[rows], tables, bounds, q[rows], seen[rows], 1, 2, 9, seq[rows])
+    assert (got[seq < 0] == -7).all() and (got[seq >= 0][:, :, 0] == 0).all()
+
+
+def test_two_calls_at_once(gpu_lib):
+    """Two streams, each with its own workspace."""
+    import torch
+    lib = gpu_lib
+    rng = np.random.default_rng(14)
+    sides = []
+    for k in range(2):
+        lens = np.array([9000, 4000, 20000 + k])
+        tables, bounds = pool(rng, list(lens), 8, 128)
+        q = rand_bf16(rng, (3, 32, 128))
+        sides.append(dict(host=(tables, bounds, q, lens, 1, 2, 40), stream=torch.cuda.Stream(),
+                          dev=(to_dev_bits(bounds), to_dev_bits(q), i32(tables), i32(lens)),
+                          sel=torch.zeros((3, 8, 40), dtype=torch.int32, device="cuda"),
+                          ws=lib.alloc_workspace(lib.pkv_select_workspace_bytes(3, 32, 8, 128, 20001,
+                                                                                40))))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for s in sides:
+            lib.pkv_select_blocks(*s["dev"], 20001, 1, 2, s["sel"], workspace=s["ws"],
+                                  stream=s["stream"])
+    torch.cuda.synchronize()
+    for s in sides:
+        check(s["sel"].cpu().numpy(), *s["host"])

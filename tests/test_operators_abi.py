@@ -91,7 +91,7 @@ def _bounds(lib, kv=None, **kw):
 def test_block_bounds_refuses(lib):
     for bad in (dict(bounds=None), dict(tables=None), dict(cached=None), dict(cu=None),
                 dict(bounds=ctypes.c_void_p(0x3008)), dict(max_blocks=-1), dict(num_seqs=-1),
-                dict(max_new=-1), dict(num_seqs=65536)):
+                dict(max_new=-1), dict(num_seqs=65536), dict(max_blocks=2**24)):
         refused(lib, lib.PKV_ERR_INVALID_ARG, _bounds(lib, **bad), "pkv_block_bounds")
     refused(lib, lib.PKV_ERR_UNSUPPORTED_SHAPE, _bounds(lib, kv=_kv(lib, 96)), "head_dim")
     for empty in (dict(num_seqs=0), dict(max_new=0), dict(max_blocks=0)):
