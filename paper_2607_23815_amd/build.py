@@ -1,4 +1,5 @@
-"""Build libpkv.so (the HIP kernels for gfx950 plus the C ABI) in-tree with hipcc.
+"""Build libpkv.so (the HIP kernels for gfx950 plus the C ABI) in-tree with hipcc, and
+_tensor_address.so (the binding's look at its tensors, host code against torch's headers).
 
     python -m paper_2607_23815_amd.build
     python -m paper_2607_23815_amd.build --sanitize   # libpkv_asan.so, see below
@@ -28,6 +29,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libpkv.so")
+BINDING = os.path.join(PKG, "_tensor_address.so")
 ASAN_LIB = os.path.join(PKG, "libpkv_asan.so")
 SANITIZE_FLAGS = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
                   "-Xarch_host", "-fno-sanitize-recover=undefined",
@@ -83,8 +85,33 @@ def build(verbose: bool = False, sanitize: bool = False) -> str:
     return out
 
 
+def build_binding(verbose: bool = False) -> str:
+    import sysconfig
+
+    from torch.utils.cpp_extension import include_paths, library_paths
+    tmp = BINDING + ".tmp"
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-o", tmp,
+           os.path.join(CSRC, "tensor_address.cpp"), "-isystem",
+           sysconfig.get_paths()["include"]]
+    for d in include_paths():
+        cmd += ["-isystem", d]
+    for d in library_paths():
+        cmd += ["-L", d]
+    cmd += ["-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10"]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        sys.stderr.write(res.stdout + res.stderr)
+        raise RuntimeError("g++ failed building _tensor_address.so")
+    os.replace(tmp, BINDING)
+    return BINDING
+
+
 if __name__ == "__main__":
     if "--asan-runtime" in sys.argv:
         print(asan_runtime())
     else:
+        if "--sanitize" not in sys.argv:
+            print(build_binding(verbose=True))
         print(build(verbose=True, sanitize="--sanitize" in sys.argv))

@@ -436,6 +436,7 @@ _torch = None
 _Tensor = None
 _raw_stream = None
 _get_device = None
+_address = _rows_address = None
 _bf16 = _i32 = _i64 = _f32 = None
 
 
@@ -477,8 +478,15 @@ def _stream(stream):
 def _launch_on(stream):
     """The current device's index, which a call launches on, and the hipStream_t (the current
     stream's, or that of an explicit one, which must be of this device)."""
-    if _torch is None:
+    global _address, _rows_address
+    if _address is None:
         _get_torch()
+        try:
+            from . import _tensor_address
+        except ImportError as e:
+            raise ImportError("_tensor_address.so is missing or does not fit this torch: build it "
+                              "with `python -m paper_2607_23815_amd.build`") from e
+        _address, _rows_address = _tensor_address.address, _tensor_address.rows_address
     dev = _get_device()
     if stream is None:
         return dev, _raw_stream(dev) if _raw_stream is not None else _stream(None)
@@ -489,8 +497,9 @@ def _launch_on(stream):
 
 def _ptr(t, name, dtype, dev):
     """A contiguous tensor of this type on the current device `dev`: its address."""
-    if isinstance(t, _Tensor) and t.dtype is dtype and t.get_device() == dev and t.is_contiguous():
-        return t.data_ptr()
+    p = _address(t, dtype, dev)
+    if p is not None:
+        return p
     _dev_ptr(t, name, dtype)
     if t is None:
         raise TypeError(f"{name} must be a GPU tensor (the library has no CPU path)")
@@ -710,14 +719,14 @@ def rope_spec(inv_freq, axis_of=None, interleaved=False, scale=1.0, num_axes=Non
 
 def _rows_ptr(t, name, rows, heads, dim, dev):
     """bf16 [rows][heads][dim] whose rows may lie apart: address and row stride."""
+    p = _rows_address(t, _bf16, dev, rows, heads, dim)
+    if p is not None:
+        return p
     if not (isinstance(t, _Tensor) and t.dtype is _bf16 and t.get_device() == dev):
         _ptr(t, name, _bf16, dev)  # (raises)
     if t.shape != (rows, heads, dim):
         raise ValueError(f"{name} must be [{rows}][{heads}][{dim}], a row per entry of slot_map")
-    s0, s1, s2 = t.stride()
-    if s2 != 1 or (s1 != dim and heads > 1):
-        raise ValueError(f"{name} must have contiguous heads")
-    return t.data_ptr(), s0 if rows > 1 else heads * dim
+    raise ValueError(f"{name} must have contiguous heads")
 
 
 def pkv_rope_append(k_cache, v_cache, q, k_new, v_new, slot_map, positions, rope: Rope, q_out,

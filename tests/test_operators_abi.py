@@ -159,3 +159,20 @@ def test_binding_refuses_host_tensors(lib):
         z = torch.zeros(1, dtype=torch.int32)
         lib.pkv_extend_tables(z.view(1, 1), z, z, z, z, z, torch.zeros(2, dtype=torch.int32), z, z,
                               0)
+
+
+def test_tensor_address_takes_gpu_tensors_only():
+    """The binding's look at a tensor (CPU side): anything but a tensor on the GPU asked for is None,
+    wrong calls are TypeErrors."""
+    import torch
+    from paper_2607_23815_amd import _tensor_address as m
+    t = torch.zeros((2, 3, 4), dtype=torch.bfloat16)
+    for x in (t, t.transpose(0, 1), torch.zeros(0), t.to_sparse(), None, 3, "t",
+              torch.empty((2, 3, 4), dtype=torch.bfloat16, device="meta")):
+        assert m.address(x, torch.bfloat16, 0) is None
+        assert m.rows_address(x, torch.bfloat16, 0, 2, 3, 4) is None
+    assert m.address(t, "dtype", 0) is None
+    for call, args in ((m.address, (t,)), (m.address, (t, t.dtype, None)),
+                       (m.rows_address, (t, t.dtype, 0)), (m.rows_address, (t, t.dtype, 0, 2, "3", 4))):
+        with pytest.raises(TypeError):
+            call(*args)
