@@ -128,6 +128,24 @@ __device__ __forceinline__ f32x4 score(const Sides<D>& q, const Box<D>& b) {
   return s;
 }
 
+// The group's heads as a product's lines (those past the group's hold its last one again: no new
+// maximum).
+template <int D>
+__device__ __forceinline__ void load_heads(const uint16_t* q, int g, u32x4 (&qv)[D / 32]) {
+  const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
+#pragma unroll
+  for (int kk = 0; kk < D / 32; ++kk) qv[kk] = ld16(q + min(col, g - 1) * D + kk * 32 + grp * 8);
+}
+// The scores of a tile's blocks, block col's in lane (col, any grp).
+template <int D>
+__device__ __forceinline__ float tile_scores(const Sides<D>& q, const Box<D>& b) {
+  float best = best_of<4>(score<D>(q, b), 0);
+  u32x2 x = with_row(__float_as_uint(best));
+  best = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+  x = with_half(__float_as_uint(best));
+  return fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+}
+
 // A wave per (row, run of tiles, kv head); a block's bounds of all heads lie together.
 template <int D>
 __global__ __launch_bounds__(64 * kScoreWaves) void score_row_kernel(const SelectArgs a, int runs,
@@ -149,11 +167,7 @@ __global__ __launch_bounds__(64 * kScoreWaves) void score_row_kernel(const Selec
     const int ids = table[min(t0 * kTileBlocks + lane, n - 1)];
     const int g = a.hq / a.hkv;
     u32x4 qv[D / 32];
-#pragma unroll
-    for (int kk = 0; kk < D / 32; ++kk) {
-      // (lines past the group's heads hold its last one again: no new maximum)
-      qv[kk] = ld16(a.q + ((size_t)row * a.hq + kvh * g + min(col, g - 1)) * D + kk * 32 + grp * 8);
-    }
+    load_heads<D>(a.q + ((size_t)row * a.hq + kvh * g) * D, g, qv);
     auto id_of = [=](int j) {  // of block col of the run's tile j
       return __builtin_amdgcn_ds_bpermute((j * kTileBlocks + col) * 4, ids);
     };
@@ -164,12 +178,7 @@ __global__ __launch_bounds__(64 * kScoreWaves) void score_row_kernel(const Selec
     float* out = a.scores + item * a.stride;
     float* most = a.tile_most + item * (a.stride / kTileBlocks);
     auto finish = [&](const Box<D>& b, int t) {
-      const f32x4 s = score<D>(q, b);
-      float best = best_of<4>(s, 0);
-      u32x2 x = with_row(__float_as_uint(best));
-      best = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
-      x = with_half(__float_as_uint(best));
-      best = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+      const float best = tile_scores<D>(q, b);
       const float top = most_value(box_most<D>(b));
       if (grp == 0 && t * kTileBlocks + col < n) out[t * kTileBlocks + col] = best;
       if (lane == 0) most[t] = top;
@@ -405,8 +414,9 @@ __device__ __forceinline__ int wg_before(int v, int* total, int* sm) {
 }
 
 // One workgroup per (row, kv head). Its scores stay in registers, 64 consecutive blocks per wave and
-// register, at most kThreads * kEach (kEach 0: in memory, any number).
-template <int D, int kThreads, int kEach>
+// register, at most kThreads * kEach (kEach 0: in memory, any number). kOwn: it takes the scores itself,
+// where the other form reads those of a launch before.
+template <int D, int kThreads, int kEach, bool kOwn = false>
 __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs a) {
   constexpr int kWaves = kThreads / 64;
   constexpr int kPer = kThreads == 1024 ? 2 : 8;  // bins of a thread
@@ -421,6 +431,7 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs a) {
   __shared__ float sm5[kWaves][5];
   __shared__ int sm1[kWaves][1], sms[kWaves];
   __shared__ int num_cand, pivot;
+  __shared__ float own[kOwn ? kThreads * kEach : 1];
   const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
   const int64_t item = blockIdx.x;
   const int64_t row = item / a.hkv;
@@ -445,6 +456,31 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs a) {
   const int32_t* table = a.tables + (size_t)seq * a.max_blocks;
   const int g = a.hq / a.hkv;
   const uint16_t* q = a.q + ((size_t)row * a.hq + kvh * g) * D;
+  uint32_t most = 0u;
+  if constexpr (kOwn) {  // tiles of 16 blocks in turn for the waves, two of a wave's in flight
+    const int col = lane & 15, grp = lane >> 4, tiles = (n + kTileBlocks - 1) / kTileBlocks;
+    u32x4 qv[D / 32];
+    load_heads<D>(q, g, qv);
+    Sides<D> sides;
+    for (int t0 = w; t0 < tiles; t0 += 2 * kWaves) {
+      const int t1 = t0 + kWaves;
+      Box<D> box[2];
+      const int id0 = table[min(t0 * kTileBlocks + col, n - 1)];
+      const int id1 = table[min(t1 * kTileBlocks + col, n - 1)];  // (past the last tile its block again)
+      load_box<D>(a, box[0], id0, kvh);
+      load_box<D>(a, box[1], id1, kvh);
+      if (t0 == w) split_q<D>(qv, sides);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int b = (k == 0 ? t0 : t1) * kTileBlocks + col;
+        const float best = tile_scores<D>(sides, box[k]);
+        most = most_of(most, box_most<D>(box[k]));
+        if (grp == 0 && b < n) own[b] = best;
+      }
+    }
+    __syncthreads();
+  }
+  auto score_of = [&](int b) { return kOwn ? own[b] : scores[b]; };
 
   // the wave's blocks: `chunks` times 64 from `base` on; a place past the last holds a NaN, which no
   // comparison, minimum or maximum below takes up
@@ -453,10 +489,13 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs a) {
   float s[kEach > 0 ? kEach : 1];
   auto block_of = [&](int k) { return base + 64 * k + lane; };
   auto value = [&](int b) {
-    const float x = scores[min(b, last - 1)];
+    const float x = score_of(min(b, last - 1));
     return b < last ? x : NAN;
   };
-  if constexpr (kEach > 0) {
+  if constexpr (kOwn) {
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) s[k] = k < chunks ? value(block_of(k)) : NAN;
+  } else if constexpr (kEach > 0) {
     // (every load before the first use, and none in a branch; past the last score they read zeros)
 #pragma unroll
     for (int k = 0; k < kEach; ++k) s[k] = __uint_as_float(buf_ld4(scores, last * 4, block_of(k) * 4));
@@ -497,7 +536,8 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs a) {
     }
     all[0] = fmaxf(all[0], row_all(norm, Add()));
   }
-  for (int k = t; k * a.most_step * kTileBlocks < n; k += kThreads)
+  if constexpr (kOwn) all[2] = most_value(most);
+  else for (int k = t; k * a.most_step * kTileBlocks < n; k += kThreads)
     all[2] = fmaxf(all[2], a.tile_most[item * (a.stride / kTileBlocks) + k * a.most_step]);
   each([&](int, float x) {
     all[3] = fmaxf(all[3], -x);
@@ -585,7 +625,7 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs a) {
     uint32_t* kl = reinterpret_cast<uint32_t*>(low);
     for (int b0 = first + w * 64; b0 < last; b0 += kThreads) {
       const int b = b0 + lane;
-      const float x = b < last ? scores[b] : 0.f;
+      const float x = b < last ? score_of(b) : 0.f;
       uint64_t key = !odd && x > hi ? ~0ull : 0ull;
       const uint64_t todo = __builtin_amdgcn_ballot_w64(b < last && (odd || (x >= lo && x <= hi)));
       for (int k = 0; k < 64; k += 4) {
@@ -665,6 +705,16 @@ size_t select_workspace_bytes(int64_t items, int32_t max_len, int32_t blocks) {
 
 namespace {
 
+// Short rows take their scores in the workgroup that chooses: one launch, and no scores in memory. 8
+// heads of 128 dims (us, so and as two launches): one sequence of up to 62 blocks 6.7 and 10.4, 512 30.2 and
+// 41.5; one of 250 9.9 and 11.5, 64 17.1 and 21.9, 256 45.7 and 57.4; one of 500 12.1 and 11.0, 256 86.6 and
+// 97.5. Rows that share a sequence read its bounds once a group in the other form: 1220 items of 62 blocks
+// 9.4 and 11.8, 6100 20.8 and 20.6, but 1220 of 250 17.6 and 14.1; 120 of 250 8.1 and 11.0.
+bool select_one_launch(const SelectArgs& a, int64_t items, int64_t n) {
+  if (n > 512 || a.blocks == a.sink + a.recent) return false;
+  return a.row_seq == nullptr || items <= 512 || (n <= 64 && items <= 4096);
+}
+
 template <int D>
 hipError_t launch_scores(const SelectArgs& a, int64_t items, int64_t n, hipStream_t stream) {
   constexpr int64_t kMostWorkgroups = 1 << 20;  // (a launch's loop takes the others)
@@ -708,6 +758,11 @@ hipError_t launch_scores(const SelectArgs& a, int64_t items, int64_t n, hipStrea
 
 template <int D>
 hipError_t launch_select(const SelectArgs& a, int64_t items, int64_t n, hipStream_t stream) {
+  if (select_one_launch(a, items, n)) {  // (a wave alone has no barriers: up to 64 blocks, 30 us against 40)
+    auto* kern = n <= 64 ? select_kernel<D, 64, 1, true> : select_kernel<D, 256, 2, true>;
+    hipLaunchKernelGGL(kern, dim3((unsigned)items), dim3(n <= 64 ? 64 : 256), 0, stream, a);
+    return hipGetLastError();
+  }
   // Registers for the longest row the call can have. Short rows take a wave each where there are many:
   // no barriers, and more rows at once (6100 items of up to 1024 blocks 47.8 us with their scores
   // against 60.5 with four waves, 12200 of 128 dims 92.0 and 135.1; but 400 items 18.6 and 16.2).
@@ -733,7 +788,7 @@ hipError_t launch_select_blocks(SelectArgs a, int head_dim, void* workspace, hip
   a.low = a.scores + items * a.stride;
   a.tile_most = a.low + items * a.stride;
   const bool wide = head_dim == 128;
-  if (n > a.blocks && a.blocks > a.sink + a.recent) {
+  if (n > a.blocks && a.blocks > a.sink + a.recent && !select_one_launch(a, items, n)) {
     const hipError_t err = wide ? launch_scores<128>(a, items, n, stream)
                                 : launch_scores<64>(a, items, n, stream);
     if (err != hipSuccess) return err;

@@ -94,6 +94,10 @@ HEADS = [(4, 2, 64), (32, 8, 128), (8, 8, 64), (16, 1, 128), (28, 4, 128), (3, 1
     ([5000, 33, 777], 3, 5, 8),
     ([5000, 33, 777], 0, 1, 200),
     ([16 * 129, 16 * 128, 16 * 127], 2, 2, 128),
+    ([16 * 64, 16 * 63 + 1, 700], 1, 2, 20),     # (up to 64 blocks: a wave each)
+    ([16 * 64 + 1, 30, 900], 0, 2, 20),
+    ([16 * 512, 16 * 511 + 3, 16 * 257], 2, 1, 100),  # (up to 512: one launch)
+    ([16 * 512 + 1, 100, 16 * 400], 2, 1, 100),
 ])
 def test_decode_rows(gpu_lib, hq, hkv, d, lens, sink, recent, blocks):
     say(f"[select] {hq}/{hkv} heads of {d}, {lens}, {sink}+{recent} of {blocks}")
@@ -135,7 +139,7 @@ def test_long_rows(gpu_lib):
     check(run(gpu_lib, *args), *args)
 
 
-@pytest.mark.parametrize("n", [40, 300, 2000])
+@pytest.mark.parametrize("n", [40, 300, 600, 2000])
 def test_scores_that_32_bits_cannot_tell_apart(gpu_lib, n):
     """Sums near 2^10 that differ by 2^-20 and less, in random order: all of them candidates."""
     rng = np.random.default_rng(n)
@@ -152,7 +156,7 @@ def test_scores_that_32_bits_cannot_tell_apart(gpu_lib, n):
         check(run(gpu_lib, *args), *args)
 
 
-@pytest.mark.parametrize("n", [100, 3000])
+@pytest.mark.parametrize("n", [40, 100, 700, 3000])
 def test_equal_scores_go_to_the_lowest_index(gpu_lib, n):
     rng = np.random.default_rng(n)
     tables, bounds = pool(rng, [n * BS], 2, 64)
@@ -171,9 +175,9 @@ def test_equal_scores_go_to_the_lowest_index(gpu_lib, n):
     check(run(gpu_lib, *args), *args)
 
 
-def test_values_that_are_not_finite(gpu_lib):
+@pytest.mark.parametrize("n", [75, 200, 900])
+def test_values_that_are_not_finite(gpu_lib, n):
     rng = np.random.default_rng(6)
-    n = 200
     tables, bounds = pool(rng, [n * BS, n * BS], 2, 128)
     q = rand_bf16(rng, (2, 8, 128))
     b = bounds.copy()
@@ -188,10 +192,10 @@ def test_values_that_are_not_finite(gpu_lib):
     check(run(gpu_lib, *args), *args)
 
 
-def test_large_and_tiny_values(gpu_lib):
+@pytest.mark.parametrize("n", [60, 300, 700])
+def test_large_and_tiny_values(gpu_lib, n):
     """Sums that pass the 32-bit range both ways, and products below it."""
     rng = np.random.default_rng(7)
-    n = 300
     for scale_q, scale_b in ((2.0**100, 2.0**100), (2.0**-100, 2.0**-60), (2.0**-130, 1.0),
                              (1.0, 2.0**-130), (2.0**120, 1.0)):
         tables, bounds = pool(rng, [n * BS], 2, 64, nan=False)
