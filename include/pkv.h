@@ -464,7 +464,9 @@ pkv_status pkv_block_bounds(const pkv_paged_kv* kv, void* bounds, const int32_t*
  * block's bounds (pkv_block_bounds) could score for any of the group's query heads:
  *   s[block] = max_h sum_d q[t][h][d] * (q[t][h][d] > 0 ? bounds[block][0][d] : bounds[block][1][d]).
  * The first sink_blocks and the last recent_blocks (>= 1: the row's own block) are always taken,
- * the others by falling s, equal ones by rising index; a block whose s is not finite comes first.
+ * the others by falling s, equal ones by rising index. A bound that is not finite, read by the
+ * sum or not, puts its block first; a query that is not finite makes all blocks of its row and
+ * kv head equal.
  * The choice is by the exact value of s (its products summed in 64 bits), whatever the order in
  * which the kernels sum. sel: int32 [rows][num_kv_heads][blocks] receives the chosen logical
  * block indices in ascending order, then -1 where the row has fewer blocks.

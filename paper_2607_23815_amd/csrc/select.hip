@@ -322,8 +322,8 @@ __device__ __forceinline__ double row_sum(double x) {  // over 16 lanes (lane 0'
 }
 
 // Scores in 64 bits by one wave, four blocks at a time: 16 lanes take block b, each of them D / 16
-// dims for every head. The key's unsigned order is the scores' order (a score that is not finite
-// counts as +infinity); it is never 0 and never ~0, and valid in the first of the 16 lanes.
+// dims for every head. The key's unsigned order is the scores' order (a bound or query that is
+// not finite makes it +infinity); it is never 0 and never ~0, and valid in the first of the 16 lanes.
 template <int D>
 __device__ __forceinline__ uint64_t exact_key(const SelectArgs& a, const uint16_t* q, int g,
                                               const int32_t* table, int kvh, int b) {

@@ -192,6 +192,23 @@ def test_values_that_are_not_finite(gpu_lib, n):
     check(run(gpu_lib, *args), *args)
 
 
+@pytest.mark.parametrize("n", [40, 300, 700])
+@pytest.mark.parametrize("side", [0, 1])
+def test_an_infinite_bound_that_no_query_takes(gpu_lib, n, side):
+    """Queries of one sign, which read the other side of the box: the block comes first all the same."""
+    rng = np.random.default_rng(8)
+    tables, bounds = pool(rng, [n * BS], 1, 128)
+    q = rand_bf16(rng, (1, 4, 128)) & 0x7FFF
+    if side == 0:
+        q |= 0x8000
+    b = bounds.copy()
+    b[tables[0, n // 2], 0, side, 77] = (0x7F80, 0xFF80)[side]
+    args = (tables, b, q, np.array([n * BS]), 1, 1, 4)
+    got = run(gpu_lib, *args)
+    check(got, *args)
+    assert n // 2 in got[0, 0].tolist()
+
+
 @pytest.mark.parametrize("n", [60, 300, 700])
 def test_large_and_tiny_values(gpu_lib, n):
     """Sums that pass the 32-bit range both ways, and products below it."""
