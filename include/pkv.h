@@ -493,8 +493,8 @@ size_t pkv_select_workspace_bytes(int32_t rows, int32_t num_q_heads, int32_t num
  * Entries of sel that name no block of the row (-1, or past its last) are passed over, as are
  * table entries outside the pool; the others must differ from one another and may come in any
  * order. Every block of a row listed, the result is pkv_decode_attention's up to the order of
- * its sums. A row without a visible key (row_lens[t] 0, nothing listed), or whose scores are all
- * -infinity, gives zeros and an LSE of -infinity. bf16 inputs, 32-bit sums, weights rounded to
+ * its sums, infinite values included. A row without a visible key (row_lens[t] 0, nothing listed), or
+ * whose scores are all -infinity, gives zeros and an LSE of -infinity. bf16 inputs, 32-bit sums, weights rounded to
  * bf16 for the value product (as in decode), bf16 output. At most 65536 blocks are
  * chosen for a row; row_lens has no such limit. workspace: at least pkv_sparse_workspace_bytes (0 where there are rows
  * enough to fill the chip), 16-byte aligned, owned by the caller, not read back; calls that

@@ -15,6 +15,11 @@
 // A column's maximum is only brought up to date when a score passes it by 2^kSlack: until then
 // weights may reach 2^kSlack, which costs neither range nor precision (32-bit sums, and bf16 has the
 // same relative step everywhere), and most steps need no lane exchange and no rescaling.
+//
+// A zero weight is no mask for a value that is not finite: 0 x inf is NaN, in the columns of the ways
+// that the value is not for. A wave whose sums end up so takes its share again with one way, whose
+// columns hold every block's weights (sparse_share): an infinite value then makes its dim infinite,
+// whatever the number of heads. Values that are finite cost one look at the sums per wave.
 #include <math.h>
 
 #include "decode_impl.h"
@@ -265,6 +270,27 @@ __device__ __forceinline__ void sparse_load_q(const SparseArgs& a, const SparseR
   }
 }
 
+// The wave's share, infinities and NaN in it as the sums' definition has them.
+template <int D, int kWays>
+__device__ __forceinline__ void sparse_share(const SparseArgs& a, const SparseRow& r,
+                                             const bf16x8 (&qf)[D / 32], const int e0,
+                                             const int e1, f32x4 (&acc)[D / 16], float& m,
+                                             float& l) {
+  const int32_t* list = a.sel + r.item * a.blocks;
+  const int32_t* table = a.tables + (size_t)r.seq * a.max_blocks;
+  sparse_range<D, kWays>(a, qf, list, table, r.kvh, r.len, e0, e1, acc, m, l);
+  if constexpr (kWays > 1) {
+    float odd = 0.f;  // NaN if a sum is not finite
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) odd = fmaf(acc[db][e], 0.f, odd);
+    }
+    if (__builtin_amdgcn_ballot_w64(odd != odd) != 0)
+      sparse_range<D, 1>(a, qf, list, table, r.kvh, r.len, e0, e1, acc, m, l);
+  }
+}
+
 // One wave per (row, kv head).
 template <int D, int kWays>
 __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2, 2)))
@@ -277,8 +303,7 @@ void sparse_wave_kernel(const SparseArgs a) {
   sparse_load_q<D, kWays>(a, r, g, qf);
   f32x4 acc[DB];
   float m, l;
-  sparse_range<D, kWays>(a, qf, a.sel + r.item * a.blocks, a.tables + (size_t)r.seq * a.max_blocks,
-                         r.kvh, r.len, 0, a.blocks, acc, m, l);
+  sparse_share<D, kWays>(a, r, qf, 0, a.blocks, acc, m, l);
   const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
   const int h = col % (16 / kWays), way = col / (16 / kWays);
   if (h >= g) return;
@@ -318,8 +343,7 @@ void sparse_group_kernel(const SparseArgs a) {
   sparse_load_q<D, kWays>(a, r, g, qf);
   f32x4 acc[DB];
   float m, l;
-  sparse_range<D, kWays>(a, qf, a.sel + r.item * a.blocks, a.tables + (size_t)r.seq * a.max_blocks,
-                         r.kvh, r.len, s0, s1, acc, m, l);
+  sparse_share<D, kWays>(a, r, qf, s0, s1, acc, m, l);
   const int hcol = col % (16 / kWays), way = col / (16 / kWays);
   if (hcol < g) {
 #pragma unroll

@@ -303,3 +303,53 @@ def test_no_rows(gpu_lib):
     gpu_lib.pkv_sparse_attention(to_dev_bits(pk), to_dev_bits(pv), e, i32(tables), i32([]),
                                  torch.empty((0, 2, 3), dtype=torch.int32, device="cuda"), 0.1, e,
                                  row_seq=i32([]))
+
+
+def kinds(x):
+    """0 where finite, 1 and -1 for the infinities, 2 for NaN."""
+    return np.where(np.isnan(x), 2, np.where(np.isinf(x), np.sign(x), 0))
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(2, 2, 64), (8, 2, 128), (16, 2, 64), (16, 1, 128), (28, 4, 128)])
+@pytest.mark.parametrize("lens,blocks", [([40, 170], 12), ([3000, 16 * 150], 188), ([60] * 300, 4)])
+def test_infinite_values_of_positive_weight(gpu_lib, hq, hkv, d, lens, blocks):
+    """An infinite value at a visible key makes its dim infinite (NaN where both infinities meet) for
+    every head of its kv head, however many these are, as in pkv_decode_attention; the other dims
+    stay within their tolerance, and a value that the list or the length hides changes nothing. A wave
+    of its own per row, four waves, and splits."""
+    import torch
+    lib = gpu_lib
+    rng = np.random.default_rng(d + hq)
+    tables, pk, pv = pools(rng, lens, hkv, d)
+    q = rand_bf16(rng, (len(lens), hq, d))
+    lens = np.array(lens)
+    n = -(-lens // BS)
+    for t in range(len(lens)):
+        for dim, bits, block in ((3, 0x7F80, 0), (17, 0xFF80, 1), (40, 0x7F80, n[t] - 1),
+                                 (50, 0x7F80, 0), (50, 0xFF80, 2)):
+            slot = rng.integers(0, (lens[t] - 1) % BS + 1)
+            pv[tables[t, block], hkv - 1, dim, slot] = bits
+    sel = np.full((len(lens), hkv, blocks), -1, np.int32)
+    for t in range(len(lens)):
+        sel[t, :, :n[t]] = np.arange(n[t])
+    args = (tables, pk, pv, q, lens, sel, d ** -0.5)
+    out, lse = run(lib, *args)
+    with np.errstate(invalid="ignore"):
+        want, tol, want_lse, ltol = expect(*args)
+    got = bf16_to_f64(out)
+    assert np.array_equal(kinds(got), kinds(want))
+    fine = np.isfinite(want)
+    assert (abs(got[fine] - want[fine]) <= tol[fine]).all() and (abs(lse - want_lse) <= ltol).all()
+    g = hq // hkv
+    for dim, kind in ((3, 1), (17, -1), (40, 1), (50, 2)):
+        assert (kinds(got[:, -g:, dim]) == kind).all()
+    assert np.isfinite(got[:, :hq - g]).all()
+    dense = torch.empty(q.shape, dtype=torch.bfloat16, device="cuda")
+    lib.pkv_decode_attention(to_dev_bits(pk), to_dev_bits(pv), to_dev_bits(q), i32(tables), i32(lens),
+                             int(lens.max()), d ** -0.5, dense)
+    assert np.array_equal(kinds(bf16_to_f64(to_host_bits(dense))), kinds(got))
+    # hidden by the list, and by the row's length
+    sel[:, :, :3] = -1
+    hide = np.maximum(n - 1, 0) * BS
+    got = run(lib, tables, pk, pv, q, hide, sel, d ** -0.5)[0]
+    assert np.isfinite(bf16_to_f64(got)).all()
