@@ -493,9 +493,10 @@ size_t pkv_select_workspace_bytes(int32_t rows, int32_t num_q_heads, int32_t num
  * Entries of sel that name no block of the row (-1, or past its last) are passed over, as are
  * table entries outside the pool; the others must differ from one another and may come in any
  * order. Every block of a row listed, the result is pkv_decode_attention's up to the order of
- * its sums, infinite values included. A row without a visible key (row_lens[t] 0, nothing listed), or
- * whose scores are all -infinity, gives zeros and an LSE of -infinity. bf16 inputs, 32-bit sums, weights rounded to
- * bf16 for the value product (as in decode), bf16 output. At most 65536 blocks are
+ * its sums and the rounding of its weights, infinite values included. A row without a visible key
+ * (row_lens[t] 0, nothing listed), or whose scores are all -infinity, gives zeros and an LSE of
+ * -infinity. bf16 inputs, 32-bit sums, bf16 output; weights reach the value product with 16 bits or more (2^-16 of themselves; rounded
+ * to bf16, as in decode, where values that are not finite are met). At most 65536 blocks are
  * chosen for a row; row_lens has no such limit. workspace: at least pkv_sparse_workspace_bytes (0 where there are rows
  * enough to fill the chip), 16-byte aligned, owned by the caller, not read back; calls that
  * share one must not overlap. */

@@ -8,18 +8,24 @@
 //
 // A product has 16 columns and a group often fewer heads, so the heads stand in the columns
 // kWays = 2 or 4 times over (g <= 8, g <= 4), and column (way w, head h) goes on with the scores of
-// blocks w, w + kWays, ... alone: its weights for the other blocks are zeros in the value product.
-// Every lane's exponentials are then of use (4 per lane and step instead of 16 at g <= 4), each way
-// keeps a softmax of its own, and the ways meet at the end of the wave's share.
+// blocks w, w + kWays, ... alone. Every lane's exponentials are then of use (4 per lane and step instead
+// of 16 at g <= 4), the ways share a maximum, and their sums meet at the end of the wave's share.
+//
+// The value product takes bf16, and a weight rounded to it would be off by up to 2^-8 of itself, which
+// stands beside the output's own rounding. So a weight goes in two parts, itself rounded and what that
+// left over, off by at most 2^-16 together. The second part costs no product where there are several
+// ways: it stands in the next way's column, whose weights for the block would be zeros (kWays 1 takes a
+// second product).
 //
 // A column's maximum is only brought up to date when a score passes it by 2^kSlack: until then
 // weights may reach 2^kSlack, which costs neither range nor precision (32-bit sums, and bf16 has the
 // same relative step everywhere), and most steps need no lane exchange and no rescaling.
 //
 // A zero weight is no mask for a value that is not finite: 0 x inf is NaN, in the columns of the ways
-// that the value is not for. A wave whose sums end up so takes its share again with one way, whose
-// columns hold every block's weights (sparse_share): an infinite value then makes its dim infinite,
-// whatever the number of heads. Values that are finite cost one look at the sums per wave.
+// that the value is not for, and two parts of either sign make NaN of it too. A wave whose sums end up
+// so takes its share again with one way and weights in one part (sparse_share): an infinite value then
+// makes its dim infinite, whatever the number of heads. Values that are finite cost one look at the sums
+// per wave.
 #include <math.h>
 
 #include "decode_impl.h"
@@ -67,10 +73,17 @@ __device__ __forceinline__ float ways_max(float x) {
   return x;
 }
 
-// One wave's share: entries [e0, e1) of a list. Leaves, merged over the ways, the unnormalised output
+// Two floats as two bf16 each, their sum off by 2^-16 of the float at most (its second part is exact in
+// 32 bits, then rounded).
+__device__ __forceinline__ void two_parts(float x, float y, uint32_t& first, uint32_t& second) {
+  first = pack_bf16x2(x, y);
+  second = pack_bf16x2(x - __uint_as_float(first << 16), y - __uint_as_float(first & 0xFFFF0000u));
+}
+
+// One wave's share: entries [e0, e1) of a list. Leaves, summed over the ways, the unnormalised output
 // (lane (col, grp) holds dims 16 db + 4 grp + 0..3 of head col % (16 / kWays)), the maximum (base 2)
 // and the weight sum.
-template <int D, int kWays>
+template <int D, int kWays, bool kTwoParts>
 __device__ __forceinline__ void sparse_range(const SparseArgs& a, const bf16x8 (&qf)[D / 32],
                                              const int32_t* __restrict__ list,
                                              const int32_t* __restrict__ table, const int kvh,
@@ -186,7 +199,7 @@ __device__ __forceinline__ void sparse_range(const SparseArgs& a, const bf16x8 (
       }
       mx *= a.scale_log2;
       if (__builtin_amdgcn_ballot_w64(mx > m + kSlack) != 0) {
-        const float m_new = fmaxf(m, dec::wave_max16(mx));
+        const float m_new = fmaxf(m, ways_max<kWays>(dec::wave_max16(mx)));
         const float alpha = fast_exp2(m - finite_max(m_new));
         m = m_new;
         lpart *= alpha;
@@ -197,7 +210,8 @@ __device__ __forceinline__ void sparse_range(const SparseArgs& a, const bf16x8 (
         }
       }
       const float m_sub = finite_max(m);
-      uint32_t p[kStep][2];
+      constexpr int kProducts = kWays == 1 && kTwoParts ? 2 : 1;
+      uint32_t p[kProducts][kStep][2];
 #pragma unroll
       for (int j = 0; j < kMine; ++j) {
         float x[4];
@@ -206,33 +220,43 @@ __device__ __forceinline__ void sparse_range(const SparseArgs& a, const bf16x8 (
           x[r] = fast_exp2(fmaf(sv[j][r], a.scale_log2, -m_sub));
           lpart += x[r];
         }
-        const uint32_t lo = pack_bf16x2(x[0], x[1]), hi = pack_bf16x2(x[2], x[3]);
 #pragma unroll
-        for (int w = 0; w < kWays; ++w) {
-          p[j * kWays + w][0] = way == w ? lo : 0u;
-          p[j * kWays + w][1] = way == w ? hi : 0u;
+        for (int e = 0; e < 2; ++e) {
+          uint32_t first, second;
+          two_parts(x[2 * e], x[2 * e + 1], first, second);
+          if constexpr (kWays == 1) {
+            p[0][j][e] = first;
+            if constexpr (kTwoParts) p[1][j][e] = second;
+          } else {
+            // (the second part of the way before, from its columns)
+            second = dpp<kWays == 4 ? kRor4 : kRor8>(second);
+#pragma unroll
+            for (int w = 0; w < kWays; ++w)
+              p[0][j * kWays + w][e] = way == w ? first : way == (w + 1) % kWays ? second : 0u;
+          }
         }
       }
 #pragma unroll
-      for (int i = 0; i < kStep; i += 2) {
-        const u32x2 x = swap_rows(p[i][0], p[i + 1][0]), y = swap_rows(p[i][1], p[i + 1][1]);
-        const u32x4 pb = {x[0], y[0], x[1], y[1]};
+      for (int k = 0; k < kProducts; ++k) {
 #pragma unroll
-        for (int db = 0; db < DB; ++db)
-          acc[db] = mfma16(as_bf16x8(v[i / 2][db]), as_bf16x8(pb), acc[db]);
+        for (int i = 0; i < kStep; i += 2) {
+          const u32x2 x = swap_rows(p[k][i][0], p[k][i + 1][0]);
+          const u32x2 y = swap_rows(p[k][i][1], p[k][i + 1][1]);
+          const u32x4 pb = {x[0], y[0], x[1], y[1]};
+#pragma unroll
+          for (int db = 0; db < DB; ++db)
+            acc[db] = mfma16(as_bf16x8(v[i / 2][db]), as_bf16x8(pb), acc[db]);
+        }
       }
       if (more) load_v(s + kStep);
     }
   }
-  const float top = ways_max<kWays>(m);
-  const float scale = fast_exp2(m - finite_max(top));
-  l_out = ways_sum<kWays>(dec::wave_sum16(lpart) * scale);
-  m_out = top;
+  l_out = ways_sum<kWays>(dec::wave_sum16(lpart));
+  m_out = m;
 #pragma unroll
   for (int db = 0; db < DB; ++db) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-      acc_out[db][r] = kWays == 1 ? acc[db][r] : ways_sum<kWays>(acc[db][r] * scale);
+    for (int r = 0; r < 4; ++r) acc_out[db][r] = ways_sum<kWays>(acc[db][r]);
   }
 }
 
@@ -278,17 +302,15 @@ __device__ __forceinline__ void sparse_share(const SparseArgs& a, const SparseRo
                                              float& l) {
   const int32_t* list = a.sel + r.item * a.blocks;
   const int32_t* table = a.tables + (size_t)r.seq * a.max_blocks;
-  sparse_range<D, kWays>(a, qf, list, table, r.kvh, r.len, e0, e1, acc, m, l);
-  if constexpr (kWays > 1) {
-    float odd = 0.f;  // NaN if a sum is not finite
+  sparse_range<D, kWays, true>(a, qf, list, table, r.kvh, r.len, e0, e1, acc, m, l);
+  float odd = 0.f;  // NaN if a sum is not finite
 #pragma unroll
-    for (int db = 0; db < D / 16; ++db) {
+  for (int db = 0; db < D / 16; ++db) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) odd = fmaf(acc[db][e], 0.f, odd);
-    }
-    if (__builtin_amdgcn_ballot_w64(odd != odd) != 0)
-      sparse_range<D, 1>(a, qf, list, table, r.kvh, r.len, e0, e1, acc, m, l);
+    for (int e = 0; e < 4; ++e) odd = fmaf(acc[db][e], 0.f, odd);
   }
+  if (__builtin_amdgcn_ballot_w64(odd != odd) != 0)
+    sparse_range<D, 1, false>(a, qf, list, table, r.kvh, r.len, e0, e1, acc, m, l);
 }
 
 // One wave per (row, kv head).

@@ -353,3 +353,30 @@ def test_infinite_values_of_positive_weight(gpu_lib, hq, hkv, d, lens, blocks):
     hide = np.maximum(n - 1, 0) * BS
     got = run(lib, tables, pk, pv, q, hide, sel, d ** -0.5)[0]
     assert np.isfinite(bf16_to_f64(got)).all()
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(2, 2, 64), (8, 2, 128), (16, 2, 64), (16, 1, 128), (28, 4, 128)])
+@pytest.mark.parametrize("lens,blocks", [([90, 33], 6), ([100, 160], 10), ([16 * 100], 100),
+                                         ([60] * 300, 4)])
+def test_weights_keep_more_than_bf16(gpu_lib, hq, hkv, d, lens, blocks):
+    """Weights reach the value product in two bf16 parts, off by 2^-16 of themselves, 2 n products per
+    element whose sums are off by 2^-23 an addition, and some 2^-24 for exp2, division and rescaling:
+        |error| <= (2^-16 + 2 delta + (5 n + 32) 2^-24) sum_p w_p |v_p| + 2^-8 |out|.
+    Weights rounded once (2^-8) are past this where values cancel."""
+    rng = np.random.default_rng(d + hq)
+    tables, pk, pv = pools(rng, lens, hkv, d)
+    q = rand_bf16(rng, (len(lens), hq, d))
+    lens = np.array(lens)
+    args = (tables, pk, pv, q, lens, lists(rng, lens, hkv, blocks), 2 * d ** -0.5)
+    want, loose = expect(*args)[:2]
+    n = (-(-lens // BS)).clip(max=blocks)[:, None, None] * BS
+    # (the looser tolerance less its share of rounded weights, and the sums' share)
+    weight = np.zeros_like(want)
+    for r in range(len(lens)):  # sum_p w_p |v_p|
+        weight[r] = expect(tables, pk, pv & 0x7FFF, q[r:r + 1], lens[r:r + 1], args[5][r:r + 1], args[6],
+                           [r])[0][0]
+    delta2 = (loose - 2.0**-8 * abs(want)) / weight - 2.0**-8  # (2 delta + n 2^-24, n visible keys)
+    tol = (2.0**-16 + delta2 + (4 * n + 32) * 2.0**-24) * weight + 2.0**-8 * abs(want)
+    err = abs(bf16_to_f64(run(gpu_lib, *args)[0]) - want)
+    say(f"  {(err / tol).max():.2f} of the tolerance")
+    assert (err <= tol).all()
