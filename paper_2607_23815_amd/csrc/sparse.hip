@@ -18,14 +18,15 @@
 // second product).
 //
 // A column's maximum is only brought up to date when a score passes it by 2^kSlack: until then
-// weights may reach 2^kSlack, which costs neither range nor precision (32-bit sums, and bf16 has the
-// same relative step everywhere), and most steps need no lane exchange and no rescaling.
+// weights may reach 2^kSlack, which costs no precision (32-bit sums, and bf16 has the same relative step
+// everywhere), and most steps need no lane exchange and no rescaling.
 //
 // A zero weight is no mask for a value that is not finite: 0 x inf is NaN, in the columns of the ways
-// that the value is not for, and two parts of either sign make NaN of it too. A wave whose sums end up
-// so takes its share again with one way and weights in one part (sparse_share): an infinite value then
-// makes its dim infinite, whatever the number of heads. Values that are finite cost one look at the sums
-// per wave.
+// that the value is not for, two parts of either sign make NaN of it too, and weights of 2^kSlack
+// may carry large values past the 32-bit range. A wave whose sums are not finite takes its share again
+// with one way, weights in one part and maxima always up to date (sparse_share), as the decode does: an
+// infinite value then makes its dim infinite, and a finite one does not, whatever the number of heads.
+// Sums that are finite cost one look per wave.
 #include <math.h>
 
 #include "decode_impl.h"
@@ -93,6 +94,7 @@ __device__ __forceinline__ void sparse_range(const SparseArgs& a, const bf16x8 (
   constexpr int KK = D / 32, DB = D / 16, SLAB = D * kBlockSize;
   constexpr int SLAB_BYTES = SLAB * 2;
   constexpr int kMine = kStep / kWays;  // blocks per step whose scores a column goes on with
+  constexpr float kPast = kTwoParts ? kSlack : 0.f;  // (the other form takes sums that overflow, too)
   const int lane = threadIdx.x & 63;
   const int col = lane & 15, grp = lane >> 4;
   const int way = col / (16 / kWays);
@@ -198,7 +200,7 @@ __device__ __forceinline__ void sparse_range(const SparseArgs& a, const bf16x8 (
         }
       }
       mx *= a.scale_log2;
-      if (__builtin_amdgcn_ballot_w64(mx > m + kSlack) != 0) {
+      if (__builtin_amdgcn_ballot_w64(mx > m + kPast) != 0) {
         const float m_new = fmaxf(m, ways_max<kWays>(dec::wave_max16(mx)));
         const float alpha = fast_exp2(m - finite_max(m_new));
         m = m_new;

@@ -380,3 +380,27 @@ def test_weights_keep_more_than_bf16(gpu_lib, hq, hkv, d, lens, blocks):
     err = abs(bf16_to_f64(run(gpu_lib, *args)[0]) - want)
     say(f"  {(err / tol).max():.2f} of the tolerance")
     assert (err <= tol).all()
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(4, 4, 64), (8, 2, 128), (16, 2, 64), (16, 1, 128)])
+def test_values_near_the_largest(gpu_lib, hq, hkv, d):
+    """A value of 2^126 at a score that passes the earlier ones by 7 (base 2): its weight is 1 in the end
+    and the sums stay finite, as in pkv_decode_attention, for each sign. (Keys of the earlier steps hold
+    ordinary values: 64 of 2^126 with a weight of 1 would pass the 32-bit range in any order.)"""
+    import torch
+    lib = gpu_lib
+    rng = np.random.default_rng(d)
+    lens = np.array([75])
+    tables, pk, pv = pools(rng, list(lens), hkv, d)
+    pk[tables[0, :5]] = 0
+    pk[tables[0, 4], :, 0, 6, 0] = 0x3F80  # 1
+    pv[tables[0, 4], :, :, 6] = np.where(rng.integers(0, 2, (hkv, d)), 0x7E80, 0xFE80)
+    q = np.zeros((1, hq, d), np.uint16)
+    q[:, :, 0] = 0x40E0  # 7
+    args = (tables, pk, pv, q, lens, np.arange(5, dtype=np.int32).reshape(1, 1, 5).repeat(hkv, 1),
+            math.log(2))
+    check(run(lib, *args), *args)
+    out = torch.empty(q.shape, dtype=torch.bfloat16, device="cuda")
+    lib.pkv_decode_attention(to_dev_bits(pk), to_dev_bits(pv), to_dev_bits(q), i32(tables), i32(lens), 75,
+                             math.log(2), out)
+    check((to_host_bits(out), None), *args)
