@@ -56,8 +56,10 @@ __device__ __forceinline__ uint32_t most_of(uint32_t most, uint32_t w) {
                             __builtin_elementwise_max(__builtin_bit_cast(u16x2, most),
                                                       __builtin_bit_cast(u16x2, w & 0x7FFF7FFFu)));
 }
-__device__ __forceinline__ float most_value(uint32_t most) {  // over the wave
-  return __uint_as_float(wave_all(max(most & 0xFFFFu, most >> 16), Max()) << 16);
+// Over the wave, a NaN as infinity: a maximum of floats would pass a NaN over, and with it all that it
+// stands for.
+__device__ __forceinline__ float most_value(uint32_t most) {
+  return __uint_as_float(min(wave_all(max(most & 0xFFFFu, most >> 16), Max()), 0x7F80u) << 16);
 }
 // The largest of n of a lane's four sums; +infinity if one of them (or their sum) is not finite.
 template <int n>

@@ -333,3 +333,54 @@ def test_two_calls_at_once(gpu_lib):
     torch.cuda.synchronize()
     for s in sides:
         check(s["sel"].cpu().numpy(), *s["host"])
+
+
+def close_boxes(rng, n, d):
+    """n boxes whose scores with queries of ones are 0, 1, .. (n - 1 times 2^-8), in random order, by
+    sums of large terms that cancel: 32-bit sums are off by more than the scores differ."""
+    large = rng.integers(128, 256, (d - 2) // 2) * 2.0 ** rng.integers(-9, 14, (d - 2) // 2)
+    terms = np.concatenate([large, -large])
+    step = rng.permutation(n)
+    box = np.empty((n, d))
+    for b in range(n):
+        box[b, :2] = step[b] // 128 * 2.0**-1, step[b] % 128 * 2.0**-8
+        box[b, 2:] = rng.permutation(terms)
+    return bf16(box)
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(4, 2, 64), (4, 1, 128)])
+@pytest.mark.parametrize("n,sink,nans,close,blocks", [
+    (40, 1, [0], range(1, 39), 20),                     # (one wave, scores of its own)
+    (40, 0, [39], range(0, 39), 20),                    # the row's own block
+    (300, 1, [0], range(64, 80), 9),                    # (four waves, both tiles the first one's)
+    (700, 1, [0], range(1, 16), 9),                     # (scores of a launch before)
+    (3000, 0, [2999], range(2992, 2999), 5)])
+def test_a_nan_bound_beside_close_scores(gpu_lib, hq, hkv, d, n, sink, nans, close, blocks):
+    """A NaN in a block that is chosen anyway: the others are chosen by their exact scores still."""
+    rng = np.random.default_rng(n + d)
+    tables, bounds = pool(rng, [n * BS], hkv, d, nan=False)
+    at = tables[0]
+    bounds[at[:n]] = bf16(np.full(d, -2.0**-6))
+    for h in range(hkv):
+        bounds[at[close.start:close.stop], h] = close_boxes(rng, len(close), d)[:, None]
+    q = bf16(np.ones((1, hq, d)))
+    args = (tables, bounds, q, np.array([n * BS]), sink, 1, blocks)
+    check(run(gpu_lib, *args), *args)
+    bounds[at[nans], :, 0, 5] = 0x7FC0
+    check(run(gpu_lib, *args), *args)
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(4, 2, 64), (4, 1, 128)])
+def test_a_nan_bound_that_only_later_rows_see(gpu_lib, hq, hkv, d):
+    rng = np.random.default_rng(d)
+    n = 600
+    tables, bounds = pool(rng, [n * BS], hkv, d, nan=False)
+    at = tables[0]
+    bounds[at[:n]] = bf16(np.full(d, -2.0**-6))
+    for h in range(hkv):
+        bounds[at[577:585], h] = close_boxes(rng, 8, d)[:, None]
+    bounds[at[595], :, 1, 7] = 0x7FC0
+    q = bf16(np.ones((3, hq, d)))
+    seen = np.array([586 * BS - 3, 586 * BS, n * BS])
+    args = (tables, bounds, q, seen, 0, 1, 5, np.zeros(3, np.int64))
+    check(run(gpu_lib, *args), *args)
