@@ -584,8 +584,8 @@ def pkv_decode_attention(k_cache, v_cache, q, block_tables, seq_lens, max_seq_le
     kv = paged_kv(k_cache, v_cache)
     b, hq, d = q.shape
     if workspace is None:  # convenience for one-off calls; timed callers pass their own
-        workspace = alloc_workspace(pkv_decode_workspace_bytes(b, hq, int(k_cache.shape[1]), d,
-                                                               int(max_seq_len)))
+        workspace = _one_off_workspace(pkv_decode_workspace_bytes(b, hq, int(k_cache.shape[1]), d,
+                                                                  int(max_seq_len)), stream)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(_lib.pkv_decode_attention(
         ctypes.byref(kv), _dev_ptr(q, "q", torch.bfloat16), hq,
@@ -626,8 +626,8 @@ def pkv_mixed_attention(k_cache, v_cache, scale: float,
     b = cached_lens.shape[0]
     bd = int(seq_lens.shape[0])
     if workspace is None:
-        workspace = alloc_workspace(pkv_decode_workspace_bytes(bd, hq, int(k_cache.shape[1]), d,
-                                                               int(max_seq_len)))
+        workspace = _one_off_workspace(pkv_decode_workspace_bytes(bd, hq, int(k_cache.shape[1]), d,
+                                                                  int(max_seq_len)), stream)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(_lib.pkv_mixed_attention(
         ctypes.byref(kv), hq, float(scale), _dev_ptr(q, "q", torch.bfloat16),
@@ -811,8 +811,8 @@ def pkv_select_blocks(bounds, q, block_tables, row_lens, max_len: int, sink_bloc
     nb, hkv, _, d = box
     n, hq, b, max_blocks, blocks = _row_sizes(q, block_tables, row_lens, row_seq, sel, hkv, d)
     if workspace is None:  # convenience for one-off calls; timed callers pass their own
-        workspace = alloc_workspace(pkv_select_workspace_bytes(n, hq, hkv, d, int(max_len),
-                                                               blocks))
+        workspace = _one_off_workspace(pkv_select_workspace_bytes(n, hq, hkv, d, int(max_len),
+                                                                  blocks), stream)
     ws, ws_bytes = _workspace(workspace, dev)
     _check(_lib.pkv_select_blocks(
         _ptr(bounds, "bounds", _bf16, dev), nb, hkv, d, _ptr(q, "q", _bf16, dev), hq,
@@ -838,7 +838,7 @@ def pkv_sparse_attention(k_cache, v_cache, q, block_tables, row_lens, sel, scale
     if lse is not None and lse.shape != (n, hq):
         raise ValueError("lse must be [rows][Hq]")
     if workspace is None:  # convenience for one-off calls; timed callers pass their own
-        workspace = alloc_workspace(pkv_sparse_workspace_bytes(n, hq, hkv, d, blocks))
+        workspace = _one_off_workspace(pkv_sparse_workspace_bytes(n, hq, hkv, d, blocks), stream)
     ws, ws_bytes = _workspace(workspace, dev)
     _check(_lib.pkv_sparse_attention(
         ctypes.byref(kv), _ptr(q, "q", _bf16, dev), hq,
@@ -856,3 +856,12 @@ def alloc_workspace(nbytes: int, device="cuda"):
     if nbytes == 0:
         return None
     return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def _one_off_workspace(nbytes: int, stream):
+    """The workspace of a call that brought none. It is dropped when the call returns, while its kernels
+    may not have run: memory of the stream that they run on, which only later work of this stream gets."""
+    if stream is None or nbytes == 0:
+        return alloc_workspace(nbytes)
+    with _get_torch().cuda.stream(stream):
+        return alloc_workspace(nbytes)
