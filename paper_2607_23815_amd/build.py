@@ -85,10 +85,18 @@ def build(verbose: bool = False, sanitize: bool = False) -> str:
     return out
 
 
-def build_binding(verbose: bool = False) -> str:
+def build_binding(verbose: bool = False):
+    """_tensor_address.so, or None where torch or g++ is missing (libpkv.so needs neither)."""
     import sysconfig
 
-    from torch.utils.cpp_extension import include_paths, library_paths
+    try:
+        from torch.utils.cpp_extension import include_paths, library_paths
+    except ImportError:
+        print("_tensor_address.so is not built: torch cannot be imported", file=sys.stderr)
+        return None
+    if shutil.which("g++") is None:
+        print("_tensor_address.so is not built: g++ not found", file=sys.stderr)
+        return None
     tmp = BINDING + ".tmp"
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-o", tmp,
            os.path.join(CSRC, "tensor_address.cpp"), "-isystem",
@@ -112,6 +120,6 @@ if __name__ == "__main__":
     if "--asan-runtime" in sys.argv:
         print(asan_runtime())
     else:
-        if "--sanitize" not in sys.argv:
-            print(build_binding(verbose=True))
         print(build(verbose=True, sanitize="--sanitize" in sys.argv))
+        if "--sanitize" not in sys.argv:
+            build_binding(verbose=True)
