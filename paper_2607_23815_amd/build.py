@@ -1,5 +1,6 @@
 """Build libpkv.so (the HIP kernels for gfx950 plus the C ABI) in-tree with hipcc, and
-_tensor_address.so (the binding's look at its tensors, host code against torch's headers).
+_tensor_address (the binding's look at its tensors, host code against torch's headers, for this
+interpreter and this torch; without it the binding looks in Python).
 
     python -m paper_2607_23815_amd.build
     python -m paper_2607_23815_amd.build --sanitize   # libpkv_asan.so, see below
@@ -24,12 +25,14 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libpkv.so")
-BINDING = os.path.join(PKG, "_tensor_address.so")
+# (the interpreter's tag: one of another version passes it over)
+BINDING = os.path.join(PKG, "_tensor_address" + sysconfig.get_config_var("EXT_SUFFIX"))
 ASAN_LIB = os.path.join(PKG, "libpkv_asan.so")
 SANITIZE_FLAGS = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
                   "-Xarch_host", "-fno-sanitize-recover=undefined",
@@ -86,21 +89,20 @@ def build(verbose: bool = False, sanitize: bool = False) -> str:
 
 
 def build_binding(verbose: bool = False):
-    """_tensor_address.so, or None where torch or g++ is missing (libpkv.so needs neither)."""
-    import sysconfig
-
+    """The module _tensor_address, or None where torch or g++ is missing (libpkv.so needs neither)."""
     try:
+        import torch
         from torch.utils.cpp_extension import include_paths, library_paths
     except ImportError:
-        print("_tensor_address.so is not built: torch cannot be imported", file=sys.stderr)
+        print("_tensor_address is not built: torch cannot be imported", file=sys.stderr)
         return None
     if shutil.which("g++") is None:
-        print("_tensor_address.so is not built: g++ not found", file=sys.stderr)
+        print("_tensor_address is not built: g++ not found", file=sys.stderr)
         return None
     tmp = BINDING + ".tmp"
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-o", tmp,
-           os.path.join(CSRC, "tensor_address.cpp"), "-isystem",
-           sysconfig.get_paths()["include"]]
+           os.path.join(CSRC, "tensor_address.cpp"), f'-DTORCH_VERSION_BUILT="{torch.__version__}"',
+           "-isystem", sysconfig.get_paths()["include"]]
     for d in include_paths():
         cmd += ["-isystem", d]
     for d in library_paths():
@@ -111,7 +113,7 @@ def build_binding(verbose: bool = False):
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         sys.stderr.write(res.stdout + res.stderr)
-        raise RuntimeError("g++ failed building _tensor_address.so")
+        raise RuntimeError("g++ failed building _tensor_address")
     os.replace(tmp, BINDING)
     return BINDING
 

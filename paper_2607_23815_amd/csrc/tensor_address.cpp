@@ -1,4 +1,5 @@
-// A Python module of two functions that the binding asks of every tensor of a call:
+// A Python module of two functions that the binding asks of every tensor of a call, and torch_version, the
+// version it was built against (a tensor's layout is that version's):
 //   address(tensor, dtype, device): the device address of a contiguous tensor of this dtype on GPU
 //     `device`;
 //   rows_address(tensor, dtype, device, rows, heads, dim): (address, row stride in elements) of such a
@@ -74,4 +75,11 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensor_address", nullptr, -1, met
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__tensor_address(void) { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__tensor_address(void) {
+  PyObject* m = PyModule_Create(&module);
+  if (m != nullptr && PyModule_AddStringConstant(m, "torch_version", TORCH_VERSION_BUILT) != 0) {
+    Py_DECREF(m);
+    return nullptr;
+  }
+  return m;
+}

@@ -475,18 +475,42 @@ def _stream(stream):
     return torch.cuda.current_stream().cuda_stream
 
 
+def _find_address():
+    """The functions that look at a call's tensors: native ones, or these where the module is not built for
+    this interpreter and this torch."""
+    global _address, _rows_address
+    torch = _get_torch()
+    try:
+        from . import _tensor_address as native
+        if getattr(native, "torch_version", None) == torch.__version__:
+            _address, _rows_address = native.address, native.rows_address
+            return
+    except ImportError:
+        pass
+
+    def on(t, dtype, dev):
+        return (isinstance(t, _Tensor) and t.dtype is dtype and t.is_cuda
+                and t.layout is torch.strided and t.get_device() == dev)
+
+    def address(t, dtype, dev):
+        return t.data_ptr() if on(t, dtype, dev) and t.is_contiguous() else None
+
+    def rows_address(t, dtype, dev, rows, heads, dim):
+        if not on(t, dtype, dev) or t.shape != (rows, heads, dim):
+            return None
+        row, head, step = t.stride()
+        if step != 1 or (heads > 1 and head != dim):
+            return None
+        return t.data_ptr(), row if rows > 1 else heads * dim
+
+    _address, _rows_address = address, rows_address
+
+
 def _launch_on(stream):
     """The current device's index, which a call launches on, and the hipStream_t (the current
     stream's, or that of an explicit one, which must be of this device)."""
-    global _address, _rows_address
     if _address is None:
-        _get_torch()
-        try:
-            from . import _tensor_address
-        except ImportError as e:
-            raise ImportError("_tensor_address.so is missing or does not fit this torch: build it "
-                              "with `python -m paper_2607_23815_amd.build`") from e
-        _address, _rows_address = _tensor_address.address, _tensor_address.rows_address
+        _find_address()
     dev = _get_device()
     if stream is None:
         return dev, _raw_stream(dev) if _raw_stream is not None else _stream(None)
