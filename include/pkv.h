@@ -39,7 +39,7 @@
  *     PKV_DEBUG_VALIDATE set in the environment (any value but "0"), or after
  *     pkv_set_debug_validate(1), every device call first runs a validation kernel over its
  *     metadata, waits for the stream, and returns PKV_ERR_BAD_METADATA (launching nothing
- *     else) naming what failed and the first offending sequence. This synchronises every
+ *     else) naming what failed and the first offending sequence or row. This synchronises every
  *     call: a debugging aid, not for graph capture or timed runs.
  *   - Interface choices: the block pool is host bookkeeping only (it takes the order in which
  *     blocks are handed out, not device pointers or a seed; the caller allocates the K/V
@@ -417,7 +417,7 @@ pkv_status pkv_extend_tables(int32_t* block_tables, int32_t max_blocks,
  * included), products and sums are 32-bit, each output is rounded once to bf16.
  * positions: int32 [num_axes][rows], an axis every pos_stride elements. slot_map: int64 [rows],
  * block * block_size + slot as pkv_extend_tables writes it; a row whose slot is outside the pool
- * (-1: padding) is skipped, in q_out too. Slots must be distinct and their blocks private to
+ * (-1: padding; PKV_DEBUG_VALIDATE refuses any other) is skipped, in q_out too. Slots must be distinct and their blocks private to
  * their sequences. No other byte of the pool changes. q_out: bf16 [rows][num_q_heads][head_dim]
  * with its own row stride; it may be q itself (same address and stride). Addresses are 16-byte
  * aligned, row strides of q, k_new, v_new and q_out multiples of 8 elements that hold a row.
@@ -457,7 +457,9 @@ pkv_status pkv_block_bounds(const pkv_paged_kv* kv, void* bounds, const int32_t*
  * [rows]; NULL: row t is sequence t, rows == num_seqs, a decode step) and sees that sequence's
  * first row_lens[t] keys (int32 [rows]). A decode step passes seq_lens; rows of longer suffixes
  * take both arrays from pkv_extend_tables. A row whose row_seq is -1 is padding: nothing of it is
- * written. num_q_heads / num_kv_heads <= 16; rows * num_kv_heads < 2^22.
+ * written. (PKV_DEBUG_VALIDATE refuses other row_seq outside the sequences and negative row_lens; for
+ * the choice also row_lens above max_len, which is cut otherwise, and ids outside the pool, for
+ * which block 0's bounds stand in otherwise.) num_q_heads / num_kv_heads <= 16; rows * num_kv_heads < 2^22.
  *
  * Choice of blocks: for each row and kv head, the `blocks` of the row's
  * ceil(row_lens[t] / block_size) blocks that matter most, by the most that any key within a
@@ -495,11 +497,11 @@ size_t pkv_select_workspace_bytes(int32_t rows, int32_t num_q_heads, int32_t num
  * order. Every block of a row listed, the result is pkv_decode_attention's up to the order of
  * its sums and the rounding of its weights, infinite values included. A row without a visible key
  * (row_lens[t] 0, nothing listed), or whose scores are all -infinity, gives zeros and an LSE of
- * -infinity. bf16 inputs, 32-bit sums, bf16 output; weights reach the value product with 16 bits or more (2^-16 of themselves; rounded
- * to bf16, as in decode, where values that are not finite are met). At most 65536 blocks are
- * chosen for a row; row_lens has no such limit. workspace: at least pkv_sparse_workspace_bytes (0 where there are rows
- * enough to fill the chip), 16-byte aligned, owned by the caller, not read back; calls that
- * share one must not overlap. */
+ * -infinity. bf16 inputs, 32-bit sums, bf16 output; weights reach the value product within 2^-16
+ * of themselves (rounded to bf16, as in decode, where sums are not finite). At most 65536 blocks
+ * are chosen for a row; row_lens has no such limit. workspace: at least
+ * pkv_sparse_workspace_bytes (0 where there are rows enough to fill the chip), 16-byte aligned,
+ * owned by the caller, not read back; calls that share one must not overlap. */
 pkv_status pkv_sparse_attention(const pkv_paged_kv* kv, const void* q, int32_t num_q_heads,
                                 const int32_t* block_tables, int32_t max_blocks,
                                 int32_t num_seqs, const int32_t* row_seq,

@@ -734,8 +734,8 @@ pkv_status pkv_sparse_attention(const pkv_paged_kv* kv, const void* q, int32_t n
                     "(see pkv_sparse_workspace_bytes)");
   const hipStream_t s = static_cast<hipStream_t>(stream);
   {
-    MetaCheck c = meta(kMetaRows, view, block_tables, max_blocks, row_lens, nullptr, rows, -1,
-                       (int64_t)max_blocks * kSupportedBlockSize, 0);
+    // (lengths past the table and entries outside the pool are in order here)
+    MetaCheck c = meta(kMetaRows, view, nullptr, 0, row_lens, nullptr, rows, -1, INT32_MAX, 0);
     c.row_seq = row_seq;
     c.table_rows = num_seqs;
     if ((st = check_metadata(fn, &c, 1, s)) != PKV_OK) return st;

@@ -213,7 +213,8 @@ struct MetaCheck {
   int64_t max_total;
   const int64_t* slots;  // kMetaSlots: [num_seqs] rows' slots, each -1 or within the pool
   const int32_t* row_seq;  // kMetaRows: [num_seqs] rows' sequences, each -1 or below table_rows
-  int32_t table_rows;      // (null: row i is sequence i), lens their visible keys (0 .. max_len)
+  int32_t table_rows;      // (null: row i is sequence i), lens their visible keys (0 .. max_len);
+                           // tables null: their entries are not looked at
 };
 // Runs the checks in order on `stream` and waits for each; *bad = the failed check's bits
 // (0 if all pass), *first_seq its lowest offending sequence, *which its index.

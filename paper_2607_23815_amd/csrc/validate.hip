@@ -45,7 +45,7 @@ __global__ __launch_bounds__(kThreads) void validate_kernel(MetaCheck c, uint32_
     if (c.row_seq != nullptr) seq = c.row_seq[i];
     const int64_t len = c.lens[i];
     if (seq < -1 || seq >= c.table_rows || len < 0 || len > c.max_len) bad |= kMetaBadLength;
-    if (!bad && seq >= 0) e1 = (len + 15) / 16;
+    if (!bad && seq >= 0 && c.tables != nullptr) e1 = (len + 15) / 16;
   } else if (c.mode == kMetaDecode) {
     const int64_t len = c.lens[i];
     if (len < 1 || len > c.max_len) bad |= kMetaBadLength;

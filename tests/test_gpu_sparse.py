@@ -404,3 +404,32 @@ def test_values_near_the_largest(gpu_lib, hq, hkv, d):
     lib.pkv_decode_attention(to_dev_bits(pk), to_dev_bits(pv), to_dev_bits(q), i32(tables), i32(lens), 75,
                              math.log(2), out)
     check((to_host_bits(out), None), *args)
+
+
+def test_validation_takes_what_the_call_passes_over(gpu_lib):
+    """Table entries outside the pool and lengths past the table are in order; rows of no sequence and
+    negative lengths are not."""
+    lib = gpu_lib
+    rng = np.random.default_rng(15)
+    tables, pk, pv = pools(rng, [500, 80], 2, 64)
+    tables = tables[:, :31].copy()
+    tables[0, 3], tables[0, 7] = -1, len(pk)
+    q = rand_bf16(rng, (4, 4, 64))
+    seen, seq = np.array([500, 2**31 - 1, 0, 64]), np.array([0, 0, -1, 1])
+    sel = lists(rng, [496, 496, 496, 64], 2, 32, "any")
+    args = (tables, pk, pv, q, seen, sel, 0.1, seq)
+    pk[tables[0, 30], :, :, 4:] = 0  # (slots that the second row sees)
+    pv[tables[0, 30], :, :, 4:] = 0
+    off = run(lib, *args)
+    check(off, *args)
+    lib.pkv_set_debug_validate(True)
+    try:
+        on = run(lib, *args)
+        assert all(np.array_equal(a, b) for a, b in zip(off, on))
+        for bad_seen, bad_seq, row in (([500, -1, 0, 64], [0, 0, -1, 1], 1),
+                                       ([500, 9, 0, 64], [0, 0, -2, 1], 2),
+                                       ([500, 9, 0, 64], [0, 0, 0, 2], 3)):
+            with pytest.raises(lib.PkvError, match=f"first offending row {row}"):
+                run(lib, tables, pk, pv, q, np.array(bad_seen), sel, 0.1, np.array(bad_seq))
+    finally:
+        lib.pkv_set_debug_validate(False)
