@@ -433,3 +433,33 @@ def test_validation_takes_what_the_call_passes_over(gpu_lib):
                 run(lib, tables, pk, pv, q, np.array(bad_seen), sel, 0.1, np.array(bad_seq))
     finally:
         lib.pkv_set_debug_validate(False)
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(4, 1, 64), (6, 3, 64), (16, 1, 128)])
+@pytest.mark.parametrize("n,blocks", [(16 * 1100, 1040), (16 * 2100 - 7, 1360), (16 * 4096, 2048),
+                                      (16 * 4096, 4096), (16 * 1500, 65536)])
+def test_long_lists_of_one_row(gpu_lib, hq, hkv, d, n, blocks):
+    """Few rows with more than 1024 blocks: as many splits as the merge has lanes."""
+    rng = np.random.default_rng(n + d)
+    pool = pools(rng, [n], hkv, d)
+    q = rand_bf16(rng, (1, hq, d))
+    for how in ("ascending", "any"):
+        args = (*pool, q, np.array([n]), lists(rng, [n], hkv, blocks, how), d ** -0.5)
+        got = run(gpu_lib, *args)
+        check(got, *args)
+        row_seq = run(gpu_lib, *args, np.array([0]))
+        assert all(np.array_equal(a, b) for a, b in zip(got, row_seq)), "with row_seq"
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(4, 1, 64), (32, 8, 128), (28, 4, 128), (6, 3, 64)])
+def test_splits_of_rows_that_share_a_sequence(gpu_lib, hq, hkv, d):
+    """Few rows of longer suffixes with long lists: several workgroups an item, in the XCDs' order."""
+    rng = np.random.default_rng(hq)
+    lens = [3000, 900]
+    pool = pools(rng, lens, hkv, d)
+    seq = np.array([0, 0, -1, 0, 1])
+    seen = np.array([2998, 2999, 50, 3000, 900])
+    q = rand_bf16(rng, (5, hq, d))
+    args = (*pool, q, seen, lists(rng, seen, hkv, 180, "any"), d ** -0.5, seq)
+    assert gpu_lib.pkv_sparse_workspace_bytes(5, hq, hkv, d, 180) > 0
+    check(run(gpu_lib, *args), *args)
