@@ -735,7 +735,9 @@ def rope_spec(inv_freq, axis_of=None, interleaved=False, scale=1.0, num_axes=Non
         raise ValueError("inv_freq and axis_of must have the same length, at most 64")
     if axes and not (min(axes) >= 0 and max(axes) < PKV_ROPE_MAX_AXES):
         raise ValueError(f"axis_of must name axes 0 to {PKV_ROPE_MAX_AXES - 1}")
-    r = Rope(2 * len(freqs), num_axes or max(axes, default=0) + 1, int(bool(interleaved)), float(scale))
+    if num_axes is None:
+        num_axes = max(axes, default=0) + 1
+    r = Rope(2 * len(freqs), int(num_axes), int(bool(interleaved)), float(scale))
     r.axis_of[:len(axes)] = axes
     r.inv_freq[:len(freqs)] = freqs
     return r

@@ -176,3 +176,10 @@ def test_tensor_address_takes_gpu_tensors_only():
                        (m.rows_address, (t, t.dtype, 0)), (m.rows_address, (t, t.dtype, 0, 2, "3", 4))):
         with pytest.raises(TypeError):
             call(*args)
+
+
+def test_rope_spec_takes_no_number_of_axes_for_none(lib):
+    assert lib.rope_spec([1.0] * 8, axis_of=[0, 2] * 4).num_axes == 3
+    for n in (0, -1):
+        refused(lib, lib.PKV_ERR_INVALID_ARG, _rope(lib, rope=lib.rope_spec([1.0] * 8, num_axes=n)),
+                "num_axes")
