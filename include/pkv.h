@@ -413,8 +413,9 @@ pkv_status pkv_extend_tables(int32_t* block_tables, int32_t max_blocks,
  *   y[a] = scale * (x[a] cos phi - x[b] sin phi),  y[b] = scale * (x[b] cos phi + x[a] sin phi),
  * (a, b) = (j, j + rot_dim / 2), or (2 j, 2 j + 1) where interleaved; dims from rot_dim on are
  * copied. Text has one axis; images and video have three (time, height, width), each turning
- * its own pairs. Angles are reduced in 64 bits (positions of any size, negative ones
- * included), products and sums are 32-bit, each output is rounded once to bf16.
+ * its own pairs. Angles are reduced in 64 bits (positions of any size, negative ones included:
+ * an angle is off by 2^-51 of itself, 2^-20 at 2^31 radians), products and sums are 32-bit, each
+ * output is rounded once to bf16.
  * positions: int32 [num_axes][rows], an axis every pos_stride elements. slot_map: int64 [rows],
  * block * block_size + slot as pkv_extend_tables writes it; a row whose slot is outside the pool
  * (-1: padding; PKV_DEBUG_VALIDATE refuses any other) is skipped, in q_out too. Slots must be distinct and their blocks private to
@@ -429,7 +430,7 @@ typedef struct {
   int32_t interleaved;  /* 0: dim j pairs with j + rot_dim / 2; 1: neighbours pair */
   float scale;          /* factor of the turned dims (1: none), finite */
   uint8_t axis_of[64];  /* [rot_dim / 2], each below num_axes */
-  double inv_freq[64];  /* [rot_dim / 2], radians per position, finite */
+  double inv_freq[64];  /* [rot_dim / 2], radians per position, at most 2^20 either way */
 } pkv_rope;
 pkv_status pkv_rope_append(const pkv_paged_kv* kv, const pkv_rope* rope, const void* q,
                            int64_t q_stride, int32_t num_q_heads, const void* k_new,

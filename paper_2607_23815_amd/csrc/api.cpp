@@ -541,8 +541,8 @@ pkv_status pkv_rope_append(const pkv_paged_kv* kv, const pkv_rope* rope, const v
   for (int j = 0; j < rope->rot_dim / 2; ++j) {
     if (rope->axis_of[j] >= rope->num_axes)
       return fail(PKV_ERR_INVALID_ARG, f + ": axis_of names an axis past num_axes");
-    if (!std::isfinite(rope->inv_freq[j]))
-      return fail(PKV_ERR_INVALID_ARG, f + ": inv_freq is not finite");
+    if (!(std::fabs(rope->inv_freq[j]) <= 0x1p20))  // (an angle of 2^51 has no fraction left)
+      return fail(PKV_ERR_INVALID_ARG, f + ": inv_freq is not finite, or above 2^20");
   }
   if (rows < 0) return fail(PKV_ERR_INVALID_ARG, f + ": negative size");
   if (rows == 0) return ok();

@@ -183,3 +183,11 @@ def test_rope_spec_takes_no_number_of_axes_for_none(lib):
     for n in (0, -1):
         refused(lib, lib.PKV_ERR_INVALID_ARG, _rope(lib, rope=lib.rope_spec([1.0] * 8, num_axes=n)),
                 "num_axes")
+
+
+def test_rope_append_refuses_frequencies_without_a_fraction(lib):
+    """Angles past the fractions of 64 bits, or past their range (NaN), are refused."""
+    for f in (1e300, -1e300, 2.0**20 * 1.001):
+        refused(lib, lib.PKV_ERR_INVALID_ARG, _rope(lib, rope=lib.rope_spec([1.0] * 7 + [f])),
+                "inv_freq")
+    assert _rope(lib, rope=lib.rope_spec([-2.0**20, 2.0**20] * 4), rows=0) == lib.PKV_OK
