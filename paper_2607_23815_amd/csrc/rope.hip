@@ -12,15 +12,18 @@
 // They are found once per (row, pair) of a workgroup and serve all its heads.
 //
 // Bound by memory (every row read once and written once). A workgroup takes a window of consecutive rows
-// and a kv head with its query heads at a time; a head's loads all go out at once, the first head's
-// before the angles are found, so that a window waits once and not once per part. V's slab holds 8
+// and a kv head with its query heads at a time; its first kBatch * kThreads units' loads go out at once,
+// before the angles are found. These are all of a window's with halves of 128 dims and up to 5 query heads
+// a kv head, which then waits once and not once per part; more heads, and neighbours and partial rotation
+// from 3 on (twice the units), load the others behind the first ones' stores. V's slab holds 8
 // tokens of one dim in 16 bytes, so a run of rows that fills a half-slab is written whole by the
 // workgroup in whose window it begins (it looks up to 7 rows past the window's end); rows of a
 // half-slab only partly covered are written in 2-byte pieces, which need no read and cannot race
 // with another workgroup's. 16-byte stores go past the caches, and a window's heads are neighbouring
 // workgroups, so that its rows are read whole at about the same time. 16k rows of 32/8 heads of 128 dims:
-// 88.8 us, 4.5 TB/s; 64/8 heads 134.9 us, 4.9 TB/s, the rate of a large copy (windows side by side instead
-// of heads 104.6 and 173.6, then with ordinary stores 108.9 and 175.3).
+// 86.8 us, 4.5 TB/s; 64/8 heads 133.0 us, 5.0 TB/s, the rate of a large copy (windows side by side instead
+// of heads 104.6 and 173.6, then with ordinary stores 108.9 and 175.3). Neighbours 97.4 and 149.6; the
+// first 64 dims turned 103.8 and 164.6.
 #include "device_utils.h"
 #include "launch.h"
 

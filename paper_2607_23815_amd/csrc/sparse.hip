@@ -509,8 +509,9 @@ hipError_t launch_sparse_attention(SparseArgs a, int head_dim, void* workspace,
   const SparseCut c = sparse_cut(items, a.blocks);
   // Rows of longer suffixes share their sequences' keys: each XCD takes a run of rows of one kv head
   // after the other, so that its L2 holds few heads' keys at a time (1525 rows of five sequences, 63
-  // blocks each: 20/5 heads 160 us against 362 with items in order, 16/16 555 and 738, 32/8 248 and
-  // 269, 16/4 of 64 dims 69.4 and 70.2).
+  // random blocks each, inputs changing: 20/5 heads 173 us against 346 with items in order, 16/16 532 and
+  // 678, 16/4 of 64 dims 65.8 and 67.3; with 8 kv heads an order of items gives each XCD one head as
+  // well: 32/8 259 both ways).
   a.xcd_items = a.row_seq != nullptr ? (items + kXcds - 1) / kXcds : 0;
   a.splits = c.splits;
   a.split_entries = c.split_entries;

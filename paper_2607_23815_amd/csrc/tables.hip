@@ -7,8 +7,9 @@
 //   table[i][p / 16] * 16 + p % 16.
 // Nothing here is bound by bytes (20 per row): the time is the launch and the chain of dependent
 // steps, so one workgroup does it all (lengths, two scans, table entries, rows) where the rows
-// are few; many rows go to a second launch that reads the tables and offsets that the first
-// wrote. Searches take a fixed number of steps, four of a thread's at a time. The checks come before
+// are few; many rows go to a second launch of many workgroups, which reads the tables and offsets that
+// the first wrote (the data do not force it: a new block's id stands in free_blocks, but each
+// workgroup would scan the lengths for itself, and seq_lens may be cached_lens). Searches take a fixed number of steps, four of a thread's at a time. The checks come before
 // the first write, so a refused step changes nothing but its status.
 #include <limits.h>
 
