@@ -121,7 +121,7 @@ __device__ __forceinline__ void lds_load16(const void* base, int bytes, int voff
 #endif
 }
 
-// 16-, 4- and 8-byte loads through a buffer resource: wave-uniform `base` (kept in scalar
+// 16- and 8-byte loads through a buffer resource: wave-uniform `base` (kept in scalar
 // registers) plus a 32-bit per-lane byte offset, so a load needs one address register
 // instead of two. Offsets at or past `bytes` read zero.
 __device__ __forceinline__ u32x4 buf_ld16(const void* base, int bytes, int voffset) {
@@ -131,15 +131,6 @@ __device__ __forceinline__ u32x4 buf_ld16(const void* base, int bytes, int voffs
   return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, voffset, 0, 0));
 #else
   return u32x4{0u, 0u, 0u, 0u};
-#endif
-}
-__device__ __forceinline__ uint32_t buf_ld4(const void* base, int bytes, int voffset) {
-#if __HIP_DEVICE_COMPILE__
-  const __amdgpu_buffer_rsrc_t rsrc =
-      __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, kBufferFlags);
-  return __builtin_amdgcn_raw_buffer_load_b32(rsrc, voffset, 0, 0);
-#else
-  return 0u;
 #endif
 }
 __device__ __forceinline__ u32x2 buf_ld8(const void* base, int bytes, int voffset) {

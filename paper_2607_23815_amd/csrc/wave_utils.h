@@ -1,5 +1,5 @@
 // Exchanges between the lanes of a wave without LDS: data-parallel moves within rows of 16 lanes, and
-// swaps of rows and halves.
+// swaps of rows and halves. And a load of 4 bytes.
 #pragma once
 
 #include "device_utils.h"
@@ -61,6 +61,17 @@ struct Add {
   __device__ int operator()(int x, int y) const { return x + y; }
   __device__ float operator()(float x, float y) const { return x + y; }
 };
+
+// A 4-byte load through a buffer resource (as buf_ld16): zero at or past `bytes`.
+__device__ __forceinline__ uint32_t buf_ld4(const void* base, int bytes, int voffset) {
+#if __HIP_DEVICE_COMPILE__
+  const __amdgpu_buffer_rsrc_t rsrc =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, kBufferFlags);
+  return __builtin_amdgcn_raw_buffer_load_b32(rsrc, voffset, 0, 0);
+#else
+  return 0u;
+#endif
+}
 
 // The sum over the lanes up to this one: within 16 lanes, then over the rows before.
 __device__ __forceinline__ int wave_scan(int v) {

@@ -23,3 +23,11 @@ def test_a_multi_rank_launch_is_refused():
     r = _run(env=env)
     assert r.returncode == 2
     assert "one GPU" in r.stderr and r.stdout == ""
+
+
+def test_the_committed_traffic_is_of_these_kernels():
+    """The bytes that the benchmark reports come from counters of the kernels' present sources: files
+    that several kernels share do not change for one that is not among them."""
+    import bench
+    for kernel in bench.KERNEL_SOURCES:
+        assert bench.traffic_from_profiles(kernel), kernel
