@@ -375,7 +375,9 @@ pkv_status pkv_mixed_attention(const pkv_paged_kv* kv, int32_t num_q_heads, floa
  * sequence 0 first; block_tables (int32 [num_seqs][max_blocks]) receives their ids after the
  * ceil(cached_lens[i] / block_size) entries that the row holds already, which stay. The blocks
  * are the ones pkv_seq_reserve would take from such a free list. Blocks that a cached prefix
- * shares are not looked at: a new token goes into a partly filled last block as it is.
+ * shares are not looked at: a new token goes into a partly filled last block as it is. So a
+ * sequence whose last block others hold too is given a copy of its own before the loop
+ * (pkv_seq_reserve_cow and pkv_copy_blocks); the blocks that it takes here are its own.
  *   cu_new_lens [num_seqs + 1], seq_lens [num_seqs]: the new tokens' offsets, and
  *     cached_lens + new_lens. *free_used_out: *free_used plus the blocks taken.
  *   For each new token, in the rows cu_new_lens[i] .. of these arrays of max_rows entries (each
@@ -387,9 +389,8 @@ pkv_status pkv_mixed_attention(const pkv_paged_kv* kv, int32_t num_q_heads, floa
  *     and every row is padding.
  * seq_lens may be cached_lens and free_used_out may be free_used (a loop's step then leaves
  * the next one's input; pkv_block_bounds still needs the old lengths); no other arrays may
- * overlap. max_rows <= 2^30. Zero sequences write an
- * empty step. All arrays are device memory. (PKV_DEBUG_VALIDATE adds nothing here: *status says
- * what a step was refused for.) */
+ * overlap. max_rows <= 2^30. Zero sequences write an empty step. All arrays are device memory.
+ * (PKV_DEBUG_VALIDATE adds nothing here: *status says what a step was refused for.) */
 enum {
   PKV_EXTEND_OUT_OF_BLOCKS = 1,  /* *free_used is negative, or too few blocks are behind it */
   PKV_EXTEND_TABLE_FULL = 2,     /* a sequence needs more than max_blocks blocks */
