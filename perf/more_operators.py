@@ -10,9 +10,9 @@ codes, key scales, value codes, value scales. With codes of e4m3 (8 bits, larges
     125 for 4, where codes saturate), a code stands for x 2^-e rounded to nearest even, the scale byte is
     e + 127. Below max|x| = 2^-100 the codes are 0 and the byte 127; where a value is not finite the codes
     are 0 and the byte is 255, which makes all 32 NaN.
-  * values, per token: s is the least number of 4 significant bits that is not below max|x| / M, kept as a
-    float, a code stands for x / s rounded to nearest even. Below 2^-100: codes 0 and s = 1; not finite:
-    codes 0 and s = NaN.
+  * values, per token: s is the least number of 4 significant bits that is not below max|x| / M (at most
+    1.125 2^119 for 8 bits and 1.25 2^125 for 4, where codes saturate), kept as a float, a code stands for
+    x / s rounded to nearest even. Below 2^-100: codes 0 and s = 1; not finite: codes 0 and s = NaN.
   * key codes are [dims in units of 16 bytes][16 slots][unit], key scales [16 slots][dims / 32], value
     codes [planes][4 quarters][16][dims / 16 / planes][4 slots of the quarter] where dim 16 a + b of slot
     4 q + j is entry b of quarter q, a, j (two planes with 8 bits and 128 dims, otherwise one), value scales
@@ -35,6 +35,7 @@ own = False
 BS = 16  # tokens per block
 MOST = {8: 448.0, 4: 6.0}  # the largest value of a code
 TOP = {8: 119, 4: 125}     # the largest exponent of a key scale
+TOP_VALUE = {8: 1.125 * 2.0 ** 119, 4: 1.25 * 2.0 ** 125}  # the largest value scale
 
 
 # ----------------------------------------------------------------------------------------
@@ -419,7 +420,9 @@ def _quantised_values(x, bits):
     live = (top >= 2.0 ** -100) & torch.isfinite(top)
     s = torch.where(live, top.double() / MOST[bits], 1.0).float()
     s = ((s.view(torch.int32) + 0xFFFFF) & -0x100000).view(torch.float32)  # up to 4 significant bits
-    codes = torch.where(live, _rounded(torch.where(live, x.double() / s, 0.0).float(), bits), 0)
+    s = s.clamp(max=TOP_VALUE[bits])
+    y = torch.where(live, x.double() / s, 0.0).clamp(-MOST[bits], MOST[bits]).float()
+    codes = torch.where(live, _rounded(y, bits), 0)
     return codes, torch.where(torch.isfinite(top), s, float("nan")).squeeze(-1)
 
 
@@ -579,7 +582,8 @@ def _exact_key_code(x, bits):
     for _ in range(10):
         e = torch.where(MOST[bits] * _exact_power(e - 1) >= top, e - 1, e)
     e = torch.where(held, e.clamp(max=TOP[bits]), 0)
-    code = _nearest(torch.where(held[:, None], x * _exact_power(-e)[:, None], 0.0), bits)
+    y = torch.where(held[:, None], x * _exact_power(-e)[:, None], 0.0).clamp(-MOST[bits], MOST[bits])
+    code = _nearest(y, bits)
     return torch.where(held[:, None], code, 0), torch.where(fine, e + 127, 255)
 
 
@@ -592,7 +596,9 @@ def _exact_value_code(x, bits):
     step = _exact_power(exp - 4)
     s = torch.ceil(frac * 16) * step
     s = torch.where((s - step) * MOST[bits] >= top, s - step, s)  # (the quotient was rounded up past s)
-    code = torch.where(held[:, None], _nearest(torch.where(held[:, None], x, 0.0) / s[:, None], bits), 0)
+    s = s.clamp(max=TOP_VALUE[bits])
+    y = (torch.where(held[:, None], x, 0.0) / s[:, None]).clamp(-MOST[bits], MOST[bits])
+    code = torch.where(held[:, None], _nearest(y, bits), 0)
     return code, torch.where(fine, torch.where(held, s, 1.0), float("nan"))
 
 
