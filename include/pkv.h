@@ -8,7 +8,8 @@
  *   - decode, one new token per sequence attending over the whole cached context.
  * Beside the two stand the calls of a step that reads a long cache sparsely, without the host in
  * between: tables grown on the GPU, rotary positions with the append, key bounds per block, the
- * choice of blocks by these bounds, and attention over the chosen ones.
+ * choice of blocks by these bounds, and attention over the chosen ones. A second pool holds keys and
+ * values in 8 or 4 bits, with its own append, block conversions, decode and prefill.
  * This is the KV-cache reuse that pipelining semantic operators relies on: the filter -> map
  * example of Section 2.1 ("Prefix sharing in semantic operators") has prompts
  * [S | C(t) | I_filter] and [S | C(t) | I_map] whose shared prefix [S | C(t)] is cached once
@@ -512,6 +513,88 @@ pkv_status pkv_sparse_attention(const pkv_paged_kv* kv, const void* q, int32_t n
                                 void* workspace, size_t workspace_bytes, void* stream);
 size_t pkv_sparse_workspace_bytes(int32_t rows, int32_t num_q_heads, int32_t num_kv_heads,
                                   int32_t head_dim, int32_t blocks);
+
+/* A cache held in 8 or 4 bits: a second pool beside the bf16 one, addressed by the same kind of block
+ * tables. cache: uint8 [num_blocks][num_kv_heads][slab], caller-allocated and 16-byte aligned,
+ * pkv_quant_block_bytes a block; a block's bytes are contiguous, so a copy (for a block that several
+ * sequences hold) is a copy of bytes. A slab holds 16 tokens for one kv head: key codes, key scales,
+ * value codes, value scales. Codes are e4m3 (bits 8, the largest M = 448) or e2m1 (bits 4, M = 6; of two in
+ * a byte the first in its low half):
+ *   - keys, per token and 32 dims: with e the least integer for which max |x| <= M 2^e (at most 119 for 8
+ *     bits and 125 for 4, where codes saturate), the code is x 2^-e rounded to nearest even and the scale
+ *     byte e + 127;
+ *   - values, per token: with s the least number of 4 significant bits that is not below max |x| / M
+ *     (at most 1.125 2^119 for 8 bits and 1.25 2^125 for 4, where codes saturate), the code is x / s
+ *     rounded to nearest even and the scale the float s.
+ * What a code stands for, key code x 2^e or value code x s, is exact in bf16. Where max |x| is below 2^-100
+ * the codes are 0 (and the scale 1); where an x is not finite all of them read back as NaN (codes 0,
+ * scale byte 255, or s NaN).
+ *   key codes   [head_dim * bits / 128 units][16 slots][16 bytes]    a unit: consecutive dims of a slot
+ *   key scales  [16 slots][head_dim / 32] bytes
+ *   value codes [planes][4 quarters q][16 b][head_dim / 16 / planes, a][4 j]   dim 16 a + b of slot 4 q + j
+ *               (two planes, the first and second half of a, for head_dim 128 with 8 bits; otherwise one)
+ *   value scales [16 slots] float
+ * head_dim 128: 136 bytes a token and kv head with 4 bits and 264 with 8, against 512 in bf16. */
+typedef struct {
+  void* cache;
+  int32_t num_blocks;
+  int32_t block_size;   /* 16 */
+  int32_t num_kv_heads;
+  int32_t head_dim;     /* 64 or 128 */
+  int32_t bits;         /* 4 or 8 */
+} pkv_quant_kv;
+/* Bytes of a block (all kv heads); 0 for a head_dim or bits that are not supported. */
+size_t pkv_quant_block_bytes(int32_t num_kv_heads, int32_t head_dim, int32_t bits);
+
+/* Append to the quantised cache: new tokens' keys and values are quantised on their way. Metadata and
+ * ownership as pkv_kv_append; row r of k_new (v_new), bf16 [num_kv_heads][head_dim], begins r * k_stride
+ * (v_stride) elements behind the first (e.g. the parts of one fused projection's rows), strides being
+ * multiples of 8 that hold a row, addresses 16-byte aligned. A row past total_new is taken for zeros. Slots
+ * other than the new tokens' keep their codes and scales. */
+pkv_status pkv_quant_append(const pkv_quant_kv* kv, const void* k_new, int64_t k_stride,
+                            const void* v_new, int64_t v_stride, const int32_t* block_tables,
+                            int32_t max_blocks, const int32_t* cached_lens,
+                            const int32_t* cu_new_lens, int32_t num_seqs, int32_t total_new,
+                            int32_t max_new_len, void* stream);
+
+/* Whole blocks from the bf16 pool into the quantised one, and back: a cached prefix is parked in a
+ * fraction of its memory, and restored for the calls that read the bf16 pool. For each k < num_pairs all
+ * 16 slots of block pairs[2k] of `from`, for every kv head, go to block pairs[2k+1] of `to` (pairs: int32
+ * device memory [num_pairs][2]). Slots that hold no token are converted like the others. The blocks
+ * written must differ from one another; a pair naming a block outside either pool is skipped. Both pools
+ * have the same num_kv_heads and head_dim. num_pairs * num_kv_heads stays below 2^26. */
+pkv_status pkv_quant_blocks(const pkv_paged_kv* from, const pkv_quant_kv* to, const int32_t* pairs,
+                            int32_t num_pairs, void* stream);
+pkv_status pkv_dequant_blocks(const pkv_quant_kv* from, const pkv_paged_kv* to, const int32_t* pairs,
+                              int32_t num_pairs, void* stream);
+
+/* Decode attention over the quantised cache: pkv_decode_attention on what its codes stand for, with its
+ * arguments, a length above max_seq_len being cut to it. Here a length may be 0 (a padding sequence): its
+ * output is zeros and its LSE -infinity, as for a row whose scores are all -infinity. 32-bit sums;
+ * weights reach the value product within 2^-16 of themselves; bf16 output. A key or value that reads
+ * back as NaN makes NaN of the heads that see it. workspace: at least pkv_quant_decode_workspace_bytes (0
+ * where there are items enough to fill the chip), 16-byte aligned, owned by the caller, not read
+ * back; calls that share one must not overlap. num_seqs * num_kv_heads stays below 2^22. */
+pkv_status pkv_quant_decode_attention(const pkv_quant_kv* kv, const void* q, int32_t num_q_heads,
+                                      const int32_t* block_tables, int32_t max_blocks,
+                                      const int32_t* seq_lens, int32_t num_seqs,
+                                      int32_t max_seq_len, float scale, void* out, float* lse,
+                                      void* workspace, size_t workspace_bytes, void* stream);
+size_t pkv_quant_decode_workspace_bytes(int32_t num_seqs, int32_t num_q_heads, int32_t num_kv_heads,
+                                        int32_t head_dim, int32_t bits, int32_t max_seq_len);
+
+/* Prefix-reuse prefill attention over the quantised cache, the new tokens appended before: with
+ * pkv_prefill_attention's arguments, optional workspace and plan, and its results on a bf16 pool that holds
+ * what the codes stand for (pkv_dequant_blocks), bit for bit. */
+pkv_status pkv_quant_prefill_attention(const pkv_quant_kv* kv, const void* q, int32_t num_q_heads,
+                                       const int32_t* block_tables, int32_t max_blocks,
+                                       const int32_t* cached_lens, const int32_t* cu_new_lens,
+                                       int32_t num_seqs, int32_t total_new, int32_t max_new_len,
+                                       int32_t max_total_len, float scale, void* out, float* lse,
+                                       void* workspace, size_t workspace_bytes, void* stream);
+size_t pkv_quant_prefill_workspace_bytes(int32_t num_seqs, int32_t total_new, int32_t num_q_heads,
+                                         int32_t num_kv_heads, int32_t head_dim, int32_t bits,
+                                         int32_t max_new_len, int32_t max_total_len);
 
 /* Paged gather (test support): copies the first lens[i] tokens of every sequence out of the
  * pool into contiguous k_out / v_out, bf16 [sum lens][num_kv_heads][head_dim], sequence i

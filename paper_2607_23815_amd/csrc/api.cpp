@@ -236,6 +236,57 @@ pkv_status check_rows(const std::string& f, int32_t num_q_heads, int32_t hkv, co
   return PKV_OK;
 }
 
+struct QuantView {
+  uint8_t* cache;
+  int32_t num_blocks, hkv, head_dim, bits;
+};
+
+pkv_status check_quant(const pkv_quant_kv* kv, const std::string& f, QuantView* view) {
+  if (kv == nullptr) return fail(PKV_ERR_INVALID_ARG, f + ": the quantised cache is NULL");
+  if (kv->cache == nullptr) return fail(PKV_ERR_INVALID_ARG, f + ": cache is NULL");
+  if (kv->num_blocks <= 0 || kv->num_kv_heads <= 0)
+    return fail(PKV_ERR_INVALID_ARG, f + ": num_blocks and num_kv_heads must be positive");
+  if (kv->block_size != kSupportedBlockSize)
+    return fail(PKV_ERR_UNSUPPORTED_SHAPE, f + ": block_size must be 16");
+  if (kv->head_dim != 64 && kv->head_dim != 128)
+    return fail(PKV_ERR_UNSUPPORTED_SHAPE, f + ": head_dim must be 64 or 128");
+  if (kv->bits != 4 && kv->bits != 8)
+    return fail(PKV_ERR_UNSUPPORTED_SHAPE, f + ": bits must be 4 or 8");
+  if (!aligned16(kv->cache))
+    return fail(PKV_ERR_INVALID_ARG, f + ": cache must be 16-byte aligned");
+  view->cache = static_cast<uint8_t*>(kv->cache);
+  view->num_blocks = kv->num_blocks;
+  view->hkv = kv->num_kv_heads;
+  view->head_dim = kv->head_dim;
+  view->bits = kv->bits;
+  return PKV_OK;
+}
+// The view that metadata is checked and a bf16 call's arguments are looked at with.
+KvView shape_of(const QuantView& v) { return KvView{nullptr, nullptr, v.num_blocks, v.hkv, v.head_dim}; }
+
+pkv_status convert_blocks(const char* fn, const pkv_paged_kv* kv, const pkv_quant_kv* quant, bool back,
+                          const int32_t* pairs, int32_t num_pairs, void* stream) {
+  const std::string f(fn);
+  KvView pool;
+  pkv_status st = check_kv(kv, fn, &pool);
+  if (st != PKV_OK) return st;
+  QuantView view;
+  st = check_quant(quant, f, &view);
+  if (st != PKV_OK) return st;
+  if (pool.hkv != view.hkv || pool.head_dim != view.head_dim)
+    return fail(PKV_ERR_INVALID_ARG, f + ": the pools' num_kv_heads or head_dim differ");
+  if (num_pairs < 0) return fail(PKV_ERR_INVALID_ARG, f + ": negative size");
+  if (num_pairs == 0) return ok();
+  if (pairs == nullptr) return fail(PKV_ERR_INVALID_ARG, f + ": NULL pointer");
+  if ((int64_t)num_pairs * view.hkv >= (1 << 26))  // (waves of a launch)
+    return fail(PKV_ERR_INVALID_ARG, f + ": 2^26 pairs x kv heads or more");
+  const QuantBlocksArgs a{view.cache, pool.k, pool.v, pairs, num_pairs, view.hkv, view.num_blocks,
+                          pool.num_blocks};
+  return launched(launch_quant_blocks(a, back, view.head_dim, view.bits,
+                                      static_cast<hipStream_t>(stream)),
+                  fn);
+}
+
 }  // namespace
 }  // namespace pkv
 
@@ -759,6 +810,182 @@ pkv_status pkv_sparse_attention(const pkv_paged_kv* kv, const void* q, int32_t n
   a.blocks = blocks;
   a.scale_log2 = scale * 1.44269504088896340736f;
   return launched(launch_sparse_attention(a, view.head_dim, workspace, s), fn);
+}
+
+size_t pkv_quant_block_bytes(int32_t num_kv_heads, int32_t head_dim, int32_t bits) {
+  if (num_kv_heads <= 0 || (head_dim != 64 && head_dim != 128) || (bits != 4 && bits != 8)) return 0;
+  return (size_t)num_kv_heads * quant_slab_bytes(head_dim, bits);
+}
+
+pkv_status pkv_quant_append(const pkv_quant_kv* kv, const void* k_new, int64_t k_stride,
+                            const void* v_new, int64_t v_stride, const int32_t* block_tables,
+                            int32_t max_blocks, const int32_t* cached_lens,
+                            const int32_t* cu_new_lens, int32_t num_seqs, int32_t total_new,
+                            int32_t max_new_len, void* stream) {
+  const char* fn = "pkv_quant_append";
+  const std::string f(fn);
+  QuantView view;
+  pkv_status st = check_quant(kv, f, &view);
+  if (st != PKV_OK) return st;
+  if (num_seqs < 0 || total_new < 0 || max_new_len < 0 || max_blocks < 0)
+    return fail(PKV_ERR_INVALID_ARG, f + ": negative size");
+  if (num_seqs == 0 || total_new == 0) return ok();
+  if (k_new == nullptr || v_new == nullptr || block_tables == nullptr || cached_lens == nullptr ||
+      cu_new_lens == nullptr)
+    return fail(PKV_ERR_INVALID_ARG, f + ": NULL pointer");
+  if (!aligned16(k_new) || !aligned16(v_new))
+    return fail(PKV_ERR_INVALID_ARG, f + ": k_new / v_new must be 16-byte aligned");
+  const int64_t row = (int64_t)view.hkv * view.head_dim;
+  if (k_stride < row || v_stride < row || (k_stride | v_stride) & 7)
+    return fail(PKV_ERR_INVALID_ARG,
+                f + ": row strides must be multiples of 8 elements that hold a row");
+  if (max_new_len == 0 || max_blocks == 0)
+    return fail(PKV_ERR_INVALID_ARG, f + ": max_new_len and max_blocks must be > 0");
+  if (num_seqs > kMaxGridZ)
+    return fail(PKV_ERR_INVALID_ARG, f + ": more than 65535 sequences per call");
+  if (((int64_t)max_new_len / kSupportedBlockSize + 2) * view.hkv >= (1 << 24))
+    return fail(PKV_ERR_INVALID_ARG, f + ": 2^24 blocks x kv heads of a sequence or more");
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  {
+    const MetaCheck c = meta(kMetaAppend, shape_of(view), block_tables, max_blocks, cached_lens,
+                             cu_new_lens, num_seqs, total_new, max_new_len,
+                             (int64_t)max_blocks * kSupportedBlockSize);
+    if ((st = check_metadata(fn, &c, 1, s)) != PKV_OK) return st;
+  }
+  QuantAppendArgs a{};
+  a.cache = view.cache;
+  a.k = static_cast<const uint16_t*>(k_new);
+  a.v = static_cast<const uint16_t*>(v_new);
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.rows = total_new;
+  a.tables = block_tables;
+  a.cached_lens = cached_lens;
+  a.cu_new_lens = cu_new_lens;
+  a.max_blocks = max_blocks;
+  a.hkv = view.hkv;
+  a.num_blocks = view.num_blocks;
+  return launched(launch_quant_append(a, num_seqs, max_new_len, view.head_dim, view.bits, s), fn);
+}
+
+pkv_status pkv_quant_blocks(const pkv_paged_kv* from, const pkv_quant_kv* to, const int32_t* pairs,
+                            int32_t num_pairs, void* stream) {
+  return convert_blocks("pkv_quant_blocks", from, to, false, pairs, num_pairs, stream);
+}
+
+pkv_status pkv_dequant_blocks(const pkv_quant_kv* from, const pkv_paged_kv* to, const int32_t* pairs,
+                              int32_t num_pairs, void* stream) {
+  return convert_blocks("pkv_dequant_blocks", to, from, true, pairs, num_pairs, stream);
+}
+
+size_t pkv_quant_decode_workspace_bytes(int32_t num_seqs, int32_t num_q_heads, int32_t num_kv_heads,
+                                        int32_t head_dim, int32_t bits, int32_t max_seq_len) {
+  if (num_seqs <= 0 || num_q_heads <= 0 || num_kv_heads <= 0 || num_q_heads % num_kv_heads != 0 ||
+      head_dim <= 0 || max_seq_len <= 0 || (int64_t)num_seqs * num_kv_heads > kMaxRowItems)
+    return 0;
+  return quant_decode_workspace_bytes(num_seqs, num_q_heads, num_kv_heads, head_dim, bits,
+                                      max_seq_len);
+}
+
+pkv_status pkv_quant_decode_attention(const pkv_quant_kv* kv, const void* q, int32_t num_q_heads,
+                                      const int32_t* block_tables, int32_t max_blocks,
+                                      const int32_t* seq_lens, int32_t num_seqs,
+                                      int32_t max_seq_len, float scale, void* out, float* lse,
+                                      void* workspace, size_t workspace_bytes, void* stream) {
+  const char* fn = "pkv_quant_decode_attention";
+  const std::string f(fn);
+  QuantView view;
+  pkv_status st = check_quant(kv, f, &view);
+  if (st != PKV_OK) return st;
+  if (num_q_heads <= 0 || num_q_heads % view.hkv != 0 || num_q_heads / view.hkv > 16)
+    return fail(PKV_ERR_UNSUPPORTED_SHAPE,
+                f + ": num_q_heads must be a multiple of num_kv_heads, with at most 16 query "
+                    "heads per kv head");
+  if (num_seqs < 0 || max_seq_len < 0 || max_blocks < 0)
+    return fail(PKV_ERR_INVALID_ARG, f + ": negative size");
+  if (num_seqs == 0) return ok();
+  if (q == nullptr || out == nullptr || block_tables == nullptr || seq_lens == nullptr)
+    return fail(PKV_ERR_INVALID_ARG, f + ": NULL pointer");
+  if (!aligned16(q) || !aligned16(out))
+    return fail(PKV_ERR_INVALID_ARG, f + ": q / out must be 16-byte aligned");
+  if (max_seq_len == 0 || max_blocks == 0)
+    return fail(PKV_ERR_INVALID_ARG, f + ": max_seq_len, max_blocks must be > 0");
+  if ((int64_t)max_blocks * kSupportedBlockSize < max_seq_len)
+    return fail(PKV_ERR_INVALID_ARG, f + ": max_seq_len exceeds max_blocks * block_size");
+  if (!(scale > 0.f)) return fail(PKV_ERR_INVALID_ARG, f + ": scale <= 0");
+  if ((int64_t)num_seqs * view.hkv > kMaxRowItems)
+    return fail(PKV_ERR_INVALID_ARG, f + ": 2^22 sequences x kv heads or more");
+  const size_t need = quant_decode_workspace_bytes(num_seqs, num_q_heads, view.hkv, view.head_dim,
+                                                   view.bits, max_seq_len);
+  if (need > 0 && (workspace == nullptr || workspace_bytes < need || !aligned16(workspace)))
+    return fail(PKV_ERR_INVALID_ARG,
+                f + ": workspace missing, too small or not 16-byte aligned "
+                    "(see pkv_quant_decode_workspace_bytes)");
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  {
+    // (a length of 0 is in order here)
+    MetaCheck c = meta(kMetaRows, shape_of(view), block_tables, max_blocks, seq_lens, nullptr,
+                       num_seqs, -1, max_seq_len, 0);
+    c.table_rows = num_seqs;
+    if ((st = check_metadata(fn, &c, 1, s)) != PKV_OK) return st;
+  }
+  QuantDecodeArgs a{};
+  a.cache = view.cache;
+  a.q = static_cast<const uint16_t*>(q);
+  a.tables = block_tables;
+  a.seq_lens = seq_lens;
+  a.out = static_cast<uint16_t*>(out);
+  a.lse = lse;
+  a.max_blocks = max_blocks;
+  a.num_seqs = num_seqs;
+  a.max_len = max_seq_len;
+  a.hq = num_q_heads;
+  a.hkv = view.hkv;
+  a.num_blocks = view.num_blocks;
+  a.scale_log2 = scale * 1.44269504088896340736f;
+  return launched(launch_quant_decode(a, view.head_dim, view.bits, workspace, s), fn);
+}
+
+size_t pkv_quant_prefill_workspace_bytes(int32_t num_seqs, int32_t total_new, int32_t num_q_heads,
+                                         int32_t num_kv_heads, int32_t head_dim, int32_t bits,
+                                         int32_t max_new_len, int32_t max_total_len) {
+  if (bits != 4 && bits != 8) return 0;
+  return pkv_prefill_workspace_bytes(num_seqs, total_new, num_q_heads, num_kv_heads, head_dim,
+                                     max_new_len, max_total_len);
+}
+
+pkv_status pkv_quant_prefill_attention(const pkv_quant_kv* kv, const void* q, int32_t num_q_heads,
+                                       const int32_t* block_tables, int32_t max_blocks,
+                                       const int32_t* cached_lens, const int32_t* cu_new_lens,
+                                       int32_t num_seqs, int32_t total_new, int32_t max_new_len,
+                                       int32_t max_total_len, float scale, void* out, float* lse,
+                                       void* workspace, size_t workspace_bytes, void* stream) {
+  const char* fn = "pkv_quant_prefill_attention";
+  QuantView view;
+  pkv_status st = check_quant(kv, fn, &view);
+  if (st != PKV_OK) return st;
+  const KvView shape = shape_of(view);
+  bool empty = false;
+  st = check_prefill(shape, fn, q, num_q_heads, block_tables, max_blocks, cached_lens, cu_new_lens,
+                     num_seqs, total_new, max_new_len, max_total_len, scale, out, workspace,
+                     workspace_bytes, &empty);
+  if (st != PKV_OK || empty) return st;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  {
+    const MetaCheck c = meta(kMetaPrefill, shape, block_tables, max_blocks, cached_lens, cu_new_lens,
+                             num_seqs, total_new, max_new_len, max_total_len);
+    if ((st = check_metadata(fn, &c, 1, s)) != PKV_OK) return st;
+  }
+  const bool plan = workspace != nullptr &&
+                    prefill_workspace_bytes(num_seqs, total_new, num_q_heads, view.hkv,
+                                            view.head_dim, max_new_len, max_total_len) > 0;
+  return launched(launch_quant_prefill(view.cache, view.num_blocks, view.hkv, view.head_dim,
+                                       view.bits, static_cast<const uint16_t*>(q), num_q_heads,
+                                       block_tables, max_blocks, cached_lens, cu_new_lens, num_seqs,
+                                       total_new, max_new_len, max_total_len, scale,
+                                       static_cast<uint16_t*>(out), lse, plan ? workspace : nullptr,
+                                       s),
+                  fn);
 }
 
 }  // extern "C"

@@ -124,6 +124,60 @@ size_t sparse_workspace_bytes(int64_t items, int32_t g, int32_t head_dim, int32_
 hipError_t launch_sparse_attention(SparseArgs a, int head_dim, void* workspace,
                                    hipStream_t stream);
 
+// A cache held in 8 or 4 bits: uint8 [num_blocks][hkv][quant_slab_bytes]; quant.h has the slab.
+size_t quant_slab_bytes(int32_t head_dim, int32_t bits);
+struct QuantAppendArgs {
+  uint8_t* cache;
+  const uint16_t* k;  // rows, k_stride and v_stride elements apart
+  const uint16_t* v;
+  int64_t k_stride, v_stride, rows;
+  const int32_t* tables;
+  const int32_t* cached_lens;
+  const int32_t* cu_new_lens;
+  int32_t max_blocks, hkv, num_blocks;
+};
+hipError_t launch_quant_append(const QuantAppendArgs& a, int32_t num_seqs, int32_t max_new_len,
+                               int head_dim, int bits, hipStream_t stream);
+// Pairs (block of the bf16 pool, block of the cache); back: (block of the cache, block of the pool).
+struct QuantBlocksArgs {
+  uint8_t* cache;
+  uint16_t* k_cache;
+  uint16_t* v_cache;
+  const int32_t* pairs;
+  int32_t num_pairs, hkv, num_blocks, pool_blocks;
+};
+hipError_t launch_quant_blocks(const QuantBlocksArgs& a, bool back, int head_dim, int bits,
+                               hipStream_t stream);
+struct QuantDecodeArgs {
+  const uint8_t* cache;
+  const uint16_t* q;
+  const int32_t* tables;
+  const int32_t* seq_lens;
+  uint16_t* out;
+  float* lse;  // or null
+  int32_t max_blocks, num_seqs, max_len, hq, hkv, num_blocks;
+  float scale_log2;
+  // set by the launch: keys per split, splits of the longest sequence, the splits' partial results, and
+  // the order of the sequences (null: see by_rank)
+  int32_t split_keys, splits;
+  bool by_rank;
+  const int32_t* order;
+  float* ws_o;
+  float* ws_ml;
+};
+size_t quant_decode_workspace_bytes(int32_t num_seqs, int32_t hq, int32_t hkv, int32_t head_dim,
+                                    int32_t bits, int32_t max_len);
+hipError_t launch_quant_decode(QuantDecodeArgs a, int head_dim, int bits, void* workspace,
+                               hipStream_t stream);
+// As launch_prefill, over the cache.
+hipError_t launch_quant_prefill(const uint8_t* cache, int32_t num_blocks, int32_t hkv, int32_t head_dim,
+                                int32_t bits, const uint16_t* q, int32_t hq,
+                                const int32_t* block_tables, int32_t max_blocks,
+                                const int32_t* cached_lens, const int32_t* cu_new_lens,
+                                int32_t num_seqs, int32_t total_new, int32_t max_new_len,
+                                int32_t max_total_len, float scale, uint16_t* out, float* lse,
+                                void* workspace, hipStream_t stream);
+
 hipError_t launch_copy_blocks(const KvView& kv, const int32_t* pairs, int32_t num_pairs,
                               hipStream_t stream);
 
@@ -137,6 +191,8 @@ struct PrefillSplit {
   int32_t nsplit;
   bool order;
 };
+// Sequences up to which every wave ranks them for itself (at most kRankSeqs).
+constexpr int32_t kPrefillRankSeqs = 16;
 PrefillSplit prefill_split_plan(int32_t num_seqs, int32_t hq, int32_t hkv, int32_t max_new_len,
                                 int32_t max_total_len);
 // Workspace of the plan (0 when it needs none): the sequence order when ordered, then when
@@ -151,6 +207,12 @@ hipError_t launch_prefill(const KvView& kv, const uint16_t* q, int32_t hq,
                           int32_t num_seqs, int32_t total_new, int32_t max_new_len,
                           int32_t max_total_len, float scale, uint16_t* out, float* lse,
                           void* workspace, hipStream_t stream);
+
+// The merge of a split prefill's partial results (prefill_split_plan has the split).
+hipError_t launch_prefill_merge(int32_t head_dim, const int32_t* cached_lens,
+                                const int32_t* cu_new_lens, int32_t num_seqs, int32_t hq,
+                                int32_t max_new_len, const PrefillSplit& sp, const float* ws_o,
+                                const float* ws_ml, uint16_t* out, float* lse, hipStream_t stream);
 
 size_t decode_workspace_bytes(int32_t num_seqs, int32_t hq, int32_t hkv, int32_t head_dim,
                               int32_t max_seq_len);

@@ -1,0 +1,483 @@
+// Decode attention over a cache held in 8 or 4 bits (gfx950): sequence i's query heads of a kv head attend
+// over its keys, out = sum_t softmax_t(scale <q, K[t]>) V[t], as pkv_decode_attention does over bf16.
+//
+// A wave takes four blocks (64 keys) at a time straight into the matrix-core operands, scores
+// S^T = K Q^T and values O^T += V^T P^T, heads as columns. The slab is laid out as the operands are (quant.h),
+// so a block's codes are one or two contiguous 16-byte loads of the wave, for keys and for values. Codes
+// become bf16 two at a time by the conversion instruction, exactly: keys with their group's power of two,
+// values as they are, since a token's value scale multiplies its weight.
+//
+// A product has 16 columns and a group often fewer heads, so the heads stand in the columns kWays = 2 or 4
+// times over (g <= 8, g <= 4), and column (way w, head h) goes on with the scores of blocks w, w + kWays, ...
+// alone: every lane's exponentials are of use. A weight goes to the value product in two bf16 parts, itself
+// rounded and what that left over, within 2^-16 of itself together; the second stands in the next way's
+// column, whose weights for the block would be zeros (kWays 1 takes a second product).
+//
+// What a weight is relative to is kept kSlack powers of two above the largest score seen when it was set, and
+// moved when a score passes it. So weights are at most 1 and most steps need no lane exchange and no
+// rescaling; the values of a cache are finite (or NaN), and zero weights are safe with them.
+#include <math.h>
+
+#include <algorithm>
+
+#include "decode_impl.h"
+#include "launch.h"
+#include "quant.h"
+
+namespace pkv {
+namespace {
+
+using dec::finite_max;
+using qnt::Slab;
+
+constexpr int kStep = 4;  // blocks per step
+constexpr int kStepKeys = kStep * kBlockSize;
+constexpr float kSlack = 8.f;  // (base 2)
+constexpr int kMergeWaves = 4;
+constexpr int kMaxSplits = 64;  // (a lane each in the merge)
+
+template <int kCtrl>
+__device__ __forceinline__ float dpp_f(float x) {
+  return __uint_as_float(dpp<kCtrl>(__float_as_uint(x)));
+}
+constexpr int kRor4 = 0x124, kRor8 = 0x128;  // rotations within 16 lanes
+
+// Sum (or maximum) over the ways, the columns that hold the same head.
+template <int kWays>
+__device__ __forceinline__ float ways_sum(float x) {
+  if constexpr (kWays >= 2) x += dpp_f<kRor8>(x);
+  if constexpr (kWays >= 4) x += dpp_f<kRor4>(x);
+  return x;
+}
+template <int kWays>
+__device__ __forceinline__ float ways_max(float x) {
+  if constexpr (kWays >= 2) x = fmaxf(x, dpp_f<kRor8>(x));
+  if constexpr (kWays >= 4) x = fmaxf(x, dpp_f<kRor4>(x));
+  return x;
+}
+// Two floats as two bf16 each, their sum off by 2^-16 of the float at most.
+__device__ __forceinline__ void two_parts(float x, float y, uint32_t& first, uint32_t& second) {
+  first = pack_bf16x2(x, y);
+  second = pack_bf16x2(x - __uint_as_float(first << 16), y - __uint_as_float(first & 0xFFFF0000u));
+}
+
+// A lane's codes of a block: of the keys (slot col, dims D / 4 * grp ..), and of the values (slots
+// 4 grp .., dims 16 a + col).
+template <int D, int BITS>
+struct BlockCodes {
+  uint32_t w[Slab<D, BITS>::kWords];
+  __device__ __forceinline__ void load(const uint8_t* slab, int first, int offset, int stride) {
+    constexpr int kLane = Slab<D, BITS>::kLane;
+    if constexpr (kLane == 8) {
+      const u32x2 x = buf_ld8(slab, Slab<D, BITS>::kBytes, first + offset);
+      w[0] = x[0], w[1] = x[1];
+    } else {
+#pragma unroll
+      for (int u = 0; u < kLane / 16; ++u) {
+        const u32x4 x = buf_ld16(slab, Slab<D, BITS>::kBytes, first + offset + u * stride);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[4 * u + e] = x[e];
+      }
+    }
+  }
+};
+__device__ __forceinline__ uint32_t buf_ld1(const void* base, int bytes, int voffset) {
+#if __HIP_DEVICE_COMPILE__
+  const __amdgpu_buffer_rsrc_t rsrc =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, kBufferFlags);
+  return __builtin_amdgcn_raw_buffer_load_b8(rsrc, voffset, 0, 0);
+#else
+  return 0u;
+#endif
+}
+
+template <int D, int BITS, int kA>
+__device__ __forceinline__ void value_products(const BlockCodes<D, BITS>& even,
+                                               const BlockCodes<D, BITS>& odd, const bf16x8 p,
+                                               f32x4 (&acc)[D / 16]) {
+  const u32x2 x = qnt::four_bf16<BITS, kA>(even.w), y = qnt::four_bf16<BITS, kA>(odd.w);
+  acc[kA] = mfma16(as_bf16x8(u32x4{x[0], x[1], y[0], y[1]}), p, acc[kA]);
+  if constexpr (kA + 1 < D / 16) value_products<D, BITS, kA + 1>(even, odd, p, acc);
+}
+
+// One wave's share: keys [k0, k1) of a sequence, k0 a multiple of 16, not empty. Leaves, summed over the
+// ways, the unnormalised output (lane (col, grp) holds dims 16 a + 4 grp + 0..3 of head col % (16 / kWays)),
+// what the weights are relative to (base 2) and their sum.
+template <int D, int BITS, int kWays>
+__device__ __forceinline__ void quant_range(const QuantDecodeArgs& a, const bf16x8 (&qf)[D / 32],
+                                            const int32_t* __restrict__ table, const int kvh,
+                                            const int k0, const int k1, f32x4 (&acc_out)[D / 16],
+                                            float& m_out, float& l_out) {
+  using S = Slab<D, BITS>;
+  constexpr int KK = D / 32, DB = D / 16;
+  constexpr int kMine = kStep / kWays;  // blocks per step whose scores a column goes on with
+  const int lane = threadIdx.x & 63;
+  const int col = lane & 15, grp = lane >> 4;
+  const int way = col / (16 / kWays);
+  // offsets of the lane's codes and scales within a slab
+  const int key_at = S::kLane == 8 ? (grp / 2) * 256 + col * 16 + (grp & 1) * 8
+                                   : grp * (S::kLane / 16) * 256 + col * 16;
+  const int key_scale_at = S::kKeyScales + col * (D / 32) + grp * D / 128;
+  const int value_at = S::kValues + lane * (S::kLane < 16 ? S::kLane : 16);
+
+  // The range's blocks in lane registers, 64 at a time and the next 64: lane l holds block 64 c + l, or
+  // pool block 0 (a stand-in) past the range and for entries outside the pool.
+  const int b_first = k0 / kBlockSize;
+  const int nblk = (k1 - k0 + kBlockSize - 1) / kBlockSize;
+  auto raw_chunk = [&](int c) {
+    const int r = 64 * c + lane;
+    return r < nblk && b_first + r < a.max_blocks ? table[b_first + r] : 0;
+  };
+  auto checked = [&](int e) { return e < 0 || e >= a.num_blocks ? 0 : e; };
+  const int raw0 = raw_chunk(0), raw1 = raw_chunk(1);
+  int tab = checked(raw0), tab_next = checked(raw1);
+  int chunk = 0;
+  const uint8_t* head = a.cache + (size_t)kvh * S::kBytes;
+  const size_t stride = (size_t)a.hkv * S::kBytes;
+
+  f32x4 acc[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) acc[db] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, lpart = 0.f;
+
+  BlockCodes<D, BITS> k[kStep], v[kStep];
+  uint32_t ks[kStep];
+  u32x4 vs[kMine];
+  // (b: a block counted from the current 64's first, below 128)
+  auto slab = [&](int b) {
+    const int e = b < 64 ? __builtin_amdgcn_readlane(tab, b)
+                         : __builtin_amdgcn_readlane(tab_next, b - 64);
+    return head + (size_t)e * stride;
+  };
+  auto load_k = [&](int b) {
+#pragma unroll
+    for (int i = 0; i < kStep; ++i) {
+      const uint8_t* s = slab(b + i);
+      k[i].load(s, 0, key_at, 256);
+      ks[i] = buf_ld1(s, S::kBytes, key_scale_at);
+    }
+  };
+  auto load_v = [&](int b) {
+#pragma unroll
+    for (int i = 0; i < kStep; ++i) v[i].load(slab(b + i), 0, value_at, 1024);
+#pragma unroll
+    for (int j = 0; j < kMine; ++j) {
+      const uint8_t* s = slab(b + j * kWays);
+#pragma unroll
+      for (int w = 1; w < kWays; ++w) {
+        const uint8_t* x = slab(b + j * kWays + w);
+        s = way == w ? x : s;
+      }
+      vs[j] = ld16(s + S::kValueScales + 16 * grp);
+    }
+  };
+  load_k(0);
+  load_v(0);
+  for (int t0 = k0, b = 0;; t0 += kStepKeys, b += kStep) {
+    if (b == 64) {
+      b = 0;
+      ++chunk;
+      tab = tab_next;
+      tab_next = checked(raw_chunk(chunk + 1));
+    }
+    f32x4 st[kStep];
+#pragma unroll
+    for (int i = 0; i < kStep; ++i) {
+      const float scale = __uint_as_float(ks[i] << 23);
+      st[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk)
+        st[i] = mfma16(as_bf16x8(qnt::eight_bf16<BITS>(k[i].w + kk * BITS / 4, scale)), qf[kk], st[i]);
+    }
+    const bool more = t0 + kStepKeys < k1;
+    if (more) load_k(b + kStep);  // (in flight through the rest of this step)
+    // lane holds keys 4 grp + r of its way's blocks
+    float sv[kMine][4], weigh[kMine][4];
+#pragma unroll
+    for (int j = 0; j < kMine; ++j) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float x = st[j * kWays][r];
+#pragma unroll
+        for (int w = 1; w < kWays; ++w) x = way == w ? st[j * kWays + w][r] : x;
+        sv[j][r] = x;
+        weigh[j][r] = __uint_as_float(vs[j][r]);
+      }
+    }
+    if (t0 + kStepKeys > k1) {  // slots past the end, which may hold anything
+#pragma unroll
+      for (int j = 0; j < kMine; ++j) {
+        const int left = k1 - t0 - (j * kWays + way) * kBlockSize - 4 * grp;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          sv[j][r] = r < left ? sv[j][r] : -INFINITY;
+          weigh[j][r] = r < left ? weigh[j][r] : 0.f;
+        }
+      }
+      if constexpr (BITS == 8) {  // (codes of 4 bits are all finite)
+#pragma unroll
+        for (int i = 0; i < kStep; ++i) {
+          const int left = min(max(k1 - t0 - i * kBlockSize - 4 * grp, 0), 4);
+          const uint32_t mask = left == 4 ? ~0u : (1u << 8 * left) - 1u;
+#pragma unroll
+          for (int e = 0; e < S::kWords; ++e) v[i].w[e] &= mask;
+        }
+      }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < kMine; ++j) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sv[j][r]);
+    }
+    mx *= a.scale_log2;
+    if (__builtin_amdgcn_ballot_w64(mx > m) != 0) {
+      const float top = ways_max<kWays>(dec::wave_max16(mx));
+      const float m_new = top > m ? top + kSlack : m;
+      const float alpha = fast_exp2(m - finite_max(m_new));
+      m = m_new;
+      lpart *= alpha;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[db][r] *= alpha;
+      }
+    }
+    const float m_sub = finite_max(m);
+    constexpr int kProducts = kWays == 1 ? 2 : 1;
+    uint32_t p[kProducts][kStep][2];
+#pragma unroll
+    for (int j = 0; j < kMine; ++j) {
+      float x[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        x[r] = fast_exp2(fmaf(sv[j][r], a.scale_log2, -m_sub));
+        lpart += x[r];
+        x[r] *= weigh[j][r];
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        uint32_t first, second;
+        two_parts(x[2 * e], x[2 * e + 1], first, second);
+        if constexpr (kWays == 1) {
+          p[0][j][e] = first;
+          p[1][j][e] = second;
+        } else {
+          // (the second part of the way before, from its columns)
+          second = dpp<kWays == 4 ? kRor4 : kRor8>(second);
+#pragma unroll
+          for (int w = 0; w < kWays; ++w)
+            p[0][j * kWays + w][e] = way == w ? first : way == (w + 1) % kWays ? second : 0u;
+        }
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < kProducts; ++n) {
+#pragma unroll
+      for (int i = 0; i < kStep; i += 2)
+        value_products<D, BITS, 0>(
+            v[i], v[i + 1],
+            as_bf16x8(u32x4{p[n][i][0], p[n][i][1], p[n][i + 1][0], p[n][i + 1][1]}), acc);
+    }
+    if (!more) break;
+    load_v(b + kStep);
+  }
+  l_out = ways_sum<kWays>(dec::wave_sum16(lpart));
+  m_out = m;
+#pragma unroll
+  for (int db = 0; db < DB; ++db) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) acc_out[db][r] = ways_sum<kWays>(acc[db][r]);
+  }
+}
+
+// kParts waves per (sequence, kv head, split): each takes an equal share of the split's keys, and the shares
+// meet in LDS. With several splits, the results are partial ones for the merge below.
+template <int D, int BITS, int kWays, int kParts>
+__global__ __launch_bounds__(64 * kParts) __attribute__((amdgpu_waves_per_eu(2)))
+void quant_decode_kernel(const QuantDecodeArgs a) {
+  constexpr int DB = D / 16;
+  __shared__ __align__(16) dec::DecodeSmem<D, kParts> sm;
+  const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int per_seq = a.hkv * a.splits;
+  const int rank = (int)(blockIdx.x / per_seq), rem = (int)(blockIdx.x % per_seq);
+  const int seq = a.order != nullptr ? a.order[rank]
+                  : a.by_rank        ? seq_at_rank(a.seq_lens, nullptr, a.num_seqs, rank)
+                                     : rank;
+  const int kvh = rem / a.splits, split = rem % a.splits;
+  const int g = a.hq / a.hkv;
+  const int len = min(a.seq_lens[seq], a.max_len);
+  const int k0 = split * a.split_keys;
+  const size_t row0 = (size_t)seq * a.hq + kvh * g;
+  if (k0 >= len) {  // (workgroup-uniform) nothing here; a sequence without keys gives zeros
+    if (len <= 0 && split == 0) {
+      for (int u = threadIdx.x; u < g * (D / 8); u += 64 * kParts)
+        st16(a.out + row0 * D + u * 8, u32x4{0u, 0u, 0u, 0u});
+      if (a.lse != nullptr && (int)threadIdx.x < g) a.lse[row0 + threadIdx.x] = -INFINITY;
+    }
+    return;
+  }
+  const int k1 = min(len, k0 + a.split_keys);
+  const int share = ((k1 - k0 + kParts - 1) / kParts + kStepKeys - 1) / kStepKeys * kStepKeys;
+  const int s0 = min(k0 + wave * share, k1), s1 = min(s0 + share, k1);
+  const int h = col % (16 / kWays), way = col / (16 / kWays);
+  if (s0 < s1) {
+    bf16x8 qf[D / 32];  // the heads kWays times over (zeros past the group's): dims D / 4 * grp ..
+#pragma unroll
+    for (int kk = 0; kk < D / 32; ++kk) {
+      u32x4 x = {0u, 0u, 0u, 0u};
+      if (h < g) x = ld16(a.q + (row0 + h) * D + grp * (D / 4) + kk * 8);
+      qf[kk] = as_bf16x8(x);
+    }
+    f32x4 acc[DB];
+    float m, l;
+    quant_range<D, BITS, kWays>(a, qf, a.tables + (size_t)seq * a.max_blocks, kvh, s0, s1, acc, m, l);
+    if (h < g) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+        if (db % kWays == way)
+          st16(&sm.o[wave][h][db * 16 + 4 * grp], __builtin_bit_cast(u32x4, acc[db]));
+      if (lane < 16 / kWays) {
+        sm.m[wave][h] = m;
+        sm.l[wave][h] = l;
+      }
+    }
+  } else if (lane < g) {
+    sm.m[wave][lane] = -INFINITY;
+    sm.l[wave][lane] = 0.f;
+  }
+  __syncthreads();
+  const int used = (k1 - k0 + share - 1) / share;  // shares that have keys
+  for (int u = threadIdx.x; u < g * (D / 4); u += 64 * kParts) {  // one thread per (head, 4 dims)
+    const int hh = u / (D / 4), d = (u % (D / 4)) * 4;
+    float mx = -INFINITY;
+#pragma unroll
+    for (int s = 0; s < kParts; ++s) mx = fmaxf(mx, sm.m[s][hh]);
+    float den = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < kParts; ++s) {
+      if (s >= used) break;
+      const float w = fast_exp2(sm.m[s][hh] - finite_max(mx));
+      den += w * sm.l[s][hh];
+      const f32x4 x = __builtin_bit_cast(f32x4, ld16(&sm.o[s][hh][d]));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += w * x[e];
+    }
+    const size_t row = row0 + hh;
+    if (a.splits == 1 || len <= a.split_keys) {
+      const float inv = 1.f / den;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = den == 0.f ? 0.f : o[e] * inv;
+      st8(a.out + row * D + d, u32x2{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])});
+      if (a.lse != nullptr && d == 0) a.lse[row] = (mx + log2f(den)) * kLn2;
+    } else {
+      const size_t slot = row * a.splits + split;
+      st16(a.ws_o + slot * D + d, __builtin_bit_cast(u32x4, o));
+      if (d == 0) {
+        a.ws_ml[slot * 2] = mx;
+        a.ws_ml[slot * 2 + 1] = den;
+      }
+    }
+  }
+}
+
+// One wave per (sequence, query head): the splits' partial results by their log-sum-exp weights.
+template <int D>
+__global__ __launch_bounds__(64 * kMergeWaves) void quant_merge_kernel(const QuantDecodeArgs a) {
+  constexpr int PER = D / 64;
+  const int64_t item = (int64_t)blockIdx.x * kMergeWaves + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  if (item >= (int64_t)a.num_seqs * a.hq) return;
+  const int len = min(a.seq_lens[item / a.hq], a.max_len);
+  const int n = (len + a.split_keys - 1) / a.split_keys;
+  if (n <= 1) return;  // (written already)
+  const float* ml = a.ws_ml + (size_t)item * a.splits * 2;
+  const float* src = a.ws_o + (size_t)item * a.splits * D + lane * PER;
+  const bool mine = lane < n;
+  const float m = mine ? ml[lane * 2] : -INFINITY;
+  const float l = mine ? ml[lane * 2 + 1] : 0.f;
+  const float top = wave_all(m, Max());
+  const float w = mine ? fast_exp2(m - finite_max(top)) : 0.f;
+  const float den = wave_all(w * l, Add());
+  float o[PER];
+#pragma unroll
+  for (int e = 0; e < PER; ++e) o[e] = 0.f;
+  for (int s = 0; s < n; s += 8) add_partials<D>(src, w, s, n, o);
+  const float inv = 1.f / den;
+#pragma unroll
+  for (int e = 0; e < PER; ++e) o[e] = den == 0.f ? 0.f : o[e] * inv;
+  uint16_t* dst = a.out + (size_t)item * D + lane * PER;
+  if constexpr (PER == 2) {
+    *reinterpret_cast<uint32_t*>(dst) = pack_bf16x2(o[0], o[1]);
+  } else {
+    dst[0] = (uint16_t)(pack_bf16x2(o[0], 0.f) & 0xFFFFu);
+  }
+  if (a.lse != nullptr && lane == 0) a.lse[item] = (top + log2f(den)) * kLn2;
+}
+
+// How a call is cut: host arithmetic on its sizes alone.
+struct QuantCut {
+  int parts;       // waves per (sequence, kv head, split)
+  int splits;      // of the longest sequence
+  int split_keys;  // (a multiple of 64)
+};
+QuantCut quant_cut(int32_t num_seqs, int32_t hkv, int32_t max_len) {
+  const int64_t groups = (int64_t)num_seqs * hkv;
+  QuantCut c{4, 1, max_len};
+  const int64_t want = std::max<int64_t>(1, 2048 / (groups * c.parts));
+  int64_t keys = std::max<int64_t>((max_len + want - 1) / want, 1024);
+  keys = std::min<int64_t>(keys, 16384);
+  keys = std::max<int64_t>(keys, (max_len + kMaxSplits - 1) / kMaxSplits);
+  c.split_keys = (int)std::min<int64_t>((keys + 255) / 256 * 256, INT32_MAX - 255);
+  c.splits = (int)(((int64_t)max_len + c.split_keys - 1) / c.split_keys);
+  return c;
+}
+
+template <int D, int BITS, int kWays>
+hipError_t launch_cut(const QuantDecodeArgs& a, const QuantCut& c, hipStream_t stream) {
+  const int64_t items = (int64_t)a.num_seqs * a.hkv * c.splits;
+  if (items * 64 * c.parts > UINT32_MAX) return hipErrorInvalidValue;
+  auto* kern = c.parts == 1 ? quant_decode_kernel<D, BITS, kWays, 1> : quant_decode_kernel<D, BITS, kWays, 4>;
+  hipLaunchKernelGGL(kern, dim3((unsigned)items), dim3(64 * c.parts), 0, stream, a);
+  const hipError_t err = hipGetLastError();
+  if (err != hipSuccess || c.splits == 1) return err;
+  const int64_t rows = (int64_t)a.num_seqs * a.hq;
+  hipLaunchKernelGGL(quant_merge_kernel<D>, dim3((unsigned)((rows + kMergeWaves - 1) / kMergeWaves)),
+                     dim3(64 * kMergeWaves), 0, stream, a);
+  return hipGetLastError();
+}
+
+template <int D, int BITS>
+hipError_t launch_ways(const QuantDecodeArgs& a, const QuantCut& c, hipStream_t stream) {
+  const int g = a.hq / a.hkv;
+  return g <= 4   ? launch_cut<D, BITS, 4>(a, c, stream)
+         : g <= 8 ? launch_cut<D, BITS, 2>(a, c, stream)
+                  : launch_cut<D, BITS, 1>(a, c, stream);
+}
+
+}  // namespace
+
+size_t quant_decode_workspace_bytes(int32_t num_seqs, int32_t hq, int32_t hkv, int32_t head_dim,
+                                    int32_t bits, int32_t max_len) {
+  const QuantCut c = quant_cut(num_seqs, hkv, max_len);
+  if (c.splits == 1) return 0;
+  return (size_t)num_seqs * hq * c.splits * (head_dim + 2) * sizeof(float);
+}
+
+hipError_t launch_quant_decode(QuantDecodeArgs a, int head_dim, int bits, void* workspace,
+                               hipStream_t stream) {
+  const QuantCut c = quant_cut(a.num_seqs, a.hkv, a.max_len);
+  a.split_keys = c.split_keys;
+  a.splits = c.splits;
+  a.by_rank = false;
+  a.order = nullptr;
+  a.ws_o = static_cast<float*>(workspace);
+  a.ws_ml = a.ws_o + (size_t)a.num_seqs * a.hq * c.splits * head_dim;
+  if (head_dim == 128)
+    return bits == 8 ? launch_ways<128, 8>(a, c, stream) : launch_ways<128, 4>(a, c, stream);
+  return bits == 8 ? launch_ways<64, 8>(a, c, stream) : launch_ways<64, 4>(a, c, stream);
+}
+
+}  // namespace pkv

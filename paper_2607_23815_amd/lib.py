@@ -47,6 +47,11 @@ class PagedKV(ctypes.Structure):
                 ("block_size", c_int32), ("num_kv_heads", c_int32), ("head_dim", c_int32)]
 
 
+class QuantKV(ctypes.Structure):
+    _fields_ = [("cache", c_void_p), ("num_blocks", c_int32), ("block_size", c_int32),
+                ("num_kv_heads", c_int32), ("head_dim", c_int32), ("bits", c_int32)]
+
+
 PKV_ROPE_MAX_AXES = 4
 
 
@@ -170,6 +175,23 @@ _SIGS = {
                                        c_float, c_void_p, c_void_p, c_void_p, c_size_t,
                                        c_void_p]),
     "pkv_sparse_workspace_bytes": (c_size_t, [c_int32] * 5),
+    "pkv_quant_block_bytes": (c_size_t, [c_int32] * 3),
+    "pkv_quant_append": (c_int32, [ctypes.POINTER(QuantKV), c_void_p, c_int64, c_void_p, c_int64,
+                                   c_void_p, c_int32, c_void_p, c_void_p, c_int32, c_int32, c_int32,
+                                   c_void_p]),
+    "pkv_quant_blocks": (c_int32, [ctypes.POINTER(PagedKV), ctypes.POINTER(QuantKV), c_void_p,
+                                   c_int32, c_void_p]),
+    "pkv_dequant_blocks": (c_int32, [ctypes.POINTER(QuantKV), ctypes.POINTER(PagedKV), c_void_p,
+                                     c_int32, c_void_p]),
+    "pkv_quant_decode_attention": (c_int32, [ctypes.POINTER(QuantKV), c_void_p, c_int32, c_void_p,
+                                             c_int32, c_void_p, c_int32, c_int32, c_float, c_void_p,
+                                             c_void_p, c_void_p, c_size_t, c_void_p]),
+    "pkv_quant_decode_workspace_bytes": (c_size_t, [c_int32] * 6),
+    "pkv_quant_prefill_attention": (c_int32, [ctypes.POINTER(QuantKV), c_void_p, c_int32, c_void_p,
+                                              c_int32, c_void_p, c_void_p, c_int32, c_int32, c_int32,
+                                              c_int32, c_float, c_void_p, c_void_p, c_void_p,
+                                              c_size_t, c_void_p]),
+    "pkv_quant_prefill_workspace_bytes": (c_size_t, [c_int32] * 8),
     "pkv_gather_kv": (c_int32, [ctypes.POINTER(PagedKV), c_void_p, c_int32, c_void_p, c_void_p,
                                 c_int32, c_int32, c_void_p, c_void_p, c_void_p]),
 }
@@ -437,15 +459,16 @@ _Tensor = None
 _raw_stream = None
 _get_device = None
 _address = _rows_address = None
-_bf16 = _i32 = _i64 = _f32 = None
+_bf16 = _i32 = _i64 = _f32 = _u8 = None
 
 
 def _get_torch():
-    global _torch, _Tensor, _raw_stream, _get_device, _bf16, _i32, _i64, _f32
+    global _torch, _Tensor, _raw_stream, _get_device, _bf16, _i32, _i64, _f32, _u8
     if _torch is None:
         import torch
         _Tensor = torch.Tensor
         _bf16, _i32, _i64, _f32 = torch.bfloat16, torch.int32, torch.int64, torch.float32
+        _u8 = torch.uint8
         _get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         _torch = torch
@@ -874,6 +897,148 @@ def pkv_sparse_attention(k_cache, v_cache, q, block_tables, row_lens, sel, scale
         _ptr(out, "out", _bf16, dev),
         None if lse is None else _ptr(lse, "lse", _f32, dev), ws, ws_bytes,
         hip_stream))
+
+
+def pkv_quant_block_bytes(num_kv_heads, head_dim, bits) -> int:
+    return int(_lib.pkv_quant_block_bytes(num_kv_heads, head_dim, bits))
+
+
+# a slab's bytes: head dim and bits
+_QUANT_SLABS = {pkv_quant_block_bytes(1, d, bits): (d, bits) for d in (64, 128) for bits in (4, 8)}
+
+
+def alloc_quant_cache(num_blocks: int, num_kv_heads: int, head_dim: int, bits: int, device="cuda"):
+    """A quantised pool's cache, uint8 [num_blocks][Hkv][slab]; the slab's size says head dim and bits."""
+    import torch
+    slab = pkv_quant_block_bytes(1, head_dim, bits)
+    if slab == 0:
+        raise ValueError("head_dim must be 64 or 128 and bits 4 or 8")
+    return torch.empty((num_blocks, num_kv_heads, slab), dtype=torch.uint8, device=device)
+
+
+def _quant_kv_on(cache, dev):
+    """The quantised pool on the current device, its kv heads, head dim and bits."""
+    shape = cache.shape
+    slab = _QUANT_SLABS.get(shape[2]) if len(shape) == 3 else None
+    if slab is None:
+        raise ValueError("cache must be [num_blocks][Hkv][slab], as alloc_quant_cache makes it")
+    d, bits = slab
+    return QuantKV(_ptr(cache, "cache", _u8, dev), shape[0], 16, shape[1], d, bits), shape[1], d, bits
+
+
+def _quant_rows(t, name, rows, heads, dim, dev):
+    p = _rows_address(t, _bf16, dev, rows, heads, dim)
+    if p is not None:
+        return p
+    if not (isinstance(t, _Tensor) and t.dtype is _bf16 and t.get_device() == dev):
+        _ptr(t, name, _bf16, dev)  # (raises)
+    raise ValueError(f"{name} must be [{rows}][{heads}][{dim}] with contiguous heads")
+
+
+def pkv_quant_append(cache, k_new, v_new, block_tables, cached_lens, cu_new_lens, max_new_len: int,
+                     stream=None) -> None:
+    """New tokens' k_new and v_new [rows][Hkv][D], whose rows may lie apart (views of one fused
+    projection), quantised into cache."""
+    dev, hip_stream = _launch_on(stream)
+    kv, hkv, d, _ = _quant_kv_on(cache, dev)
+    n, b, tables = k_new.shape[0], cached_lens.numel(), block_tables.shape
+    if len(tables) != 2 or tables[0] != b or cu_new_lens.numel() != b + 1:
+        raise ValueError("block_tables, cached_lens and cu_new_lens must have a row, an entry and "
+                         "a step per sequence")
+    kp, ks = _quant_rows(k_new, "k_new", n, hkv, d, dev)
+    vp, vs = _quant_rows(v_new, "v_new", n, hkv, d, dev)
+    _check(_lib.pkv_quant_append(
+        ctypes.byref(kv), kp, ks, vp, vs, _ptr(block_tables, "block_tables", _i32, dev), tables[1],
+        _ptr(cached_lens, "cached_lens", _i32, dev), _ptr(cu_new_lens, "cu_new_lens", _i32, dev), b, n,
+        int(max_new_len), hip_stream))
+
+
+def _pairs_ptr(pairs, dev):
+    if pairs.dim() != 2 or pairs.shape[1] != 2:
+        raise ValueError("pairs must be [n][2]")
+    return _ptr(pairs, "pairs", _i32, dev), pairs.shape[0]
+
+
+def pkv_quant_blocks(k_cache, v_cache, cache, pairs, stream=None) -> None:
+    """pairs: int32 [n][2] of (block of the bf16 pool, block of cache that takes it)."""
+    dev, hip_stream = _launch_on(stream)
+    kv = _paged_kv_on(k_cache, v_cache, dev)[0]
+    quant = _quant_kv_on(cache, dev)[0]
+    p, n = _pairs_ptr(pairs, dev)
+    _check(_lib.pkv_quant_blocks(ctypes.byref(kv), ctypes.byref(quant), p, n, hip_stream))
+
+
+def pkv_dequant_blocks(cache, k_cache, v_cache, pairs, stream=None) -> None:
+    """pairs: int32 [n][2] of (block of cache, block of the bf16 pool that takes it)."""
+    dev, hip_stream = _launch_on(stream)
+    kv = _paged_kv_on(k_cache, v_cache, dev)[0]
+    quant = _quant_kv_on(cache, dev)[0]
+    p, n = _pairs_ptr(pairs, dev)
+    _check(_lib.pkv_dequant_blocks(ctypes.byref(quant), ctypes.byref(kv), p, n, hip_stream))
+
+
+def _attended_sizes(q, out, lse, block_tables, seqs, d):
+    """Rows, query heads and table width of an attention's arrays."""
+    q_shape, tables = q.shape, block_tables.shape
+    if len(q_shape) != 3 or q_shape[2] != d or out.shape != q_shape:
+        raise ValueError("q and out must be [rows][Hq][D] of the cache's head dim")
+    if len(tables) != 2 or tables[0] != seqs:
+        raise ValueError("block_tables must be [num_seqs][max_blocks]")
+    if lse is not None and lse.shape != q_shape[:2]:
+        raise ValueError("lse must be [rows][Hq]")
+    return q_shape[0], q_shape[1], tables[1]
+
+
+def pkv_quant_decode_workspace_bytes(num_seqs, num_q_heads, num_kv_heads, head_dim, bits,
+                                     max_seq_len) -> int:
+    return int(_lib.pkv_quant_decode_workspace_bytes(num_seqs, num_q_heads, num_kv_heads, head_dim,
+                                                     bits, max_seq_len))
+
+
+def pkv_quant_decode_attention(cache, q, block_tables, seq_lens, max_seq_len: int, scale: float, out,
+                               lse=None, workspace=None, stream=None) -> None:
+    """One query per sequence, q [num_seqs][Hq][D], over its seq_lens keys in cache."""
+    dev, hip_stream = _launch_on(stream)
+    kv, hkv, d, bits = _quant_kv_on(cache, dev)
+    b = seq_lens.numel()
+    n, hq, max_blocks = _attended_sizes(q, out, lse, block_tables, b, d)
+    if n != b:
+        raise ValueError("q must have a row per entry of seq_lens")
+    if workspace is None:  # convenience for one-off calls; timed callers pass their own
+        workspace = _one_off_workspace(pkv_quant_decode_workspace_bytes(b, hq, hkv, d, bits,
+                                                                        int(max_seq_len)), stream)
+    ws, ws_bytes = _workspace(workspace, dev)
+    _check(_lib.pkv_quant_decode_attention(
+        ctypes.byref(kv), _ptr(q, "q", _bf16, dev), hq, _ptr(block_tables, "block_tables", _i32, dev),
+        max_blocks, _ptr(seq_lens, "seq_lens", _i32, dev), b, int(max_seq_len), float(scale),
+        _ptr(out, "out", _bf16, dev), None if lse is None else _ptr(lse, "lse", _f32, dev), ws, ws_bytes,
+        hip_stream))
+
+
+def pkv_quant_prefill_workspace_bytes(num_seqs, total_new, num_q_heads, num_kv_heads, head_dim, bits,
+                                      max_new_len, max_total_len) -> int:
+    return int(_lib.pkv_quant_prefill_workspace_bytes(num_seqs, total_new, num_q_heads, num_kv_heads,
+                                                      head_dim, bits, max_new_len, max_total_len))
+
+
+def pkv_quant_prefill_attention(cache, q, block_tables, cached_lens, cu_new_lens, max_new_len: int,
+                                max_total_len: int, scale: float, out, lse=None, workspace=None,
+                                stream=None) -> None:
+    """Suffix rows q [total_new][Hq][D] over their sequences' cached and new keys in cache (the new
+    ones appended before). Without a workspace the keys are not split."""
+    dev, hip_stream = _launch_on(stream)
+    kv, hkv, d, _ = _quant_kv_on(cache, dev)
+    b = cached_lens.numel()
+    n, hq, max_blocks = _attended_sizes(q, out, lse, block_tables, b, d)
+    if cu_new_lens.numel() != b + 1:
+        raise ValueError("cu_new_lens must have one entry more than cached_lens")
+    ws, ws_bytes = _workspace(workspace, dev)
+    _check(_lib.pkv_quant_prefill_attention(
+        ctypes.byref(kv), _ptr(q, "q", _bf16, dev), hq, _ptr(block_tables, "block_tables", _i32, dev),
+        max_blocks, _ptr(cached_lens, "cached_lens", _i32, dev),
+        _ptr(cu_new_lens, "cu_new_lens", _i32, dev), b, n, int(max_new_len), int(max_total_len),
+        float(scale), _ptr(out, "out", _bf16, dev),
+        None if lse is None else _ptr(lse, "lse", _f32, dev), ws, ws_bytes, hip_stream))
 
 
 def alloc_workspace(nbytes: int, device="cuda"):
