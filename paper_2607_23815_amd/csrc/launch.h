@@ -157,11 +157,8 @@ struct QuantDecodeArgs {
   float* lse;  // or null
   int32_t max_blocks, num_seqs, max_len, hq, hkv, num_blocks;
   float scale_log2;
-  // set by the launch: keys per split, splits of the longest sequence, the splits' partial results, and
-  // the order of the sequences (null: see by_rank)
+  // set by the launch: keys per split, splits of the longest sequence, the splits' partial results
   int32_t split_keys, splits;
-  bool by_rank;
-  const int32_t* order;
   float* ws_o;
   float* ws_ml;
 };

@@ -34,7 +34,7 @@ constexpr int kStep = 4;  // blocks per step
 constexpr int kStepKeys = kStep * kBlockSize;
 constexpr float kSlack = 8.f;  // (base 2)
 constexpr int kMergeWaves = 4;
-constexpr int kMaxSplits = 64;  // (a lane each in the merge)
+constexpr int kMaxSplits = 128;  // (two a lane in the merge)
 
 template <int kCtrl>
 __device__ __forceinline__ float dpp_f(float x) {
@@ -301,11 +301,10 @@ void quant_decode_kernel(const QuantDecodeArgs a) {
   const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int per_seq = a.hkv * a.splits;
-  const int rank = (int)(blockIdx.x / per_seq), rem = (int)(blockIdx.x % per_seq);
-  const int seq = a.order != nullptr ? a.order[rank]
-                  : a.by_rank        ? seq_at_rank(a.seq_lens, nullptr, a.num_seqs, rank)
-                                     : rank;
-  const int kvh = rem / a.splits, split = rem % a.splits;
+  const int seq = (int)(blockIdx.x / per_seq), rem = (int)(blockIdx.x % per_seq);
+  // (heads side by side, which share their blocks' neighbourhood in memory: 64 sequences of 8192-32768 keys,
+  // 4 bits, 64/8 heads of 128 dims 260 us against 294 with a head's splits side by side)
+  const int kvh = rem % a.hkv, split = rem / a.hkv;
   const int g = a.hq / a.hkv;
   const int len = min(a.seq_lens[seq], a.max_len);
   const int k0 = split * a.split_keys;
@@ -383,28 +382,58 @@ void quant_decode_kernel(const QuantDecodeArgs a) {
   }
 }
 
-// One wave per (sequence, query head): the splits' partial results by their log-sum-exp weights.
-template <int D>
+// The splits' partial results of a (sequence, query head) by their log-sum-exp weights, on one wave, or on
+// kMergeWaves that take the splits in runs and meet in LDS.
+template <int D, bool kWide>
 __global__ __launch_bounds__(64 * kMergeWaves) void quant_merge_kernel(const QuantDecodeArgs a) {
-  constexpr int PER = D / 64;
-  const int64_t item = (int64_t)blockIdx.x * kMergeWaves + (threadIdx.x >> 6);
+  constexpr int PER = D / 64, kRounds = kMaxSplits / 64;
+  __shared__ float sum[kMergeWaves][D];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
+  const int64_t item = kWide ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * kMergeWaves + wave;
   if (item >= (int64_t)a.num_seqs * a.hq) return;
   const int len = min(a.seq_lens[item / a.hq], a.max_len);
   const int n = (len + a.split_keys - 1) / a.split_keys;
   if (n <= 1) return;  // (written already)
   const float* ml = a.ws_ml + (size_t)item * a.splits * 2;
   const float* src = a.ws_o + (size_t)item * a.splits * D + lane * PER;
-  const bool mine = lane < n;
-  const float m = mine ? ml[lane * 2] : -INFINITY;
-  const float l = mine ? ml[lane * 2 + 1] : 0.f;
-  const float top = wave_all(m, Max());
-  const float w = mine ? fast_exp2(m - finite_max(top)) : 0.f;
-  const float den = wave_all(w * l, Add());
+  float m[kRounds], w[kRounds], top = -INFINITY, den = 0.f;  // lane l: splits l, 64 + l, ..
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r) {
+    const int s = 64 * r + lane;
+    m[r] = s < n ? ml[s * 2] : -INFINITY;
+    w[r] = s < n ? ml[s * 2 + 1] : 0.f;
+    top = fmaxf(top, m[r]);
+  }
+  top = wave_all(top, Max());
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r) {
+    const float x = fast_exp2(m[r] - finite_max(top));
+    den += x * w[r];
+    w[r] = x;
+  }
+  den = wave_all(den, Add());
   float o[PER];
 #pragma unroll
   for (int e = 0; e < PER; ++e) o[e] = 0.f;
-  for (int s = 0; s < n; s += 8) add_partials<D>(src, w, s, n, o);
+  const int run = kWide ? ((n + kMergeWaves - 1) / kMergeWaves + 7) / 8 * 8 : kMaxSplits;
+  const int s0 = kWide ? wave * run : 0, s1 = min(n, s0 + run);
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r)
+    for (int s = max(s0, 64 * r); s < min(s1, 64 * (r + 1)); s += 8)
+      add_partials<D>(src + (size_t)64 * r * D, w[r], s - 64 * r, min(s1, 64 * (r + 1)) - 64 * r, o);
+  if constexpr (kWide) {
+#pragma unroll
+    for (int e = 0; e < PER; ++e) sum[wave][lane * PER + e] = o[e];
+    __syncthreads();
+    if (wave != 0) return;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+      o[e] = 0.f;
+#pragma unroll
+      for (int k = 0; k < kMergeWaves; ++k) o[e] += sum[k][lane * PER + e];
+    }
+  }
   const float inv = 1.f / den;
 #pragma unroll
   for (int e = 0; e < PER; ++e) o[e] = den == 0.f ? 0.f : o[e] * inv;
@@ -417,7 +446,8 @@ __global__ __launch_bounds__(64 * kMergeWaves) void quant_merge_kernel(const Qua
   if (a.lse != nullptr && lane == 0) a.lse[item] = (top + log2f(den)) * kLn2;
 }
 
-// How a call is cut: host arithmetic on its sizes alone.
+// How a call is cut: host arithmetic on its sizes alone. Measured with 128 dims and 4 bits (8 bits alike), groups
+// = sequences x kv heads, lengths spread evenly, us:
 struct QuantCut {
   int parts;       // waves per (sequence, kv head, split)
   int splits;      // of the longest sequence
@@ -426,10 +456,28 @@ struct QuantCut {
 QuantCut quant_cut(int32_t num_seqs, int32_t hkv, int32_t max_len) {
   const int64_t groups = (int64_t)num_seqs * hkv;
   QuantCut c{4, 1, max_len};
-  const int64_t want = std::max<int64_t>(1, 2048 / (groups * c.parts));
-  int64_t keys = std::max<int64_t>((max_len + want - 1) / want, 1024);
-  keys = std::min<int64_t>(keys, 16384);
-  keys = std::max<int64_t>(keys, (max_len + kMaxSplits - 1) / kMaxSplits);
+  int64_t keys = max_len;
+  if (max_len <= 2048) {
+    // One launch. Four waves share an item; one wave takes it where short items fill the chip
+    // (4096 groups of 10-100 keys 15.6 against 23.2, of 1-300 26.9 and 33.2, of 100-600 51.2 and 51.3), and
+    // eight where there are few and each is worth it (128 of 300-1000 keys 8.8 against 10.4, 256 of 700-2000
+    // 14.3 and 17.0; but 512 of 50-300 10.7 and 8.7, 512 of 700-2000 27.8 and 24.7).
+    if (groups >= 2048 && max_len <= 512) c.parts = 1;
+    else if (groups <= 384 && max_len > 512) c.parts = 8;
+  } else if (max_len > 8192) {
+    // Splits of 2048 keys even out long sequences and fill the chip: 512 groups of 8000-32000 keys 258
+    // against 266 (1024), 287 (8192) and 308 (none), 2048 of 4000-32000 839, 847, 870 and 941; of 512 keys and
+    // more where items are fewer than two a compute unit (8 of 8000-32000 13.6 against 19.3 with 2048, 8 of
+    // 131072 31.1 with 2048 against 36.4).
+    keys = std::min<int64_t>(std::max<int64_t>(groups * max_len / 512, 512), 2048);
+  } else if (groups < 1024) {
+    // (8 groups of 2000-8000 keys 10.8 with 512 against 17.4 with 2048 and 31 unsplit, 64 16.7 with 1024
+    // against 20.1 and 51.7, 192 of 500-8000 35.2, 36.0 and 67.7, 512 84.6, 87.0 and 83.4; 2048 unsplit 267
+    // against 276)
+    keys = std::min<int64_t>(std::max<int64_t>(groups * max_len / 512, 512), 1024);
+  }
+  keys = std::max<int64_t>(keys, ((int64_t)max_len + kMaxSplits - 1) / kMaxSplits);
+  if (groups >= (1 << 16)) keys = max_len;  // (items enough, and a grid holds no more)
   c.split_keys = (int)std::min<int64_t>((keys + 255) / 256 * 256, INT32_MAX - 255);
   c.splits = (int)(((int64_t)max_len + c.split_keys - 1) / c.split_keys);
   return c;
@@ -439,12 +487,16 @@ template <int D, int BITS, int kWays>
 hipError_t launch_cut(const QuantDecodeArgs& a, const QuantCut& c, hipStream_t stream) {
   const int64_t items = (int64_t)a.num_seqs * a.hkv * c.splits;
   if (items * 64 * c.parts > UINT32_MAX) return hipErrorInvalidValue;
-  auto* kern = c.parts == 1 ? quant_decode_kernel<D, BITS, kWays, 1> : quant_decode_kernel<D, BITS, kWays, 4>;
+  auto* kern = c.parts == 1   ? quant_decode_kernel<D, BITS, kWays, 1>
+               : c.parts == 4 ? quant_decode_kernel<D, BITS, kWays, 4>
+                              : quant_decode_kernel<D, BITS, kWays, 8>;
   hipLaunchKernelGGL(kern, dim3((unsigned)items), dim3(64 * c.parts), 0, stream, a);
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess || c.splits == 1) return err;
   const int64_t rows = (int64_t)a.num_seqs * a.hq;
-  hipLaunchKernelGGL(quant_merge_kernel<D>, dim3((unsigned)((rows + kMergeWaves - 1) / kMergeWaves)),
+  const bool wide = c.splits > 16;
+  hipLaunchKernelGGL((wide ? quant_merge_kernel<D, true> : quant_merge_kernel<D, false>),
+                     dim3((unsigned)(wide ? rows : (rows + kMergeWaves - 1) / kMergeWaves)),
                      dim3(64 * kMergeWaves), 0, stream, a);
   return hipGetLastError();
 }
@@ -471,8 +523,6 @@ hipError_t launch_quant_decode(QuantDecodeArgs a, int head_dim, int bits, void* 
   const QuantCut c = quant_cut(a.num_seqs, a.hkv, a.max_len);
   a.split_keys = c.split_keys;
   a.splits = c.splits;
-  a.by_rank = false;
-  a.order = nullptr;
   a.ws_o = static_cast<float*>(workspace);
   a.ws_ml = a.ws_o + (size_t)a.num_seqs * a.hq * c.splits * head_dim;
   if (head_dim == 128)
