@@ -67,7 +67,7 @@ void mixed_kernel(const uint16_t* __restrict__ q, const uint16_t* __restrict__ k
           ws_o, ws_ml, d_out, d_lse, wg, sm.decode);
     }
   } else {
-    pre::prefill_body<D>(q, pre::PoolTiles{k_cache, v_cache}, block_tables, max_blocks, cached_lens,
+    pre::prefill_body<D>(q, k_cache, v_cache, block_tables, max_blocks, cached_lens,
                          cu_new_lens, num_seqs, hq, hkv, num_blocks, qtiles, scale_log2, out,
                          lse, (unsigned)((pos - before) * 8 + x), sm.prefill);
   }

@@ -25,11 +25,11 @@ void prefill_kernel(const uint16_t* __restrict__ q, const uint16_t* __restrict__
                     const int32_t* __restrict__ order, bool by_rank) {
   __shared__ __align__(16) pre::PrefillSmem<D> sm;
   if constexpr (kPlan)
-    pre::prefill_body<D>(q, pre::PoolTiles{k_cache, v_cache}, block_tables, max_blocks, cached_lens,
+    pre::prefill_body<D>(q, k_cache, v_cache, block_tables, max_blocks, cached_lens,
                          cu_new_lens, num_seqs, hq, hkv, num_blocks, qtiles, scale_log2, out,
                          lse, blockIdx.x, sm, split_keys, nsplit, ws_o, ws_ml, order, by_rank);
   else
-    pre::prefill_body<D>(q, pre::PoolTiles{k_cache, v_cache}, block_tables, max_blocks, cached_lens,
+    pre::prefill_body<D>(q, k_cache, v_cache, block_tables, max_blocks, cached_lens,
                          cu_new_lens, num_seqs, hq, hkv, num_blocks, qtiles, scale_log2, out,
                          lse, blockIdx.x, sm);
 }

@@ -131,14 +131,6 @@ struct Staging {
   }
 };
 
-// Where an item's tiles come from: the bf16 pool, whose slabs go to LDS as they are, or a cache of codes
-// (quant_prefill.hip), which a wave takes through registers and converts on their way.
-struct PoolTiles {
-  static constexpr bool kDirect = true;
-  const uint16_t* k;
-  const uint16_t* v;
-};
-
 // Q as the B operand of S^T = K Q^T: lane (lc, hh) of wave `wave` holds column
 // qt * kCols + 32 wave + lc, dims 16 kk + 8 hh .. +7. A lane past the last column reads a
 // valid row (token n - 1); the caller zeroes it before use.
@@ -159,9 +151,10 @@ __device__ __forceinline__ void load_q(const uint16_t* __restrict__ q, int hq, i
 // group, whose cached prefix is p tokens and whose n new tokens start at row row0 of q and
 // out. t_first and t_lane are entry 0 and entry `lane` of the sequence's block-table row
 // (-1 past the row).
-template <int D, typename Tiles>
+template <int D>
 __device__ __forceinline__ void prefill_item(
-    const uint16_t* __restrict__ q, const Tiles& tiles, const int32_t* __restrict__ block_tables,
+    const uint16_t* __restrict__ q, const uint16_t* __restrict__ k_cache,
+    const uint16_t* __restrict__ v_cache, const int32_t* __restrict__ block_tables,
     int32_t max_blocks, int32_t hq, int32_t hkv, int32_t num_blocks, float scale_log2,
     uint16_t* __restrict__ out, float* __restrict__ lse, const int i, const int kvh,
     const int qt, const int p, const int row0, const int n, const int32_t t_first,
@@ -247,23 +240,10 @@ __device__ __forceinline__ void prefill_item(
   };
   // One slab = one buffer resource (base = the slab, 4 KB, bounds-checked by the hardware).
   auto issue_k = [&](int kt, int buf) {
-    const int blk = block_of(kchunk, kchunk_id, kt);
-    if constexpr (Tiles::kDirect) st.issue(tiles.k, sm.k[buf], st.kofs, blk, hkv, kvh);
-    else tiles.issue_k(sm.k[buf] + slab * SLAB, blk, hkv, kvh);
+    st.issue(k_cache, sm.k[buf], st.kofs, block_of(kchunk, kchunk_id, kt), hkv, kvh);
   };
   auto issue_v = [&](int kt, int buf) {
-    const int blk = block_of(vchunk, vchunk_id, kt);
-    if constexpr (Tiles::kDirect) st.issue(tiles.v, sm.v[buf], st.vofs, blk, hkv, kvh);
-    else tiles.issue_v(sm.v[buf] + slab * SLAB, blk, hkv, kvh);
-  };
-  // Before the barrier of step kt, the codes that this wave loaded in step kt - 1 (K(kt + 1) and V(kt - 1),
-  // as far as there are such tiles) become bf16 in their place.
-  auto land = [&](bool k, int kt_k, bool v, int kt_v) {
-    if constexpr (!Tiles::kDirect) {
-      wait_vmem();
-      if (k) tiles.land_k(sm.k[kt_k & 1] + slab * SLAB);
-      if (v) tiles.land_v(sm.v[kt_v & 1] + slab * SLAB);
-    }
+    st.issue(v_cache, sm.v[buf], st.vofs, block_of(vchunk, vchunk_id, kt), hkv, kvh);
   };
 
   // lane-constant LDS read offsets (elements)
@@ -415,7 +395,6 @@ __device__ __forceinline__ void prefill_item(
   // (V(0) is loaded by the prologue, whose buffers are all free).
   auto step = [&](auto has_prev, auto has_next, int kt, f32x16 (&cur)[2], f32x16 (&nxt)[2],
                   bf16x8 (&pprev)[2][2], bf16x8 (&pcur)[2][2]) {
-    land(kt > kt0 && kt + 1 < kt_end, kt + 1, kt > kt0 + 1, kt - 1);
     wait_vmem();
     __syncthreads();  // K(kt+1) and V(kt-1) have landed; all waves are done with step kt-1
     constexpr bool HN = decltype(has_next)::value, HP = decltype(has_prev)::value;
@@ -499,17 +478,10 @@ __device__ __forceinline__ void prefill_item(
     kchunk_id = vchunk_id = kt0 / 16;
     kchunk = vchunk = load_chunk(kchunk_id);
   }
-  if constexpr (Tiles::kDirect) {
-    st.issue(tiles.k, sm.k[0], st.kofs, __builtin_amdgcn_readlane(kchunk, slab), hkv, kvh);
-    if (nt > 1)
-      st.issue(tiles.k, sm.k[1], st.kofs, __builtin_amdgcn_readlane(kchunk, 4 + slab), hkv, kvh);
-    st.issue(tiles.v, sm.v[0], st.vofs, __builtin_amdgcn_readlane(kchunk, slab), hkv, kvh);
-  } else {
-    tiles.issue_k(sm.k[0] + slab * SLAB, __builtin_amdgcn_readlane(kchunk, slab), hkv, kvh);
-    if (nt > 1)
-      tiles.issue_k(sm.k[1] + slab * SLAB, __builtin_amdgcn_readlane(kchunk, 4 + slab), hkv, kvh);
-    tiles.issue_v(sm.v[0] + slab * SLAB, __builtin_amdgcn_readlane(kchunk, slab), hkv, kvh);
-  }
+  st.issue(k_cache, sm.k[0], st.kofs, __builtin_amdgcn_readlane(kchunk, slab), hkv, kvh);
+  if (nt > 1)
+    st.issue(k_cache, sm.k[1], st.kofs, __builtin_amdgcn_readlane(kchunk, 4 + slab), hkv, kvh);
+  st.issue(v_cache, sm.v[0], st.vofs, __builtin_amdgcn_readlane(kchunk, slab), hkv, kvh);
   // Q fragments; a lane past the last column computes with zeros
   load_q<D>(q, hq, hkv, kvh, qt, row0, n, wave, lane, qf);
 #pragma unroll
@@ -517,8 +489,6 @@ __device__ __forceinline__ void prefill_item(
     const u32x4 zero = {0u, 0u, 0u, 0u};
     qf[kk] = col_ok ? qf[kk] : as_bf16x8(zero);
   }
-  land(true, 0, true, 0);
-  land(nt > 1, 1, false, 0);
   wait_vmem();
   __syncthreads();
   f32x16 sa[2], sb[2];
@@ -556,7 +526,6 @@ __device__ __forceinline__ void prefill_item(
   // product, with the weights in pa when nt is odd and in pb when it is even
   {
     const int kt = kt_end - 1;
-    land(false, 0, nt > 1, kt);
     wait_vmem();
     __syncthreads();
     if ((kt + 1) * kKeys > len) {
@@ -663,9 +632,9 @@ __device__ __forceinline__ void prefill_item(
 
 // The body of one prefill workgroup of a one-item-per-workgroup launch (the mixed launch);
 // `wg` is its index in the launch's work list.
-template <int D, typename Tiles>
-__device__ __forceinline__ void prefill_body(const uint16_t* __restrict__ q, const Tiles& tiles,
-                    const int32_t* __restrict__ block_tables,
+template <int D>
+__device__ __forceinline__ void prefill_body(const uint16_t* __restrict__ q, const uint16_t* __restrict__ k_cache,
+                    const uint16_t* __restrict__ v_cache, const int32_t* __restrict__ block_tables,
                     int32_t max_blocks, const int32_t* __restrict__ cached_lens,
                     const int32_t* __restrict__ cu_new_lens, int32_t num_seqs, int32_t hq,
                     int32_t hkv, int32_t num_blocks, int32_t qtiles, float scale_log2,
@@ -710,7 +679,7 @@ __device__ __forceinline__ void prefill_body(const uint16_t* __restrict__ q, con
   const int row0 = cu_new_lens[i];
   const int n = cu_new_lens[i + 1] - row0;
   if (qt * kCols >= n * (hq / hkv)) return;
-  prefill_item<D>(q, tiles, block_tables, max_blocks, hq, hkv, num_blocks, scale_log2,
+  prefill_item<D>(q, k_cache, v_cache, block_tables, max_blocks, hq, hkv, num_blocks, scale_log2,
                   out, lse, i, kvh, qt, p, row0, n, t_first, t_lane, sm, split_keys, sp, nsplit,
                   ws_o, ws_ml);
 }

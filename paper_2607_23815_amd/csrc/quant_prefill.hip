@@ -1,11 +1,24 @@
-// Prefix-reuse prefill attention over a cache held in 8 or 4 bits (gfx950): the items, products, softmax and
-// plan of the bf16 prefill (prefill_impl.h), on tiles that come from codes.
+// Prefix-reuse prefill attention over a cache held in 8 or 4 bits (gfx950): items, columns, tiles, lazy
+// softmax, key splits and their order as in the bf16 prefill (prefill_impl.h), on tiles that stay codes in LDS.
 //
-// A code times its scale is exact in bf16 (quant.h), so a tile in LDS is what the block's restored copy in the
-// bf16 pool would be, and the results are pkv_prefill_attention's on that copy, bit for bit. A wave loads the
-// codes of its block of a tile straight into the place of the tile in LDS, a quarter or half of it, and when
-// they have landed takes them out, and puts the block there as bf16: no registers are held through a
-// step's products, of which the softmax and the accumulators leave none.
+// What bounds the bf16 kernel is LDS: four waves read 32 KB of a tile's keys and values each per step (128 dims),
+// which takes longer than the products. Here a tile is a half or a quarter of that, and a wave takes its
+// operands from codes: a lane reads 16 bytes of a key and has four products' operands of them (two with
+// 8 bits), converted two codes an instruction beside the products, exactly (quant.h). For this
+//   - the lane of half hh supplies dims 32 (2 (kk / 4) + hh) + 8 (kk % 4) .. + 7 to score product kk, which
+//     stand side by side in the slab and under one scale; the queries are loaded in the same order;
+//   - row r of output block db is dim 16 (D / 32 (r / 16) + db) + r % 16, so that a lane's codes of a quarter
+//     block for all output blocks stand side by side.
+// A value's scale multiplies the weight of its token. The product is one where 0 times anything is 0
+// (v_mul_legacy_f32): a masked token's weight is 0, whatever its scale, so that values that read back as NaN
+// reach only the rows that see them, and slots past the sequence's end none.
+// Tiles and what is in flight at step kt: the score products of tile kt + 1, the softmax of tile kt and the value
+// products of tile kt - 1 are one block; K(kt + 2) with its tokens' value scales and V(kt) are loaded. The
+// scales outlive their keys by a step, so four buffers hold them.
+#include <math.h>
+
+#include <type_traits>
+
 #include "launch.h"
 #include "prefill_impl.h"
 #include "quant.h"
@@ -13,96 +26,14 @@
 namespace pkv {
 namespace {
 
-template <int D, int BITS>
-struct CodeTiles {
-  using S = qnt::Slab<D, BITS>;
-  static constexpr bool kDirect = false;
-  const uint8_t* cache;
+using pre::kCols;
+using pre::kKeys;
+using pre::kThreads;
+using pre::kWaves;
 
-  // The codes of one side of a block, then its scales (64 bytes of values', D / 2 of keys'), to lds.
-  template <int kScales>
-  __device__ __forceinline__ static void issue(const uint8_t* from, uint16_t* lds, int lane) {
-    uint8_t* to = reinterpret_cast<uint8_t*>(lds);
-    constexpr int kBytes = S::kCodes + kScales;
-    issue_loads<0, kBytes>(from, to, lane);
-  }
-  template <int kPart, int kBytes>
-  __device__ __forceinline__ static void issue_loads(const uint8_t* from, uint8_t* to, int lane) {
-    if constexpr ((kPart + 1) * 1024 <= kBytes)
-      lds_load16(from, kBytes, kPart * 1024 + lane * 16, to + kPart * 1024);
-    else if (lane < (kBytes - kPart * 1024) / 16)
-      lds_load16(from, kBytes, kPart * 1024 + lane * 16, to + kPart * 1024);
-    if constexpr ((kPart + 1) * 1024 < kBytes) issue_loads<kPart + 1, kBytes>(from, to, lane);
-  }
-  __device__ __forceinline__ const uint8_t* slab(int blk, int hkv, int kvh) const {
-    return cache + ((size_t)blk * hkv + kvh) * S::kBytes;
-  }
-  __device__ __forceinline__ void issue_k(uint16_t* lds, int blk, int hkv, int kvh) const {
-    issue<D / 2>(slab(blk, hkv, kvh), lds, lane_now());
-  }
-  __device__ __forceinline__ void issue_v(uint16_t* lds, int blk, int hkv, int kvh) const {
-    issue<4 * kBlockSize>(slab(blk, hkv, kvh) + S::kValues, lds, lane_now());
-  }
-
-  // (the lane index afresh where it is used, so that no address made of it is kept through the steps)
-  __device__ __forceinline__ static int lane_now() {
-    int lane;
-    asm volatile("v_and_b32 %0, 63, %1" : "=v"(lane) : "v"((int)threadIdx.x));
-    return lane;
-  }
-  // This lane's codes, from a block's in LDS. (What follows writes where other lanes read here: the fence
-  // keeps the wave's reads ahead.)
-  __device__ __forceinline__ static void take(const uint8_t* lds, int at, int stride, uint32_t* w) {
-    if constexpr (S::kLane == 8) {
-      const u32x2 x = ld8(lds + at);
-      w[0] = x[0], w[1] = x[1];
-    } else {
-#pragma unroll
-      for (int u = 0; u < S::kLane / 16; ++u) {
-        const u32x4 x = ld16(lds + at + u * stride);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[4 * u + e] = x[e];
-      }
-    }
-  }
-  __device__ __forceinline__ static void taken() {
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-  }
-  // Chunk c of slot s goes to the unit that the score product reads it from.
-  __device__ __forceinline__ void land_k(uint16_t* lds) const {
-    const int lane = lane_now();
-    const int col = lane & 15, grp = lane >> 4;
-    const uint8_t* raw = reinterpret_cast<const uint8_t*>(lds);
-    uint32_t k[S::kWords];
-    take(raw, S::kLane == 8 ? (grp / 2) * 256 + col * 16 + (grp & 1) * 8
-                            : grp * (S::kLane / 16) * 256 + col * 16, 256, k);
-    const float scale =
-        __uint_as_float((uint32_t)raw[S::kKeyScales + col * (D / 32) + grp * D / 128] << 23);
-    taken();
-    uint16_t* to = lds + (grp * (D / 32) * kBlockSize + pre::swap23(col)) * 8;
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i)
-      st16(to + i * kBlockSize * 8, qnt::eight_bf16<BITS>(k + i * BITS / 4, scale));
-  }
-  template <int kA>
-  __device__ __forceinline__ static void put_values(const uint32_t* v, const u32x4 scale, uint16_t* to) {
-    st8(to + kA * 16 * kBlockSize, qnt::four_scaled<BITS, kA>(v, scale));
-    if constexpr (kA + 1 < D / 16) put_values<kA + 1>(v, scale, to);
-  }
-  // (the half that holds slots 8 h .. of dim d is unit 2 d + (h ^ (d / 8 % 2)))
-  __device__ __forceinline__ void land_v(uint16_t* lds) const {
-    const int lane = lane_now();
-    const int col = lane & 15, grp = lane >> 4;
-    const uint8_t* raw = reinterpret_cast<const uint8_t*>(lds);
-    uint32_t v[S::kWords];
-    take(raw, lane * (S::kLane < 16 ? S::kLane : 16), 1024, v);
-    const u32x4 scale = ld16(raw + S::kCodes + 16 * grp);
-    taken();
-    put_values<0>(v, scale, lds + (2 * col + ((grp >> 1) ^ (col >> 3))) * 8 + (grp & 1) * 4);
-  }
-};
+typedef __attribute__((ext_vector_type(8))) int i32x8;
+typedef __attribute__((ext_vector_type(16))) uint32_t u32x16;
+typedef __attribute__((ext_vector_type(32))) __bf16 bf16x32;
 
 struct QuantPrefillArgs {
   const uint8_t* cache;
@@ -120,21 +51,597 @@ struct QuantPrefillArgs {
   float scale_log2;
 };
 
-// (kPlan as in prefill.hip)
-template <int D, int BITS, bool kPlan>
-__global__ __attribute__((amdgpu_flat_work_group_size(pre::kThreads, pre::kThreads),
-                          amdgpu_waves_per_eu(2, 2)))
+// (the outputs leave through the values' space, after the last product)
+template <int D, int BITS>
+struct CodeSmem {
+  using S = qnt::Slab<D, BITS>;
+  uint8_t k[2][4][S::kCodes + D / 2];  // a tile's four blocks: codes, then scales
+  uint8_t vc[2][4][S::kCodes];
+  float vs[4][kKeys];                  // value scales of tile kt in [kt % 4]
+  uint16_t v[2][4][D * kBlockSize];    // values as bf16: [dim][16 slots], halves of odd eights of dims swapped
+};
+
+// x times s, 0 where either is 0. (By the compiler's own name for the instruction and not as assembly: one that
+// takes an exponential's result has a wait state to keep, which the compiler counts for what it knows.)
+#if __HIP_DEVICE_COMPILE__
+__device__ float mul_zero(float x, float s) __asm("llvm.amdgcn.fmul.legacy");
+#else
+__device__ __forceinline__ float mul_zero(float x, float s) { return x * s; }
+#endif
+
+// kBytes bytes from the slab to LDS, 16 a lane.
+template <int kBytes, int kPart = 0>
+__device__ __forceinline__ void load_codes(const uint8_t* from, uint8_t* to, int lane) {
+  if ((kPart + 1) * 1024 <= kBytes || lane < (kBytes - kPart * 1024) / 16)
+    lds_load16(from, kBytes, kPart * 1024 + lane * 16, to + kPart * 1024);
+  if constexpr ((kPart + 1) * 1024 < kBytes) load_codes<kBytes, kPart + 1>(from, to, lane);
+}
+
+constexpr int kParts = 3;  // of a query beside 4-bit keys
+
+// The product of 4-bit codes (A) and a part of the queries (B, e2m3), 32x32x64. Lane l holds k 32 (l / 32) .. of A's
+// row and of B's column l % 32, and their scales for these in byte kA of ka and byte kB of kb.
+template <int kA, int kB>
+__device__ __forceinline__ f32x16 mfma_codes(i32x8 x, i32x8 y, f32x16 c, uint32_t ka, uint32_t kb) {
+#if __HIP_DEVICE_COMPILE__
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 2, kA, (int)ka, kB, (int)kb);
+#else
+  return c;
+#endif
+}
+
+// A group of 32 queries (16 words of bf16) in kParts parts of e2m3 and their scale bytes (byte i: part i's). The
+// group's largest magnitude is brought to 4 .. 8 by a power of two; a part is the nearest code to what the
+// parts before it leave, times 16^i. A code has 4 significant bits above 1 and steps of 1/8 below, so the parts'
+// sum is the query if that is at least 2^-6 of the group's largest, and within 2^-14 of the largest otherwise.
+// Where a query is not finite the bytes are 255, which makes the products NaN.
+__device__ __forceinline__ uint32_t query_parts(u32x16 x, i32x8 (&part)[kParts]) {
+#if __HIP_DEVICE_COMPILE__
+  uint32_t top = 0;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) top = qnt::top_of(x[e], top);
+  const uint32_t byte = max((int)(top >> 23) - 2, 9);
+#pragma unroll
+  for (int i = 0; i < kParts; ++i) {
+    const float scale = __uint_as_float((byte - 4 * i) << 23);
+    const auto code = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(__builtin_bit_cast(bf16x32, x), scale);
+#pragma unroll
+    for (int e = 0; e < 6; ++e) part[i][e] = (int)code[e];
+    part[i][6] = part[i][7] = 0;
+    const u32x16 back = __builtin_bit_cast(u32x16, __builtin_amdgcn_cvt_scalef32_pk32_bf16_fp6(code, scale));
+#pragma unroll
+    for (int e = 0; e < 16; ++e)  // (exact)
+      x[e] = pack_bf16x2(__uint_as_float(x[e] << 16) - __uint_as_float(back[e] << 16),
+                         __uint_as_float(x[e] & 0xFFFF0000u) - __uint_as_float(back[e] & 0xFFFF0000u));
+  }
+  return top >= qnt::kInfinite ? 0xFFFFFFu : byte | (byte - 4) << 8 | (byte - 8) << 16;
+#else
+  return 0u;
+#endif
+}
+
+// The queries as the score products' operands, and the products' number for a tile.
+template <int D, int BITS>
+struct Queries {  // 4 bits: dims 32 (2 u + hh) .. in parts
+  static constexpr int kProducts = D / 32 * kParts;
+  i32x8 part[D / 64][kParts];
+  uint32_t scale[D / 64];
+  __device__ __forceinline__ void load(const uint16_t* row, int hh, bool ok) {
+#pragma unroll
+    for (int u = 0; u < D / 64; ++u) {
+      u32x16 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const u32x4 y = ld16(row + u * 64 + hh * 32 + e * 8);
+#pragma unroll
+        for (int f = 0; f < 4; ++f) x[4 * e + f] = ok ? y[f] : 0u;
+      }
+      scale[u] = query_parts(x, part[u]);
+    }
+  }
+};
+template <int D>
+struct Queries<D, 8> {  // dims 32 (2 (kk / 4) + hh) + 8 (kk % 4) ..
+  static constexpr int kProducts = D / 8;
+  bf16x8 x[D / 16];
+  __device__ __forceinline__ void load(const uint16_t* row, int hh, bool ok) {
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) {
+      const u32x4 zero = {0u, 0u, 0u, 0u};
+      const u32x4 y = ld16(row + kk / 4 * 64 + hh * 32 + kk % 4 * 8);
+      x[kk] = as_bf16x8(ok ? y : zero);
+    }
+  }
+};
+
+template <int D, int BITS>
+__device__ __forceinline__ void quant_prefill_item(const QuantPrefillArgs& a, const int i, const int kvh,
+                                                   const int qt, const int p, const int row0, const int n,
+                                                   const int split, CodeSmem<D, BITS>& sm) {
+  using S = qnt::Slab<D, BITS>;
+  constexpr int DB = D / 32;   // output blocks
+  constexpr int kGroups = DB;  // groups that a tile's score products, and its value products, are issued in
+  constexpr int QOPS = Queries<D, BITS>::kProducts / kGroups, VOPS = 4;
+  const int32_t* table = a.tables + (size_t)i * a.max_blocks;
+  const int g = a.hq / a.hkv;
+  const int ncols = n * g;
+  const int col0 = qt * kCols;
+  const int len = p + n;
+  const int tid = threadIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = tid & 63, lc = lane & 31, hh = lane >> 5;
+  const int gcol = col0 + wave * 32 + lc;
+  const bool col_ok = gcol < ncols;
+  const int j = col_ok ? gcol / g : n - 1;
+  const int lim_h = p + j - 8 * hh;  // last key this column sees, less the lane's offset within a block
+  const int jmax = min(n - 1, (col0 + kCols - 1) / g);
+  const int ntiles = (p + jmax + kKeys) / kKeys;
+  const int kt0 = a.split_keys > 0 ? split * (a.split_keys / kKeys) : 0;
+  const int kt_end = a.split_keys > 0 ? min(ntiles, kt0 + a.split_keys / kKeys) : ntiles;
+  if (kt0 >= kt_end) return;  // (workgroup-uniform) an empty split
+  const int nt = kt_end - kt0;
+  const int wcol0 = col0 + wave * 32;
+  const int wj_lo = min(wcol0 / g, n - 1);
+  const bool wave_live = wcol0 < ncols;
+
+  f32x16 o[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[db][r] = 0.f;
+  float m = -INFINITY, lpart = 0.f;
+  Queries<D, BITS> qf;
+
+  // ---- blocks: 64 table entries in lane registers for the K and for the V stream, the sequence's first
+  // block (or block 0) standing in for entries past the sequence, the table or the pool ----
+  auto checked = [&](int e, int other) { return e >= 0 && e < a.num_blocks ? e : other; };
+  const int first = checked(table[0], 0);
+  auto load_chunk = [&](int c) {
+    const int e = c * 64 + lane;
+    return e < a.max_blocks && e * kBlockSize < len ? checked(table[e], first) : first;
+  };
+  int chunk_id = kt0 / 16, vchunk_id = chunk_id;
+  int kchunk = load_chunk(chunk_id), vchunk = kchunk;
+  auto block_of = [&](int& chunk, int& id, int kt) {
+    const int e = kt * 4 + wave;  // the block of tile kt that this wave loads
+    if (e >> 6 != id) {
+      id = e >> 6;
+      chunk = load_chunk(id);
+    }
+    return a.cache + ((size_t)__builtin_amdgcn_readlane(chunk, e & 63) * a.hkv + kvh) * S::kBytes;
+  };
+  auto issue_k = [&](int kt) {
+    const uint8_t* slab = block_of(kchunk, chunk_id, kt);
+    load_codes<S::kCodes + D / 2>(slab, sm.k[kt & 1][wave], lane);
+    if (lane < 4)
+      lds_load16(slab + S::kValueScales, 4 * kBlockSize, lane * 16, &sm.vs[kt & 3][wave * kBlockSize]);
+  };
+  auto issue_v = [&](int kt) {
+    load_codes<S::kCodes>(block_of(vchunk, vchunk_id, kt) + S::kValues, sm.vc[kt & 1][wave], lane);
+  };
+
+  // ---- values: the wave's own block of a tile, from codes to bf16 ----
+  const int col = lane & 15, quarter = lane >> 4;
+  uint32_t vw[S::kWords];
+  auto read_codes = [&](int kt, auto last) {
+    const uint8_t* at = &sm.vc[kt & 1][wave][lane * (S::kLane < 16 ? S::kLane : 16)];
+    if constexpr (S::kLane == 8) {
+      const u32x2 x = ld8(at);
+      vw[0] = x[0], vw[1] = x[1];
+    } else {
+#pragma unroll
+      for (int u = 0; u < S::kLane / 16; ++u) {
+        const u32x4 x = ld16(at + u * 1024);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) vw[4 * u + e] = x[e];
+      }
+    }
+    if constexpr (BITS == 8 && decltype(last)::value) {
+      // (slots past the sequence's end may hold anything; codes of 4 bits are all finite)
+      const int keep = min(max(len - kt * kKeys - wave * kBlockSize - 4 * quarter, 0), 4);
+      const uint32_t mask = keep == 4 ? ~0u : (1u << 8 * keep) - 1u;
+#pragma unroll
+      for (int e = 0; e < S::kWords; ++e) vw[e] &= mask;
+    }
+  };
+  const int v_to = (2 * col + ((quarter >> 1) ^ (col >> 3))) * 8 + (quarter & 1) * 4;
+  auto land = [&](int kt, auto part) {  // dims 16 part ..
+    constexpr int kA = decltype(part)::value;
+    st8(&sm.v[kt & 1][wave][v_to + kA * 16 * kBlockSize], qnt::four_bf16<BITS, kA>(vw));
+  };
+  auto land_some = [&](int kt, auto first, auto end) {
+    constexpr int kA = decltype(first)::value, kEnd = decltype(end)::value;
+    if constexpr (kA < kEnd) land(kt, std::integral_constant<int, kA>());
+    if constexpr (kA + 1 < kEnd) land(kt, std::integral_constant<int, kA + 1>());
+    if constexpr (kA + 2 < kEnd) land(kt, std::integral_constant<int, kA + 2>());
+    if constexpr (kA + 3 < kEnd) land(kt, std::integral_constant<int, kA + 3>());
+    static_assert(kEnd - kA <= 4, "dims of a call");
+  };
+  const int vread = (2 * lc + (hh ^ ((lc >> 3) & 1))) * 8;
+  auto value_frag = [&](int buf, int f) {
+    return ld16(&sm.v[buf][f / DB][vread + f % DB * 512]);
+  };
+
+  // ---- key operands: the lane's key of half-tile beta is block 2 beta + lc / 16, slot swap23(lc % 16)
+  // (prefill_impl.h has why) ----
+  const int slot = pre::swap23(lc & 15), blk = lc >> 4;
+  uint32_t ks[2];  // the scale bytes of groups hh and 2 + hh, in bytes 0 and 2
+  auto read_ks = [&](int buf) {
+#pragma unroll
+    for (int beta = 0; beta < 2; ++beta) {
+      const uint8_t* at = &sm.k[buf][2 * beta + blk][S::kCodes + slot * (D / 32)];
+      if constexpr (D == 128) ks[beta] = *reinterpret_cast<const uint32_t*>(at) >> (8 * hh);
+      else ks[beta] = at[hh];
+    }
+  };
+  // 16 bytes of codes: dims 32 (2 u + hh) .., 16 i further on with 8 bits
+  auto key_codes = [&](int buf, int beta, int u, int i) {
+    return ld16(&sm.k[buf][2 * beta + blk][((2 * u + hh) * (BITS / 4) + i) * 256 + slot * 16]);
+  };
+  // The score products of group kG: 4 bits take half of a half-tile's parts for each of two half-tiles in turn, 8 bits
+  // two fragments of 16 dims for each. kc holds the codes, read a group ahead.
+  u32x4 kc[2][2];
+  auto read_first_codes = [&](int buf) {
+    kc[0][0] = key_codes(buf, 0, 0, 0);
+    kc[0][1] = key_codes(buf, 1, 0, 0);
+  };
+  auto scores = [&](auto index, int buf, f32x16 (&sc)[2]) {
+    constexpr int kG = decltype(index)::value;
+    if constexpr (BITS == 4) {
+      if constexpr (D == 128 && kG == 1) {
+        kc[1][0] = key_codes(buf, 0, 1, 0);
+        kc[1][1] = key_codes(buf, 1, 1, 0);
+      }
+      auto product = [&](auto number) {  // dims 64 t / 6 .., part t / 2 % 3, half-tile t % 2
+        constexpr int t = decltype(number)::value, u = t / (2 * kParts), i = t / 2 % kParts, beta = t % 2;
+        const u32x4 c = kc[u][beta];
+        const i32x8 x = {(int)c[0], (int)c[1], (int)c[2], (int)c[3], 0, 0, 0, 0};
+        sc[beta] = mfma_codes<2 * u, i>(x, qf.part[u][i], sc[beta], ks[beta], qf.scale[u]);
+      };
+      product(std::integral_constant<int, QOPS * kG>());
+      product(std::integral_constant<int, QOPS * kG + 1>());
+      product(std::integral_constant<int, QOPS * kG + 2>());
+    } else {
+      if constexpr (kG + 1 < kGroups) {
+        kc[(kG + 1) & 1][0] = key_codes(buf, 0, (kG + 1) / 2, (kG + 1) % 2);
+        kc[(kG + 1) & 1][1] = key_codes(buf, 1, (kG + 1) / 2, (kG + 1) % 2);
+      }
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const int beta = t % 2, kk = 2 * kG + t / 2;
+        const uint32_t byte = kG < 2 ? ks[beta] & 255u : ks[beta] >> 16 & 255u;
+        const uint32_t w[2] = {kc[kG & 1][beta][t / 2 * 2], kc[kG & 1][beta][t / 2 * 2 + 1]};
+        sc[beta] = mfma32(as_bf16x8(qnt::eight_bf16<BITS>(w, __uint_as_float(byte << 23))), qf.x[kk], sc[beta]);
+      }
+    }
+  };
+
+  // register r of half-tile beta: key key0 + 32 beta + 16 (r / 8) + 8 hh + r % 8
+  auto mask_tile = [&](int key0, f32x16 (&sc)[2]) {
+    const int d = lim_h - key0;
+#pragma unroll
+    for (int beta = 0; beta < 2; ++beta)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int c = 32 * beta + 16 * (r >> 3) + (r & 7);
+        sc[beta][r] = c <= d ? sc[beta][r] : -INFINITY;
+      }
+  };
+  // a slice's four tokens' value scales: half e2 of the eight of (beta, u)
+  auto read_scales = [&](int kt, int b, int e2) {
+    return ld16(&sm.vs[kt & 3][b * kBlockSize + 8 * hh + 4 * e2]);
+  };
+  auto weight_pair = [&](const f32x16 (&sc)[2], int b, int e, const u32x4& s, float neg_m, float (&sum)[4]) {
+    const int beta = b >> 1, u = b & 1;
+    const float x = fast_exp2(__builtin_fmaf(sc[beta][8 * u + 2 * e], a.scale_log2, neg_m));
+    const float y = fast_exp2(__builtin_fmaf(sc[beta][8 * u + 2 * e + 1], a.scale_log2, neg_m));
+    sum[2 * (e & 1)] += x;
+    sum[2 * (e & 1) + 1] += y;
+    return pack_bf16x2(mul_zero(x, __uint_as_float(s[2 * (e & 1)])),
+                       mul_zero(y, __uint_as_float(s[2 * (e & 1) + 1])));
+  };
+  auto total = [](const float (&sum)[4]) {
+    return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  };
+  auto weights = [&](int kt, f32x16 (&sc)[2], bf16x8 (&pw)[2][2]) {
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      u32x4 w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const u32x4 s = read_scales(kt, b, e >> 1);
+        w[e] = weight_pair(sc, b, e, s, -m, sum);
+      }
+      pw[b >> 1][b & 1] = as_bf16x8(w);
+    }
+    return total(sum);
+  };
+
+  // The matrix-core work of a step, in groups: score products of the keys of tile kt + 1 (QK), then value
+  // products of tile kt - 1 with the weights pw (PV); beside them the sixteen slices of the softmax of cur (SM)
+  // and the landing of the wave's block of V(kt) (LAND; last: kt is the item's last tile).
+  auto block = [&](auto qk, auto pv, auto smx, auto landing, auto last, int kt, f32x16 (&sc)[2],
+                   const bf16x8 (&pw)[2][2], const f32x16 (&cur)[2], bf16x8 (&pcur)[2][2], float (&sum)[4]) {
+    constexpr bool QK = decltype(qk)::value, PV = decltype(pv)::value, SM = decltype(smx)::value;
+    constexpr bool LAND = decltype(landing)::value;
+    constexpr int GQ = QK ? kGroups : 0, NG = GQ + (PV ? kGroups : 0);
+    constexpr int SLICES = SM ? 16 / NG : 0;
+    constexpr int CHUNKS = LAND ? D / 16 : 0;
+    const int kbuf = (kt + 1) & 1, vbuf = (kt - 1) & 1;
+    const float neg_m = -m;
+    uint32_t w[4][4];
+    constexpr int QUADS = SLICES / 2;  // value scales of a group's slices, read a group ahead
+    u32x4 s[2][QUADS > 0 ? QUADS : 1];
+    u32x4 fr[8];
+    auto scales_of = [&](int index, int group) {
+#pragma unroll
+      for (int h = 0; h < QUADS; ++h) {
+        const int quad = QUADS * group + h;
+        s[index][h] = read_scales(kt, quad >> 1, quad & 1);
+      }
+    };
+    if constexpr (SM) scales_of(0, 0);
+    if constexpr (QK) {
+      read_ks(kbuf);
+      read_first_codes(kbuf);
+    }
+    if constexpr (LAND) read_codes(kt, last);
+    if constexpr (!QK) {
+#pragma unroll
+      for (int f = 0; f < 4; ++f) fr[f] = value_frag(vbuf, f);
+    }
+    auto group = [&](auto index) {
+      constexpr int G = decltype(index)::value;
+      if constexpr (SM && G + 1 < NG) scales_of((G + 1) & 1, G + 1);
+      if constexpr (G < GQ) {
+        scores(index, kbuf, sc);
+        if constexpr (PV && G == GQ - 1) {
+#pragma unroll
+          for (int f = 0; f < 4; ++f) fr[f] = value_frag(vbuf, f);
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < VOPS; ++k) {
+          const int f = (G - GQ) * VOPS + k, b = f / DB;
+          if (f + 4 < 4 * DB) fr[(f + 4) & 7] = value_frag(vbuf, f + 4);
+          o[f % DB] = mfma32(as_bf16x8(fr[f & 7]), pw[b >> 1][b & 1], o[f % DB]);
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < SLICES; ++h) {
+        const int it = SLICES * G + h;  // slice (b, e)
+        const int b = it >> 2, e = it & 3;
+        w[b][e] = weight_pair(cur, b, e, s[G & 1][h / 2], neg_m, sum);
+        asm volatile("" ::"v"(w[b][e]));  // the pack stays in this group
+      }
+      if constexpr (LAND)
+        land_some(kt, std::integral_constant<int, G * CHUNKS / NG>(),
+                  std::integral_constant<int, (G + 1) * CHUNKS / NG>());
+      constexpr int kOps = G < GQ ? QOPS : VOPS;
+      constexpr int kVec = (SM ? 9 * SLICES : 0) + 2 * CHUNKS / NG + (BITS == 8 && G < GQ ? 16 : 1);
+      if constexpr (G == 0) {  // the first operands are on their way
+        __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, kVec / 2, 0);
+      }
+#pragma unroll
+      for (int k = 0; k < kOps; ++k) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // 1 MFMA
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);  // LDS reads
+        __builtin_amdgcn_sched_group_barrier(0x002, (kVec + kOps - 1) / kOps, 0);  // vector ops
+        __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);  // an LDS write
+      }
+      // (the products stay in this group: the compiler takes them for pure, and would move them to their use)
+      if constexpr (G < GQ) asm volatile("" ::"v"(sc[0]), "v"(sc[1]));
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    using std::integral_constant;
+    group(integral_constant<int, 0>());
+    group(integral_constant<int, 1>());
+    if constexpr (NG > 2) {
+      group(integral_constant<int, 2>());
+      group(integral_constant<int, 3>());
+    }
+    if constexpr (NG > 4) {
+      group(integral_constant<int, 4>());
+      group(integral_constant<int, 5>());
+      group(integral_constant<int, 6>());
+      group(integral_constant<int, 7>());
+    }
+    if constexpr (SM) {
+#pragma unroll
+      for (int b = 0; b < 4; ++b) pcur[b >> 1][b & 1] = as_bf16x8(u32x4{w[b][0], w[b][1], w[b][2], w[b][3]});
+    }
+  };
+  auto zero_scores = [&](f32x16 (&sc)[2]) {
+#pragma unroll
+    for (int beta = 0; beta < 2; ++beta)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sc[beta][r] = 0.f;
+  };
+  using yes_t = std::true_type;
+  using no_t = std::false_type;
+
+  auto land_all = [&](int kt, auto last) {
+    read_codes(kt, last);
+    land_some(kt, std::integral_constant<int, 0>(), std::integral_constant<int, 4>());
+    if constexpr (D == 128)
+      land_some(kt, std::integral_constant<int, 4>(), std::integral_constant<int, 8>());
+  };
+  auto step = [&](auto has_prev, auto has_next, int kt, f32x16 (&cur)[2], f32x16 (&nxt)[2],
+                  bf16x8 (&pprev)[2][2], bf16x8 (&pcur)[2][2]) {
+    constexpr bool HN = decltype(has_next)::value, HP = decltype(has_prev)::value;
+    using last_t = std::integral_constant<bool, !HN>;
+    pre::wait_vmem();
+    __syncthreads();  // K(kt + 1), V(kt)'s codes and V(kt - 1) have landed; all waves are done with step kt - 1
+    if (kt + 2 < kt_end) issue_k(kt + 2);
+    if constexpr (HN) issue_v(kt + 1);
+    if (!wave_live) {
+      land_all(kt, last_t());
+      return;
+    }
+    const int key0 = kt * kKeys;
+    if (key0 + kKeys - 1 > p + wj_lo) mask_tile(key0, cur);
+    __builtin_amdgcn_s_setprio(2);
+    float lnew = 0.f;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (HN) zero_scores(nxt);
+    if constexpr (HP) {
+      block(has_next, yes_t(), yes_t(), yes_t(), last_t(), kt, nxt, pprev, cur, pcur, sum);
+      lnew = total(sum);
+    } else {
+      if constexpr (HN) block(yes_t(), no_t(), no_t(), yes_t(), last_t(), kt, nxt, pprev, cur, pcur, sum);
+      else land_all(kt, last_t());
+      const u32x4 zero = {0u, 0u, 0u, 0u};
+#pragma unroll
+      for (int b = 0; b < 4; ++b) pcur[b >> 1][b & 1] = as_bf16x8(zero);
+    }
+    asm volatile("" ::"v"(__builtin_bit_cast(u32x4, pcur[0][0])),
+                 "v"(__builtin_bit_cast(u32x4, pcur[0][1])),
+                 "v"(__builtin_bit_cast(u32x4, pcur[1][0])),
+                 "v"(__builtin_bit_cast(u32x4, pcur[1][1])), "v"(lnew));
+    __builtin_amdgcn_s_setprio(0);
+    bool check = true;
+    if constexpr (HP) check = __builtin_amdgcn_ballot_w64(!(lnew <= pre::kRescaleLimit)) != 0;
+    if (check) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int beta = 0; beta < 2; ++beta)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, cur[beta][r]);
+      mx = fmaxf(mx, pre::swap_halves(mx)) * a.scale_log2;
+      const bool grow = mx > m + pre::kRescaleThreshold;
+      if (__builtin_amdgcn_ballot_w64(grow)) {
+        const float m_new = grow ? mx : m;
+        const float alpha = fast_exp2(m - m_new);
+        m = m_new;
+        lpart *= alpha;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[db][r] *= alpha;
+        lnew = weights(kt, cur, pcur);
+      }
+    }
+    lpart += lnew;
+  };
+
+  // prologue
+  issue_k(kt0);
+  if (nt > 1) issue_k(kt0 + 1);
+  issue_v(kt0);
+  {
+    const int head = kvh * g + gcol % g;  // (a lane past the last column reads a valid row)
+    qf.load(a.q + ((size_t)(row0 + j) * a.hq + (col_ok ? head : kvh * g)) * D, hh, col_ok);
+  }
+  pre::wait_vmem();
+  __syncthreads();
+  f32x16 sa[2], sb[2];
+  bf16x8 pa[2][2], pb[2][2];
+  if (wave_live) {
+    float sum[4];
+    zero_scores(sa);
+    block(yes_t(), no_t(), no_t(), no_t(), no_t(), kt0 - 1, sa, pa, sb, pb, sum);
+  }
+  if (nt == 1) {
+    step(no_t(), no_t(), kt0, sa, sb, pb, pa);
+  } else {
+    step(no_t(), yes_t(), kt0, sa, sb, pb, pa);
+    int kt = kt0 + 1;
+    for (; kt + 2 < kt_end; kt += 2) {
+      step(yes_t(), yes_t(), kt, sb, sa, pa, pb);
+      step(yes_t(), yes_t(), kt + 1, sa, sb, pb, pa);
+    }
+    if (kt + 1 < kt_end) {
+      step(yes_t(), yes_t(), kt, sb, sa, pa, pb);
+      step(yes_t(), no_t(), kt + 1, sa, sb, pb, pa);
+    } else {
+      step(yes_t(), no_t(), kt, sb, sa, pa, pb);
+    }
+  }
+  // value products of the last tile
+  __syncthreads();
+  if (wave_live) {
+    float sum[4];
+    if (nt & 1) block(no_t(), yes_t(), no_t(), no_t(), no_t(), kt_end, sa, pa, sb, pb, sum);
+    else block(no_t(), yes_t(), no_t(), no_t(), no_t(), kt_end, sa, pb, sb, pa, sum);
+  }
+  __syncthreads();  // (the outputs take the values' space)
+
+  const float l = lpart + pre::swap_halves(lpart);
+  if (!wave_live) return;
+  constexpr int CH = D / 8;     // 16-byte units per row
+  constexpr int RPI = 64 / CH;  // rows per store
+  uint16_t* tile = &sm.v[0][0][0] + wave * 32 * D;
+  int ln;  // (the lane index afresh, so that nothing derived from it is kept through the steps)
+  asm volatile("v_and_b32 %0, 63, %1" : "=v"(ln) : "v"((int)threadIdx.x));
+  const int lcl = ln & 31, hhl = ln >> 5;
+  // registers 4 r .. 4 r + 3 of output block db: dims 32 db + 8 r + 4 hhl ..
+  auto unit = [&](int db, int r) { return 4 * db + r; };
+  if (a.split_keys > 0) {
+    const int gcp = wcol0 + lcl;
+    const int jp = gcp / g;
+    if (gcp < ncols && p + jp >= a.split_keys && p + jp >= kt0 * kKeys) {
+      const size_t at =
+          ((size_t)(row0 + jp) * a.hq + kvh * g + gcp % g) * (size_t)a.nsplit + (size_t)split;
+      float* wo = a.ws_o + at * D + 4 * hhl;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          st16(wo + 8 * unit(db, r),
+               u32x4{__float_as_uint(o[db][4 * r + 0]), __float_as_uint(o[db][4 * r + 1]),
+                     __float_as_uint(o[db][4 * r + 2]), __float_as_uint(o[db][4 * r + 3])});
+      if (hhl == 0) {
+        a.ws_ml[at * 2 + 0] = m;
+        a.ws_ml[at * 2 + 1] = l;
+      }
+    }
+    if (split > 0) return;
+  }
+  auto row_ends_here = [&](int gc) { return a.split_keys == 0 || p + gc / g < a.split_keys; };
+  const float inv = 1.f / l;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const u32x2 x = {pack_bf16x2(o[db][4 * r + 0] * inv, o[db][4 * r + 1] * inv),
+                       pack_bf16x2(o[db][4 * r + 2] * inv, o[db][4 * r + 3] * inv)};
+      st8(tile + lcl * D + (unit(db, r) ^ (lcl % CH)) * 8 + 4 * hhl, x);
+    }
+#pragma unroll
+  for (int k = 0; k < 32 / RPI; ++k) {
+    const int r = k * RPI + ln / CH;
+    const int u = ln % CH;
+    const u32x4 x = ld16(tile + r * D + ((u ^ (r % CH)) * 8));
+    const int gc = wcol0 + r;
+    if (gc < ncols && row_ends_here(gc))
+      st16_nt(a.out + ((size_t)(row0 + gc / g) * a.hq + kvh * g + gc % g) * D + u * 8, x);
+  }
+  const int gcl = wcol0 + lcl;
+  if (a.lse != nullptr && hhl == 0 && gcl < ncols && row_ends_here(gcl))
+    a.lse[(size_t)(row0 + gcl / g) * a.hq + kvh * g + gcl % g] = (m + log2f(l)) * kLn2;
+}
+
+// One item per workgroup, in the order of the bf16 prefill (prefill_body has the reasons).
+template <int D, int BITS>
+__global__ __attribute__((amdgpu_flat_work_group_size(kThreads, kThreads), amdgpu_waves_per_eu(2, 2)))
 void quant_prefill_kernel(const QuantPrefillArgs a) {
-  __shared__ __align__(16) pre::PrefillSmem<D> sm;
-  const CodeTiles<D, BITS> tiles{a.cache};
-  if constexpr (kPlan)
-    pre::prefill_body<D>(a.q, tiles, a.tables, a.max_blocks, a.cached_lens, a.cu_new_lens, a.num_seqs,
-                         a.hq, a.hkv, a.num_blocks, a.qtiles, a.scale_log2, a.out, a.lse, blockIdx.x,
-                         sm, a.split_keys, a.nsplit, a.ws_o, a.ws_ml, a.order, a.by_rank);
-  else
-    pre::prefill_body<D>(a.q, tiles, a.tables, a.max_blocks, a.cached_lens, a.cu_new_lens, a.num_seqs,
-                         a.hq, a.hkv, a.num_blocks, a.qtiles, a.scale_log2, a.out, a.lse, blockIdx.x,
-                         sm);
+  __shared__ __align__(16) CodeSmem<D, BITS> sm;
+  const int per = a.qtiles * a.nsplit;
+  const int xcd = blockIdx.x & 7, pos = blockIdx.x >> 3;
+  const int gpos = pos / per, group = gpos * 8 + xcd;
+  const int idx = (pos % per + gpos) % per;
+  const int qt = a.qtiles - 1 - idx / a.nsplit, split = idx % a.nsplit;
+  if (group >= a.num_seqs * a.hkv) return;
+  const int kvh = group % a.hkv;
+  const int i = a.order != nullptr ? a.order[group / a.hkv]
+                : a.by_rank ? seq_at_rank(a.cached_lens, a.cu_new_lens, a.num_seqs, group / a.hkv)
+                            : group / a.hkv;
+  const int p = a.cached_lens[i], row0 = a.cu_new_lens[i];
+  const int n = a.cu_new_lens[i + 1] - row0;
+  if (qt * kCols >= n * (a.hq / a.hkv)) return;
+  quant_prefill_item<D, BITS>(a, i, kvh, qt, p, row0, n, split, sm);
 }
 
 }  // namespace
@@ -183,13 +690,9 @@ hipError_t launch_quant_prefill(const uint8_t* cache, int32_t num_blocks, int32_
   a.split_keys = sp.split_keys;
   a.nsplit = sp.nsplit;
   a.scale_log2 = scale * kLog2e;
-  const bool plan = sp.order || sp.nsplit > 1;
-  auto* kern = head_dim == 128
-                   ? (bits == 8 ? (plan ? quant_prefill_kernel<128, 8, true> : quant_prefill_kernel<128, 8, false>)
-                                : (plan ? quant_prefill_kernel<128, 4, true> : quant_prefill_kernel<128, 4, false>))
-                   : (bits == 8 ? (plan ? quant_prefill_kernel<64, 8, true> : quant_prefill_kernel<64, 8, false>)
-                                : (plan ? quant_prefill_kernel<64, 4, true> : quant_prefill_kernel<64, 4, false>));
-  hipLaunchKernelGGL(kern, dim3((unsigned)pg.items), dim3(pre::kThreads), 0, stream, a);
+  auto* kern = head_dim == 128 ? (bits == 8 ? quant_prefill_kernel<128, 8> : quant_prefill_kernel<128, 4>)
+                               : (bits == 8 ? quant_prefill_kernel<64, 8> : quant_prefill_kernel<64, 4>);
+  hipLaunchKernelGGL(kern, dim3((unsigned)pg.items), dim3(kThreads), 0, stream, a);
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess || sp.nsplit <= 1) return err;
   return launch_prefill_merge(head_dim, cached_lens, cu_new_lens, num_seqs, hq, max_new_len, sp, a.ws_o,
