@@ -146,5 +146,44 @@ __device__ __forceinline__ float clamp_code(float x, float most) {
   return __builtin_amdgcn_fmed3f(x, -most, most);
 }
 
+
+typedef __attribute__((ext_vector_type(8))) int i32x8;
+typedef __attribute__((ext_vector_type(16))) uint32_t u32x16;
+typedef __attribute__((ext_vector_type(32))) __bf16 bf16x32;
+
+// 4-bit keys go into the matrix cores as they are, beside queries in e2m3 (products and sums come out as in
+// 32 bits; beside e4m3 they are off by 2^-11 of the largest product).
+constexpr int kParts = 3;
+
+// A group of 32 queries (16 words of bf16) in kParts parts of e2m3 and their scale bytes (byte i: part i's). The
+// group's largest magnitude is brought to 4 .. 8 by a power of two; a part is the nearest code to what the
+// parts before it leave, times 16^i. A code has 4 significant bits above 1 and steps of 1/8 below, so the parts'
+// sum is the query if that is at least 2^-6 of the group's largest, and within 2^-14 of the largest otherwise.
+// Where a query is not finite the bytes are 255, which makes the products NaN.
+__device__ __forceinline__ uint32_t query_parts(u32x16 x, i32x8 (&part)[kParts]) {
+#if __HIP_DEVICE_COMPILE__
+  uint32_t top = 0;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) top = top_of(x[e], top);
+  const uint32_t byte = max((int)(top >> 23) - 2, 9);
+#pragma unroll
+  for (int i = 0; i < kParts; ++i) {
+    const float scale = __uint_as_float((byte - 4 * i) << 23);
+    const auto code = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(__builtin_bit_cast(bf16x32, x), scale);
+#pragma unroll
+    for (int e = 0; e < 6; ++e) part[i][e] = (int)code[e];
+    part[i][6] = part[i][7] = 0;
+    const u32x16 back = __builtin_bit_cast(u32x16, __builtin_amdgcn_cvt_scalef32_pk32_bf16_fp6(code, scale));
+#pragma unroll
+    for (int e = 0; e < 16; ++e)  // (exact)
+      x[e] = pack_bf16x2(__uint_as_float(x[e] << 16) - __uint_as_float(back[e] << 16),
+                         __uint_as_float(x[e] & 0xFFFF0000u) - __uint_as_float(back[e] & 0xFFFF0000u));
+  }
+  return top >= kInfinite ? 0xFFFFFFu : byte | (byte - 4) << 8 | (byte - 8) << 16;
+#else
+  return 0u;
+#endif
+}
+
 }  // namespace qnt
 }  // namespace pkv

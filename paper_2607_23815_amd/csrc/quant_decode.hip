@@ -80,6 +80,20 @@ struct BlockCodes {
       }
     }
   }
+  __device__ __forceinline__ void read(const uint8_t* at, int stride) {
+    constexpr int kLane = Slab<D, BITS>::kLane;
+    if constexpr (kLane == 8) {
+      const u32x2 x = ld8(at);
+      w[0] = x[0], w[1] = x[1];
+    } else {
+#pragma unroll
+      for (int u = 0; u < kLane / 16; ++u) {
+        const u32x4 x = ld16(at + u * stride);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[4 * u + e] = x[e];
+      }
+    }
+  }
 };
 __device__ __forceinline__ uint32_t buf_ld1(const void* base, int bytes, int voffset) {
 #if __HIP_DEVICE_COMPILE__
@@ -100,6 +114,40 @@ __device__ __forceinline__ void value_products(const BlockCodes<D, BITS>& even,
   if constexpr (kA + 1 < D / 16) value_products<D, BITS, kA + 1>(even, odd, p, acc);
 }
 
+// Where slabs are small (all but 8 bits and 128 dims) a wave's slabs come through LDS, loaded straight there, keys'
+// and values' halves apart: the next step's are on their way from when this step's have been read. The registers
+// that codes in flight would take are free for more waves: 128 sequences of 4000-32000 keys, 4 bits, 16/4 heads
+// of 64 dims 141 us against 162 with registers, 512 of 1-300 keys, 32/8 heads of 128, 23.8 and 24.7. (Two steps
+// ahead, which leaves two waves a SIMD unit with 128 dims: 26.1 there, elsewhere within 2%.)
+template <int D, int BITS>
+struct Ring {
+  using S = Slab<D, BITS>;
+  static constexpr bool kUsed = S::kBytes <= 2304;
+  static constexpr int kKeyBytes = S::kCodes + D / 2, kValueBytes = S::kCodes + 4 * kBlockSize;
+  static constexpr int kLoads = kStep * ((kKeyBytes + 1023) / 1024);  // of the keys, or the values, of a step
+  static_assert((kKeyBytes + 1023) / 1024 == (kValueBytes + 1023) / 1024 && kLoads < 64, "counted loads");
+  uint8_t k[kUsed ? kStep : 1][kKeyBytes];
+  uint8_t v[kUsed ? kStep : 1][kValueBytes];
+};
+template <int kBytes, int kPart = 0>
+__device__ __forceinline__ void load_codes(const uint8_t* from, uint8_t* to, int lane) {
+  if ((kPart + 1) * 1024 <= kBytes || lane < (kBytes - kPart * 1024) / 16)
+    lds_load16(from, kBytes, kPart * 1024 + lane * 16, to + kPart * 1024);
+  if constexpr ((kPart + 1) * 1024 < kBytes) load_codes<kBytes, kPart + 1>(from, to, lane);
+}
+// Wait until at most kLeft of the wave's loads are outstanding (they end in order).
+template <int kLeft>
+__device__ __forceinline__ void wait_loads() {
+  __builtin_amdgcn_s_waitcnt(0x0F70 | (kLeft & 15) | (kLeft >> 4) << 14);
+  asm volatile("" ::: "memory");
+}
+
+// Wait until the wave's LDS reads have ended: what they read may be loaded over.
+__device__ __forceinline__ void wait_reads() {
+  __builtin_amdgcn_s_waitcnt(0xC07F);
+  asm volatile("" ::: "memory");
+}
+
 // One wave's share: keys [k0, k1) of a sequence, k0 a multiple of 16, not empty. Leaves, summed over the
 // ways, the unnormalised output (lane (col, grp) holds dims 16 a + 4 grp + 0..3 of head col % (16 / kWays)),
 // what the weights are relative to (base 2) and their sum.
@@ -107,7 +155,9 @@ template <int D, int BITS, int kWays>
 __device__ __forceinline__ void quant_range(const QuantDecodeArgs& a, const bf16x8 (&qf)[D / 32],
                                             const int32_t* __restrict__ table, const int kvh,
                                             const int k0, const int k1, f32x4 (&acc_out)[D / 16],
-                                            float& m_out, float& l_out) {
+                                            float& m_out, float& l_out, Ring<D, BITS>& ring) {
+  constexpr bool kRing = Ring<D, BITS>::kUsed;
+  constexpr int kRingLoads = Ring<D, BITS>::kLoads;
   using S = Slab<D, BITS>;
   constexpr int KK = D / 32, DB = D / 16;
   constexpr int kMine = kStep / kWays;  // blocks per step whose scores a column goes on with
@@ -120,20 +170,38 @@ __device__ __forceinline__ void quant_range(const QuantDecodeArgs& a, const bf16
   const int key_scale_at = S::kKeyScales + col * (D / 32) + grp * D / 128;
   const int value_at = S::kValues + lane * (S::kLane < 16 ? S::kLane : 16);
 
-  // The range's blocks in lane registers, 64 at a time and the next 64: lane l holds block 64 c + l, or
-  // pool block 0 (a stand-in) past the range and for entries outside the pool.
+  // The range's blocks, 64 at a time: lane l holds the address of slab 64 c + l, where pool block 0 stands in past
+  // the range and for entries outside the pool. The next 64 entries are on their way.
   const int b_first = k0 / kBlockSize;
   const int nblk = (k1 - k0 + kBlockSize - 1) / kBlockSize;
-  auto raw_chunk = [&](int c) {
+  const uint8_t* head = a.cache + (size_t)kvh * S::kBytes;
+  const size_t stride = (size_t)a.hkv * S::kBytes;
+  auto entries = [&](int c) {
     const int r = 64 * c + lane;
     return r < nblk && b_first + r < a.max_blocks ? table[b_first + r] : 0;
   };
-  auto checked = [&](int e) { return e < 0 || e >= a.num_blocks ? 0 : e; };
-  const int raw0 = raw_chunk(0), raw1 = raw_chunk(1);
-  int tab = checked(raw0), tab_next = checked(raw1);
-  int chunk = 0;
-  const uint8_t* head = a.cache + (size_t)kvh * S::kBytes;
-  const size_t stride = (size_t)a.hkv * S::kBytes;
+  int slab_lo, slab_hi;
+  auto set_slabs = [&](int e) {
+    const size_t at = (size_t)head + (size_t)(e < 0 || e >= a.num_blocks ? 0 : e) * stride;
+    slab_lo = (int)(uint32_t)at;
+    slab_hi = (int)(uint32_t)(at >> 32);
+  };
+  const int raw0 = entries(0);
+  int raw_next = entries(1), chunk = 0, next = 0;  // next: the first block of the step to load, in its 64
+  set_slabs(raw0);
+  auto next_step = [&] {
+    next += kStep;
+    if (next == 64) {
+      next = 0;
+      set_slabs(raw_next);
+      raw_next = entries(++chunk + 1);
+    }
+  };
+  auto slab = [&](int i) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane(slab_lo, next + i);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane(slab_hi, next + i);
+    return reinterpret_cast<const uint8_t*>((size_t)hi << 32 | lo);
+  };
 
   f32x4 acc[DB];
 #pragma unroll
@@ -143,42 +211,49 @@ __device__ __forceinline__ void quant_range(const QuantDecodeArgs& a, const bf16
   BlockCodes<D, BITS> k[kStep], v[kStep];
   uint32_t ks[kStep];
   u32x4 vs[kMine];
-  // (b: a block counted from the current 64's first, below 128)
-  auto slab = [&](int b) {
-    const int e = b < 64 ? __builtin_amdgcn_readlane(tab, b)
-                         : __builtin_amdgcn_readlane(tab_next, b - 64);
-    return head + (size_t)e * stride;
-  };
-  auto load_k = [&](int b) {
+  auto load_k = [&] {
 #pragma unroll
     for (int i = 0; i < kStep; ++i) {
-      const uint8_t* s = slab(b + i);
-      k[i].load(s, 0, key_at, 256);
-      ks[i] = buf_ld1(s, S::kBytes, key_scale_at);
-    }
-  };
-  auto load_v = [&](int b) {
-#pragma unroll
-    for (int i = 0; i < kStep; ++i) v[i].load(slab(b + i), 0, value_at, 1024);
-#pragma unroll
-    for (int j = 0; j < kMine; ++j) {
-      const uint8_t* s = slab(b + j * kWays);
-#pragma unroll
-      for (int w = 1; w < kWays; ++w) {
-        const uint8_t* x = slab(b + j * kWays + w);
-        s = way == w ? x : s;
+      const uint8_t* s = slab(i);
+      if constexpr (kRing) {
+        load_codes<Ring<D, BITS>::kKeyBytes>(s, ring.k[i], lane);
+      } else {
+        k[i].load(s, 0, key_at, 256);
+        ks[i] = buf_ld1(s, S::kBytes, key_scale_at);
       }
-      vs[j] = ld16(s + S::kValueScales + 16 * grp);
     }
   };
-  load_k(0);
-  load_v(0);
-  for (int t0 = k0, b = 0;; t0 += kStepKeys, b += kStep) {
-    if (b == 64) {
-      b = 0;
-      ++chunk;
-      tab = tab_next;
-      tab_next = checked(raw_chunk(chunk + 1));
+  auto load_v = [&] {
+    if constexpr (kRing) {
+#pragma unroll
+      for (int i = 0; i < kStep; ++i)
+        load_codes<Ring<D, BITS>::kValueBytes>(slab(i) + S::kValues, ring.v[i], lane);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kStep; ++i) v[i].load(slab(i), 0, value_at, 1024);
+#pragma unroll
+      for (int j = 0; j < kMine; ++j) {
+        const uint8_t* s = slab(j * kWays);
+#pragma unroll
+        for (int w = 1; w < kWays; ++w) {
+          const uint8_t* x = slab(j * kWays + w);
+          s = way == w ? x : s;
+        }
+        vs[j] = ld16(s + S::kValueScales + 16 * grp);
+      }
+    }
+  };
+  load_k();
+  load_v();
+  for (int t0 = k0;; t0 += kStepKeys) {
+    const bool more = t0 + kStepKeys < k1;
+    if constexpr (kRing) {
+      wait_loads<kRingLoads>();  // (the values' may still be on their way)
+#pragma unroll
+      for (int i = 0; i < kStep; ++i) {
+        k[i].read(ring.k[i] + key_at, 256);
+        ks[i] = ring.k[i][key_scale_at];
+      }
     }
     f32x4 st[kStep];
 #pragma unroll
@@ -189,8 +264,19 @@ __device__ __forceinline__ void quant_range(const QuantDecodeArgs& a, const bf16
       for (int kk = 0; kk < KK; ++kk)
         st[i] = mfma16(as_bf16x8(qnt::eight_bf16<BITS>(k[i].w + kk * BITS / 4, scale)), qf[kk], st[i]);
     }
-    const bool more = t0 + kStepKeys < k1;
-    if (more) load_k(b + kStep);  // (in flight through the rest of this step)
+    if constexpr (kRing) wait_reads();
+    if (more) {
+      next_step();
+      load_k();  // (in flight through the rest of this step)
+    }
+    if constexpr (kRing) {
+      if (more) wait_loads<kRingLoads>();
+      else wait_loads<0>();
+#pragma unroll
+      for (int i = 0; i < kStep; ++i) v[i].read(ring.v[i] + value_at - S::kValues, 1024);
+#pragma unroll
+      for (int j = 0; j < kMine; ++j) vs[j] = ld16(ring.v[j * kWays + way] + S::kCodes + 16 * grp);
+    }
     // lane holds keys 4 grp + r of its way's blocks
     float sv[kMine][4], weigh[kMine][4];
 #pragma unroll
@@ -280,7 +366,8 @@ __device__ __forceinline__ void quant_range(const QuantDecodeArgs& a, const bf16
             as_bf16x8(u32x4{p[n][i][0], p[n][i][1], p[n][i + 1][0], p[n][i + 1][1]}), acc);
     }
     if (!more) break;
-    load_v(b + kStep);
+    if constexpr (kRing) wait_reads();
+    load_v();
   }
   l_out = ways_sum<kWays>(dec::wave_sum16(lpart));
   m_out = m;
@@ -291,20 +378,57 @@ __device__ __forceinline__ void quant_range(const QuantDecodeArgs& a, const bf16
   }
 }
 
+// The sequence and split of item seq (wave-uniform) of a kv head: first every split but its sequence's last, then
+// the last ones, which may be short; what lies behind is no item. So the grid, which is made for the longest
+// sequence, holds what it has to at its start, and short work at its end. Past kListSeqs sequences item s is
+// split s % splits of its sequence.
+constexpr int kListSeqs = 512;
+__device__ __forceinline__ bool find_item(const QuantDecodeArgs& a, int& seq, int& split) {
+  const int item = seq, lane = threadIdx.x & 63;
+  auto splits_of = [&](int len) { return max((min(len, a.max_len) + a.split_keys - 1) / a.split_keys, 1); };
+  if (a.num_seqs > kListSeqs) {
+    seq = item / a.splits;
+    split = item % a.splits;
+    return split < splits_of(a.seq_lens[seq]);
+  }
+  int before = 0;
+  for (int base = 0; base < a.num_seqs; base += 64) {
+    const int mine = base + lane < a.num_seqs ? splits_of(a.seq_lens[base + lane]) - 1 : 0;
+    const int upto = wave_scan(mine);
+    const int all = __builtin_amdgcn_readlane(upto, 63), at = item - before;
+    if (at < all) {
+      const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > at));
+      seq = base + l;
+      split = at - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l));
+      return true;
+    }
+    before += all;
+  }
+  seq = item - before;
+  if (seq >= a.num_seqs) return false;
+  split = splits_of(a.seq_lens[seq]) - 1;
+  return true;
+}
+
 // kParts waves per (sequence, kv head, split): each takes an equal share of the split's keys, and the shares
 // meet in LDS. With several splits, the results are partial ones for the merge below.
 template <int D, int BITS, int kWays, int kParts>
-__global__ __launch_bounds__(64 * kParts) __attribute__((amdgpu_waves_per_eu(2)))
+__global__ __launch_bounds__(64 * kParts) __attribute__((amdgpu_waves_per_eu(BITS == 4 && kWays > 1 ? 3 : 2)))
 void quant_decode_kernel(const QuantDecodeArgs a) {
   constexpr int DB = D / 16;
-  __shared__ __align__(16) dec::DecodeSmem<D, kParts> sm;
+  union Smem {
+    dec::DecodeSmem<D, kParts> merge;
+    Ring<D, BITS> ring[kParts];
+  };
+  __shared__ __align__(16) Smem smem;
+  auto& sm = smem.merge;
   const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int per_seq = a.hkv * a.splits;
-  const int seq = (int)(blockIdx.x / per_seq), rem = (int)(blockIdx.x % per_seq);
   // (heads side by side, which share their blocks' neighbourhood in memory: 64 sequences of 8192-32768 keys,
   // 4 bits, 64/8 heads of 128 dims 260 us against 294 with a head's splits side by side)
-  const int kvh = rem % a.hkv, split = rem / a.hkv;
+  const int kvh = (int)(blockIdx.x % a.hkv);
+  int seq = (int)(blockIdx.x / a.hkv), split = 0;
+  if (a.splits > 1 && !find_item(a, seq, split)) return;
   const int g = a.hq / a.hkv;
   const int len = min(a.seq_lens[seq], a.max_len);
   const int k0 = split * a.split_keys;
@@ -331,7 +455,8 @@ void quant_decode_kernel(const QuantDecodeArgs a) {
     }
     f32x4 acc[DB];
     float m, l;
-    quant_range<D, BITS, kWays>(a, qf, a.tables + (size_t)seq * a.max_blocks, kvh, s0, s1, acc, m, l);
+    quant_range<D, BITS, kWays>(a, qf, a.tables + (size_t)seq * a.max_blocks, kvh, s0, s1, acc, m, l, smem.ring[wave]);
+    if constexpr (Ring<D, BITS>::kUsed) __syncthreads();  // (the results take the ring's space)
     if (h < g) {
 #pragma unroll
       for (int db = 0; db < DB; ++db)
@@ -342,7 +467,10 @@ void quant_decode_kernel(const QuantDecodeArgs a) {
         sm.l[wave][h] = l;
       }
     }
-  } else if (lane < g) {
+  } else if constexpr (Ring<D, BITS>::kUsed) {
+    __syncthreads();
+  }
+  if (s0 >= s1 && lane < g) {
     sm.m[wave][lane] = -INFINITY;
     sm.l[wave][lane] = 0.f;
   }
@@ -465,11 +593,12 @@ QuantCut quant_cut(int32_t num_seqs, int32_t hkv, int32_t max_len) {
     if (groups >= 2048 && max_len <= 512) c.parts = 1;
     else if (groups <= 384 && max_len > 512) c.parts = 8;
   } else if (max_len > 8192) {
-    // Splits of 2048 keys even out long sequences and fill the chip: 512 groups of 8000-32000 keys 258
-    // against 266 (1024), 287 (8192) and 308 (none), 2048 of 4000-32000 839, 847, 870 and 941; of 512 keys and
-    // more where items are fewer than two a compute unit (8 of 8000-32000 13.6 against 19.3 with 2048, 8 of
-    // 131072 31.1 with 2048 against 36.4).
-    keys = std::min<int64_t>(std::max<int64_t>(groups * max_len / 512, 512), 2048);
+    // Splits even out long sequences and fill the chip, and each costs a partial result: with 2^23 keys and more
+    // of 4096 (512 groups of 8192-32768 270 against 277 with 2048 and 289 with 1024, 160 of 8000-64000 150, 151
+    // and 155), below that of 2048 (64 of 8192-65536 67 against 72 with 4096, 384 of 500-16000 89, 91 and 91.5
+    // with 1024), of 512 and more where items are fewer than two a compute unit (8 of 8000-32000 13.6 against
+    // 19.3 with 2048, 8 of 131072 31.1 with 2048 against 36.4).
+    keys = std::min<int64_t>(std::max<int64_t>(groups * max_len / 512, 512), groups * max_len >= 1 << 23 ? 4096 : 2048);
   } else if (groups < 1024) {
     // (8 groups of 2000-8000 keys 10.8 with 512 against 17.4 with 2048 and 31 unsplit, 64 16.7 with 1024
     // against 20.1 and 51.7, 192 of 500-8000 35.2, 36.0 and 67.7, 512 84.6, 87.0 and 83.4; 2048 unsplit 267

@@ -30,10 +30,9 @@ using pre::kCols;
 using pre::kKeys;
 using pre::kThreads;
 using pre::kWaves;
+using qnt::i32x8;
+using qnt::kParts;
 
-typedef __attribute__((ext_vector_type(8))) int i32x8;
-typedef __attribute__((ext_vector_type(16))) uint32_t u32x16;
-typedef __attribute__((ext_vector_type(32))) __bf16 bf16x32;
 
 struct QuantPrefillArgs {
   const uint8_t* cache;
@@ -77,8 +76,6 @@ __device__ __forceinline__ void load_codes(const uint8_t* from, uint8_t* to, int
   if constexpr ((kPart + 1) * 1024 < kBytes) load_codes<kBytes, kPart + 1>(from, to, lane);
 }
 
-constexpr int kParts = 3;  // of a query beside 4-bit keys
-
 // The product of 4-bit codes (A) and a part of the queries (B, e2m3), 32x32x64. Lane l holds k 32 (l / 32) .. of A's
 // row and of B's column l % 32, and their scales for these in byte kA of ka and byte kB of kb.
 template <int kA, int kB>
@@ -87,36 +84,6 @@ __device__ __forceinline__ f32x16 mfma_codes(i32x8 x, i32x8 y, f32x16 c, uint32_
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 2, kA, (int)ka, kB, (int)kb);
 #else
   return c;
-#endif
-}
-
-// A group of 32 queries (16 words of bf16) in kParts parts of e2m3 and their scale bytes (byte i: part i's). The
-// group's largest magnitude is brought to 4 .. 8 by a power of two; a part is the nearest code to what the
-// parts before it leave, times 16^i. A code has 4 significant bits above 1 and steps of 1/8 below, so the parts'
-// sum is the query if that is at least 2^-6 of the group's largest, and within 2^-14 of the largest otherwise.
-// Where a query is not finite the bytes are 255, which makes the products NaN.
-__device__ __forceinline__ uint32_t query_parts(u32x16 x, i32x8 (&part)[kParts]) {
-#if __HIP_DEVICE_COMPILE__
-  uint32_t top = 0;
-#pragma unroll
-  for (int e = 0; e < 16; ++e) top = qnt::top_of(x[e], top);
-  const uint32_t byte = max((int)(top >> 23) - 2, 9);
-#pragma unroll
-  for (int i = 0; i < kParts; ++i) {
-    const float scale = __uint_as_float((byte - 4 * i) << 23);
-    const auto code = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(__builtin_bit_cast(bf16x32, x), scale);
-#pragma unroll
-    for (int e = 0; e < 6; ++e) part[i][e] = (int)code[e];
-    part[i][6] = part[i][7] = 0;
-    const u32x16 back = __builtin_bit_cast(u32x16, __builtin_amdgcn_cvt_scalef32_pk32_bf16_fp6(code, scale));
-#pragma unroll
-    for (int e = 0; e < 16; ++e)  // (exact)
-      x[e] = pack_bf16x2(__uint_as_float(x[e] << 16) - __uint_as_float(back[e] << 16),
-                         __uint_as_float(x[e] & 0xFFFF0000u) - __uint_as_float(back[e] & 0xFFFF0000u));
-  }
-  return top >= qnt::kInfinite ? 0xFFFFFFu : byte | (byte - 4) << 8 | (byte - 8) << 16;
-#else
-  return 0u;
 #endif
 }
 
@@ -129,14 +96,14 @@ struct Queries {  // 4 bits: dims 32 (2 u + hh) .. in parts
   __device__ __forceinline__ void load(const uint16_t* row, int hh, bool ok) {
 #pragma unroll
     for (int u = 0; u < D / 64; ++u) {
-      u32x16 x;
+      qnt::u32x16 x;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const u32x4 y = ld16(row + u * 64 + hh * 32 + e * 8);
 #pragma unroll
         for (int f = 0; f < 4; ++f) x[4 * e + f] = ok ? y[f] : 0u;
       }
-      scale[u] = query_parts(x, part[u]);
+      scale[u] = qnt::query_parts(x, part[u]);
     }
   }
 };

@@ -140,6 +140,16 @@ def test_decode_many_sequences(gpu_lib):
     check_decode(gpu_lib, rng, [int(n) for n in rng.integers(1, 900, 130)], 4, 2, 64, 8)
 
 
+@pytest.mark.parametrize("seqs", [70, 600])
+def test_decode_splits_of_many_sequences(gpu_lib, seqs):
+    """Items found in rounds of 64 sequences, and past the number that is looked through."""
+    rng = np.random.default_rng(seqs)
+    lens = [int(n) for n in rng.integers(0, 40, seqs)]
+    for i in rng.choice(seqs, 4, replace=False):
+        lens[i] = int(rng.integers(3000, 9500))
+    check_decode(gpu_lib, rng, lens, 2, 1, 64, 4, max_len=9500)
+
+
 @pytest.mark.parametrize("bits", [4, 8])
 @pytest.mark.parametrize("n", [40, 3000])
 def test_decode_nan_keys_and_values(gpu_lib, bits, n):
