@@ -50,14 +50,15 @@ struct QuantPrefillArgs {
   float scale_log2;
 };
 
+constexpr int kAhead = 4;  // fragments of values that are read ahead of their products
+
 // (the outputs leave through the values' space, after the last product)
 template <int D, int BITS>
 struct CodeSmem {
   using S = qnt::Slab<D, BITS>;
-  uint8_t k[2][4][S::kCodes + D / 2];  // a tile's four blocks: codes, then scales
-  uint8_t vc[2][4][S::kCodes];
-  float vs[4][kKeys];                  // value scales of tile kt in [kt % 4]
-  uint16_t v[2][4][D * kBlockSize];    // values as bf16: [dim][16 slots], halves of odd eights of dims swapped
+  uint8_t k[2][4][S::kCodes + D / 2];             // a tile's four blocks: codes, then scales
+  uint8_t vc[2][4][S::kCodes + 4 * kBlockSize];   // likewise
+  uint16_t v[2][4][D * kBlockSize];  // values as bf16: [dim][16 slots], halves of odd eights of dims swapped
 };
 
 // x times s, 0 where either is 0. (By the compiler's own name for the instruction and not as assembly: one that
@@ -68,12 +69,13 @@ __device__ float mul_zero(float x, float s) __asm("llvm.amdgcn.fmul.legacy");
 __device__ __forceinline__ float mul_zero(float x, float s) { return x * s; }
 #endif
 
-// kBytes bytes from the slab to LDS, 16 a lane.
-template <int kBytes, int kPart = 0>
-__device__ __forceinline__ void load_codes(const uint8_t* from, uint8_t* to, int lane) {
-  if ((kPart + 1) * 1024 <= kBytes || lane < (kBytes - kPart * 1024) / 16)
-    lds_load16(from, kBytes, kPart * 1024 + lane * 16, to + kPart * 1024);
-  if constexpr ((kPart + 1) * 1024 < kBytes) load_codes<kBytes, kPart + 1>(from, to, lane);
+// kBytes bytes, 16 a lane, from a slab of kSlab bytes to LDS (at: 16 lane from where they begin).
+template <int kBytes, int kSlab>
+__device__ __forceinline__ void load_codes(const uint8_t* slab, int at, uint8_t* to, int lane) {
+  if constexpr (kBytes >= 1024) lds_load16(slab, kSlab, at, to);
+  if constexpr (kBytes >= 2048) lds_load16<1024>(slab, kSlab, at, to);
+  constexpr int kLeft = kBytes % 1024, kAt = kBytes - kLeft;
+  if (lane < kLeft / 16) lds_load16<kAt>(slab, kSlab, at, to);
 }
 
 // The product of 4-bit codes (A) and a part of the queries (B, e2m3), 32x32x64. Lane l holds k 32 (l / 32) .. of A's
@@ -159,39 +161,39 @@ __device__ __forceinline__ void quant_prefill_item(const QuantPrefillArgs& a, co
   float m = -INFINITY, lpart = 0.f;
   Queries<D, BITS> qf;
 
-  // ---- blocks: 64 table entries in lane registers for the K and for the V stream, the sequence's first
-  // block (or block 0) standing in for entries past the sequence, the table or the pool ----
+  // ---- the wave's blocks: lane l holds the address of the slab that the wave loads of tile kt0 + 64 c + l, where
+  // the sequence's first block (or block 0) stands in past the sequence, the table and outside the pool ----
   auto checked = [&](int e, int other) { return e >= 0 && e < a.num_blocks ? e : other; };
   const int first = checked(table[0], 0);
-  auto load_chunk = [&](int c) {
-    const int e = c * 64 + lane;
-    return e < a.max_blocks && e * kBlockSize < len ? checked(table[e], first) : first;
+  int slab_lo, slab_hi;
+  auto set_slabs = [&](int from) {
+    const int e = (from + lane) * 4 + wave;
+    const int block = e < a.max_blocks && e * kBlockSize < len ? checked(table[e], first) : first;
+    const size_t at = (size_t)a.cache + ((size_t)block * a.hkv + kvh) * S::kBytes;
+    slab_lo = (int)(uint32_t)at;
+    slab_hi = (int)(uint32_t)(at >> 32);
   };
-  int chunk_id = kt0 / 16, vchunk_id = chunk_id;
-  int kchunk = load_chunk(chunk_id), vchunk = kchunk;
-  auto block_of = [&](int& chunk, int& id, int kt) {
-    const int e = kt * 4 + wave;  // the block of tile kt that this wave loads
-    if (e >> 6 != id) {
-      id = e >> 6;
-      chunk = load_chunk(id);
-    }
-    return a.cache + ((size_t)__builtin_amdgcn_readlane(chunk, e & 63) * a.hkv + kvh) * S::kBytes;
+  set_slabs(kt0);
+  const uint8_t* slab;  // of the newest tile whose keys are loaded or on their way
+  auto next_slab = [&](int kt) {
+    const int at = (kt - kt0) & 63;
+    if (at == 0 && kt != kt0) set_slabs(kt);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane(slab_lo, at);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane(slab_hi, at);
+    slab = reinterpret_cast<const uint8_t*>((size_t)hi << 32 | lo);
   };
-  auto issue_k = [&](int kt) {
-    const uint8_t* slab = block_of(kchunk, chunk_id, kt);
-    load_codes<S::kCodes + D / 2>(slab, sm.k[kt & 1][wave], lane);
-    if (lane < 4)
-      lds_load16(slab + S::kValueScales, 4 * kBlockSize, lane * 16, &sm.vs[kt & 3][wave * kBlockSize]);
+  auto issue_k = [&](auto buf) {
+    load_codes<S::kCodes + D / 2, S::kBytes>(slab, lane * 16, sm.k[buf][wave], lane);
   };
-  auto issue_v = [&](int kt) {
-    load_codes<S::kCodes>(block_of(vchunk, vchunk_id, kt) + S::kValues, sm.vc[kt & 1][wave], lane);
+  auto issue_v = [&](auto buf) {
+    load_codes<S::kCodes + 4 * kBlockSize, S::kBytes>(slab, S::kValues + lane * 16, sm.vc[buf][wave], lane);
   };
 
   // ---- values: the wave's own block of a tile, from codes to bf16 ----
   const int col = lane & 15, quarter = lane >> 4;
   uint32_t vw[S::kWords];
-  auto read_codes = [&](int kt, auto last) {
-    const uint8_t* at = &sm.vc[kt & 1][wave][lane * (S::kLane < 16 ? S::kLane : 16)];
+  auto read_codes = [&](int kt, auto buf, auto last) {
+    const uint8_t* at = &sm.vc[buf][wave][lane * (S::kLane < 16 ? S::kLane : 16)];
     if constexpr (S::kLane == 8) {
       const u32x2 x = ld8(at);
       vw[0] = x[0], vw[1] = x[1];
@@ -212,16 +214,16 @@ __device__ __forceinline__ void quant_prefill_item(const QuantPrefillArgs& a, co
     }
   };
   const int v_to = (2 * col + ((quarter >> 1) ^ (col >> 3))) * 8 + (quarter & 1) * 4;
-  auto land = [&](int kt, auto part) {  // dims 16 part ..
+  auto land = [&](auto buf, auto part) {  // dims 16 part ..
     constexpr int kA = decltype(part)::value;
-    st8(&sm.v[kt & 1][wave][v_to + kA * 16 * kBlockSize], qnt::four_bf16<BITS, kA>(vw));
+    st8(&sm.v[buf][wave][v_to + kA * 16 * kBlockSize], qnt::four_bf16<BITS, kA>(vw));
   };
-  auto land_some = [&](int kt, auto first, auto end) {
+  auto land_some = [&](auto buf, auto first, auto end) {
     constexpr int kA = decltype(first)::value, kEnd = decltype(end)::value;
-    if constexpr (kA < kEnd) land(kt, std::integral_constant<int, kA>());
-    if constexpr (kA + 1 < kEnd) land(kt, std::integral_constant<int, kA + 1>());
-    if constexpr (kA + 2 < kEnd) land(kt, std::integral_constant<int, kA + 2>());
-    if constexpr (kA + 3 < kEnd) land(kt, std::integral_constant<int, kA + 3>());
+    if constexpr (kA < kEnd) land(buf, std::integral_constant<int, kA>());
+    if constexpr (kA + 1 < kEnd) land(buf, std::integral_constant<int, kA + 1>());
+    if constexpr (kA + 2 < kEnd) land(buf, std::integral_constant<int, kA + 2>());
+    if constexpr (kA + 3 < kEnd) land(buf, std::integral_constant<int, kA + 3>());
     static_assert(kEnd - kA <= 4, "dims of a call");
   };
   const int vread = (2 * lc + (hh ^ ((lc >> 3) & 1))) * 8;
@@ -260,14 +262,14 @@ __device__ __forceinline__ void quant_prefill_item(const QuantPrefillArgs& a, co
         kc[1][1] = key_codes(buf, 1, 1, 0);
       }
       auto product = [&](auto number) {  // dims 64 t / 6 .., part t / 2 % 3, half-tile t % 2
-        constexpr int t = decltype(number)::value, u = t / (2 * kParts), i = t / 2 % kParts, beta = t % 2;
+        constexpr int t = 3 * kG + decltype(number)::value, u = t / (2 * kParts), i = t / 2 % kParts, beta = t % 2;
         const u32x4 c = kc[u][beta];
         const i32x8 x = {(int)c[0], (int)c[1], (int)c[2], (int)c[3], 0, 0, 0, 0};
         sc[beta] = mfma_codes<2 * u, i>(x, qf.part[u][i], sc[beta], ks[beta], qf.scale[u]);
       };
-      product(std::integral_constant<int, QOPS * kG>());
-      product(std::integral_constant<int, QOPS * kG + 1>());
-      product(std::integral_constant<int, QOPS * kG + 2>());
+      product(std::integral_constant<int, 0>());
+      product(std::integral_constant<int, 1>());
+      product(std::integral_constant<int, 2>());
     } else {
       if constexpr (kG + 1 < kGroups) {
         kc[(kG + 1) & 1][0] = key_codes(buf, 0, (kG + 1) / 2, (kG + 1) % 2);
@@ -295,8 +297,8 @@ __device__ __forceinline__ void quant_prefill_item(const QuantPrefillArgs& a, co
       }
   };
   // a slice's four tokens' value scales: half e2 of the eight of (beta, u)
-  auto read_scales = [&](int kt, int b, int e2) {
-    return ld16(&sm.vs[kt & 3][b * kBlockSize + 8 * hh + 4 * e2]);
+  auto read_scales = [&](int buf, int b, int e2) {
+    return ld16(&sm.vc[buf][b][S::kCodes + 4 * (8 * hh + 4 * e2)]);
   };
   auto weight_pair = [&](const f32x16 (&sc)[2], int b, int e, const u32x4& s, float neg_m, float (&sum)[4]) {
     const int beta = b >> 1, u = b & 1;
@@ -310,32 +312,33 @@ __device__ __forceinline__ void quant_prefill_item(const QuantPrefillArgs& a, co
   auto total = [](const float (&sum)[4]) {
     return (sum[0] + sum[1]) + (sum[2] + sum[3]);
   };
-  auto weights = [&](int kt, f32x16 (&sc)[2], bf16x8 (&pw)[2][2]) {
+  auto weights = [&](int buf, f32x16 (&sc)[2], bf16x8 (&pw)[2][2]) {
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
       u32x4 w;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const u32x4 s = read_scales(kt, b, e >> 1);
+        const u32x4 s = read_scales(buf, b, e >> 1);
         w[e] = weight_pair(sc, b, e, s, -m, sum);
       }
       pw[b >> 1][b & 1] = as_bf16x8(w);
+      __builtin_amdgcn_sched_barrier(0);  // (registers for one block's scales)
     }
     return total(sum);
   };
 
-  // The matrix-core work of a step, in groups: score products of the keys of tile kt + 1 (QK), then value
-  // products of tile kt - 1 with the weights pw (PV); beside them the sixteen slices of the softmax of cur (SM)
+  // The matrix-core work of a step, in groups: value products of tile kt - 1 with the weights pw (PV), then score
+  // products of the keys of tile kt + 1 (QK), which take the registers that pw leaves; beside them the sixteen slices of the softmax of cur (SM)
   // and the landing of the wave's block of V(kt) (LAND; last: kt is the item's last tile).
-  auto block = [&](auto qk, auto pv, auto smx, auto landing, auto last, int kt, f32x16 (&sc)[2],
+  auto block = [&](auto qk, auto pv, auto smx, auto landing, auto last, int kt, auto buf, f32x16 (&sc)[2],
                    const bf16x8 (&pw)[2][2], const f32x16 (&cur)[2], bf16x8 (&pcur)[2][2], float (&sum)[4]) {
     constexpr bool QK = decltype(qk)::value, PV = decltype(pv)::value, SM = decltype(smx)::value;
     constexpr bool LAND = decltype(landing)::value;
-    constexpr int GQ = QK ? kGroups : 0, NG = GQ + (PV ? kGroups : 0);
+    constexpr int GV = PV ? kGroups : 0, NG = GV + (QK ? kGroups : 0);
     constexpr int SLICES = SM ? 16 / NG : 0;
     constexpr int CHUNKS = LAND ? D / 16 : 0;
-    const int kbuf = (kt + 1) & 1, vbuf = (kt - 1) & 1;
+    constexpr int kbuf = 1 - decltype(buf)::value, vbuf = kbuf;
     const float neg_m = -m;
     uint32_t w[4][4];
     constexpr int QUADS = SLICES / 2;  // value scales of a group's slices, read a group ahead
@@ -345,35 +348,35 @@ __device__ __forceinline__ void quant_prefill_item(const QuantPrefillArgs& a, co
 #pragma unroll
       for (int h = 0; h < QUADS; ++h) {
         const int quad = QUADS * group + h;
-        s[index][h] = read_scales(kt, quad >> 1, quad & 1);
+        s[index][h] = read_scales(buf, quad >> 1, quad & 1);
       }
     };
     if constexpr (SM) scales_of(0, 0);
-    if constexpr (QK) {
+    if constexpr (PV) {
+#pragma unroll
+      for (int f = 0; f < kAhead; ++f) fr[f] = value_frag(vbuf, f);
+    } else {
       read_ks(kbuf);
       read_first_codes(kbuf);
     }
-    if constexpr (LAND) read_codes(kt, last);
-    if constexpr (!QK) {
-#pragma unroll
-      for (int f = 0; f < 4; ++f) fr[f] = value_frag(vbuf, f);
-    }
+    if constexpr (LAND) read_codes(kt, buf, last);
+    using std::integral_constant;
     auto group = [&](auto index) {
       constexpr int G = decltype(index)::value;
       if constexpr (SM && G + 1 < NG) scales_of((G + 1) & 1, G + 1);
-      if constexpr (G < GQ) {
-        scores(index, kbuf, sc);
-        if constexpr (PV && G == GQ - 1) {
-#pragma unroll
-          for (int f = 0; f < 4; ++f) fr[f] = value_frag(vbuf, f);
-        }
-      } else {
+      if constexpr (G < GV) {
 #pragma unroll
         for (int k = 0; k < VOPS; ++k) {
-          const int f = (G - GQ) * VOPS + k, b = f / DB;
-          if (f + 4 < 4 * DB) fr[(f + 4) & 7] = value_frag(vbuf, f + 4);
+          const int f = G * VOPS + k, b = f / DB;
+          if (f + kAhead < 4 * DB) fr[(f + kAhead) & 7] = value_frag(vbuf, f + kAhead);
           o[f % DB] = mfma32(as_bf16x8(fr[f & 7]), pw[b >> 1][b & 1], o[f % DB]);
         }
+        if constexpr (QK && G == GV - 1) {
+          read_ks(kbuf);
+          read_first_codes(kbuf);
+        }
+      } else {
+        scores(integral_constant<int, G - GV>(), kbuf, sc);
       }
 #pragma unroll
       for (int h = 0; h < SLICES; ++h) {
@@ -383,10 +386,10 @@ __device__ __forceinline__ void quant_prefill_item(const QuantPrefillArgs& a, co
         asm volatile("" ::"v"(w[b][e]));  // the pack stays in this group
       }
       if constexpr (LAND)
-        land_some(kt, std::integral_constant<int, G * CHUNKS / NG>(),
+        land_some(buf, std::integral_constant<int, G * CHUNKS / NG>(),
                   std::integral_constant<int, (G + 1) * CHUNKS / NG>());
-      constexpr int kOps = G < GQ ? QOPS : VOPS;
-      constexpr int kVec = (SM ? 9 * SLICES : 0) + 2 * CHUNKS / NG + (BITS == 8 && G < GQ ? 16 : 1);
+      constexpr int kOps = G < GV ? VOPS : QOPS;
+      constexpr int kVec = (SM ? 9 * SLICES : 0) + 2 * CHUNKS / NG + (BITS == 8 && G >= GV ? 16 : 1);
       if constexpr (G == 0) {  // the first operands are on their way
         __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
         __builtin_amdgcn_sched_group_barrier(0x002, kVec / 2, 0);
@@ -399,10 +402,9 @@ __device__ __forceinline__ void quant_prefill_item(const QuantPrefillArgs& a, co
         __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);  // an LDS write
       }
       // (the products stay in this group: the compiler takes them for pure, and would move them to their use)
-      if constexpr (G < GQ) asm volatile("" ::"v"(sc[0]), "v"(sc[1]));
+      if constexpr (G >= GV) asm volatile("" ::"v"(sc[0]), "v"(sc[1]));
       __builtin_amdgcn_sched_barrier(0);
     };
-    using std::integral_constant;
     group(integral_constant<int, 0>());
     group(integral_constant<int, 1>());
     if constexpr (NG > 2) {
@@ -429,22 +431,25 @@ __device__ __forceinline__ void quant_prefill_item(const QuantPrefillArgs& a, co
   using yes_t = std::true_type;
   using no_t = std::false_type;
 
-  auto land_all = [&](int kt, auto last) {
-    read_codes(kt, last);
-    land_some(kt, std::integral_constant<int, 0>(), std::integral_constant<int, 4>());
+  auto land_all = [&](int kt, auto buf, auto last) {
+    read_codes(kt, buf, last);
+    land_some(buf, std::integral_constant<int, 0>(), std::integral_constant<int, 4>());
     if constexpr (D == 128)
-      land_some(kt, std::integral_constant<int, 4>(), std::integral_constant<int, 8>());
+      land_some(buf, std::integral_constant<int, 4>(), std::integral_constant<int, 8>());
   };
-  auto step = [&](auto has_prev, auto has_next, int kt, f32x16 (&cur)[2], f32x16 (&nxt)[2],
+  auto step = [&](auto has_prev, auto has_next, int kt, auto buf, f32x16 (&cur)[2], f32x16 (&nxt)[2],
                   bf16x8 (&pprev)[2][2], bf16x8 (&pcur)[2][2]) {
     constexpr bool HN = decltype(has_next)::value, HP = decltype(has_prev)::value;
     using last_t = std::integral_constant<bool, !HN>;
     pre::wait_vmem();
     __syncthreads();  // K(kt + 1), V(kt)'s codes and V(kt - 1) have landed; all waves are done with step kt - 1
-    if (kt + 2 < kt_end) issue_k(kt + 2);
-    if constexpr (HN) issue_v(kt + 1);
+    if constexpr (HN) issue_v(std::integral_constant<int, 1 - decltype(buf)::value>());
+    if (kt + 2 < kt_end) {
+      next_slab(kt + 2);
+      issue_k(buf);
+    }
     if (!wave_live) {
-      land_all(kt, last_t());
+      land_all(kt, buf, last_t());
       return;
     }
     const int key0 = kt * kKeys;
@@ -454,11 +459,11 @@ __device__ __forceinline__ void quant_prefill_item(const QuantPrefillArgs& a, co
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
     if constexpr (HN) zero_scores(nxt);
     if constexpr (HP) {
-      block(has_next, yes_t(), yes_t(), yes_t(), last_t(), kt, nxt, pprev, cur, pcur, sum);
+      block(has_next, yes_t(), yes_t(), yes_t(), last_t(), kt, buf, nxt, pprev, cur, pcur, sum);
       lnew = total(sum);
     } else {
-      if constexpr (HN) block(yes_t(), no_t(), no_t(), yes_t(), last_t(), kt, nxt, pprev, cur, pcur, sum);
-      else land_all(kt, last_t());
+      if constexpr (HN) block(yes_t(), no_t(), no_t(), yes_t(), last_t(), kt, buf, nxt, pprev, cur, pcur, sum);
+      else land_all(kt, buf, last_t());
       const u32x4 zero = {0u, 0u, 0u, 0u};
 #pragma unroll
       for (int b = 0; b < 4; ++b) pcur[b >> 1][b & 1] = as_bf16x8(zero);
@@ -487,16 +492,22 @@ __device__ __forceinline__ void quant_prefill_item(const QuantPrefillArgs& a, co
         for (int db = 0; db < DB; ++db)
 #pragma unroll
           for (int r = 0; r < 16; ++r) o[db][r] *= alpha;
-        lnew = weights(kt, cur, pcur);
+        lnew = weights(buf, cur, pcur);
       }
     }
     lpart += lnew;
   };
 
   // prologue
-  issue_k(kt0);
-  if (nt > 1) issue_k(kt0 + 1);
-  issue_v(kt0);
+  using even_t = std::integral_constant<int, 0>;  // (tile kt's buffers are those of kt - kt0's parity)
+  using odd_t = std::integral_constant<int, 1>;
+  next_slab(kt0);
+  issue_k(even_t());
+  issue_v(even_t());
+  if (nt > 1) {
+    next_slab(kt0 + 1);
+    issue_k(odd_t());
+  }
   {
     const int head = kvh * g + gcol % g;  // (a lane past the last column reads a valid row)
     qf.load(a.q + ((size_t)(row0 + j) * a.hq + (col_ok ? head : kvh * g)) * D, hh, col_ok);
@@ -508,30 +519,30 @@ __device__ __forceinline__ void quant_prefill_item(const QuantPrefillArgs& a, co
   if (wave_live) {
     float sum[4];
     zero_scores(sa);
-    block(yes_t(), no_t(), no_t(), no_t(), no_t(), kt0 - 1, sa, pa, sb, pb, sum);
+    block(yes_t(), no_t(), no_t(), no_t(), no_t(), kt0 - 1, odd_t(), sa, pa, sb, pb, sum);
   }
   if (nt == 1) {
-    step(no_t(), no_t(), kt0, sa, sb, pb, pa);
+    step(no_t(), no_t(), kt0, even_t(), sa, sb, pb, pa);
   } else {
-    step(no_t(), yes_t(), kt0, sa, sb, pb, pa);
+    step(no_t(), yes_t(), kt0, even_t(), sa, sb, pb, pa);
     int kt = kt0 + 1;
     for (; kt + 2 < kt_end; kt += 2) {
-      step(yes_t(), yes_t(), kt, sb, sa, pa, pb);
-      step(yes_t(), yes_t(), kt + 1, sa, sb, pb, pa);
+      step(yes_t(), yes_t(), kt, odd_t(), sb, sa, pa, pb);
+      step(yes_t(), yes_t(), kt + 1, even_t(), sa, sb, pb, pa);
     }
     if (kt + 1 < kt_end) {
-      step(yes_t(), yes_t(), kt, sb, sa, pa, pb);
-      step(yes_t(), no_t(), kt + 1, sa, sb, pb, pa);
+      step(yes_t(), yes_t(), kt, odd_t(), sb, sa, pa, pb);
+      step(yes_t(), no_t(), kt + 1, even_t(), sa, sb, pb, pa);
     } else {
-      step(yes_t(), no_t(), kt, sb, sa, pa, pb);
+      step(yes_t(), no_t(), kt, odd_t(), sb, sa, pa, pb);
     }
   }
   // value products of the last tile
   __syncthreads();
   if (wave_live) {
     float sum[4];
-    if (nt & 1) block(no_t(), yes_t(), no_t(), no_t(), no_t(), kt_end, sa, pa, sb, pb, sum);
-    else block(no_t(), yes_t(), no_t(), no_t(), no_t(), kt_end, sa, pb, sb, pa, sum);
+    if (nt & 1) block(no_t(), yes_t(), no_t(), no_t(), no_t(), kt_end, odd_t(), sa, pa, sb, pb, sum);
+    else block(no_t(), yes_t(), no_t(), no_t(), no_t(), kt_end, even_t(), sa, pb, sb, pa, sum);
   }
   __syncthreads();  // (the outputs take the values' space)
 
