@@ -574,7 +574,8 @@ pkv_status pkv_dequant_blocks(const pkv_quant_kv* from, const pkv_paged_kv* to, 
  * weights reach the value product within 2^-16 of themselves; bf16 output. A key or value that reads
  * back as NaN makes NaN of the heads that see it. workspace: at least pkv_quant_decode_workspace_bytes (0
  * where there are items enough to fill the chip), 16-byte aligned, owned by the caller, not read
- * back; calls that share one must not overlap. num_seqs * num_kv_heads stays below 2^22. */
+ * back; calls that share one must not overlap. num_seqs * num_kv_heads stays below 2^22, max_seq_len at
+ * most 2^30. */
 pkv_status pkv_quant_decode_attention(const pkv_quant_kv* kv, const void* q, int32_t num_q_heads,
                                       const int32_t* block_tables, int32_t max_blocks,
                                       const int32_t* seq_lens, int32_t num_seqs,
@@ -584,8 +585,10 @@ size_t pkv_quant_decode_workspace_bytes(int32_t num_seqs, int32_t num_q_heads, i
                                         int32_t head_dim, int32_t bits, int32_t max_seq_len);
 
 /* Prefix-reuse prefill attention over the quantised cache, the new tokens appended before: with
- * pkv_prefill_attention's arguments, optional workspace and plan, and its results on a bf16 pool that holds
- * what the codes stand for (pkv_dequant_blocks), bit for bit. */
+ * pkv_prefill_attention's arguments, optional workspace and plan, over what the codes stand for. 32-bit sums; a
+ * weight times its token's value scale is rounded to bf16 once. Beside 4-bit keys a query is exact where it is at
+ * least 2^-6 of the largest of its 32 dims, and within 2^-14 of the largest otherwise. A key or value that reads
+ * back as NaN makes NaN of the rows that see it, and of no other. max_total_len is at most 2^30. */
 pkv_status pkv_quant_prefill_attention(const pkv_quant_kv* kv, const void* q, int32_t num_q_heads,
                                        const int32_t* block_tables, int32_t max_blocks,
                                        const int32_t* cached_lens, const int32_t* cu_new_lens,

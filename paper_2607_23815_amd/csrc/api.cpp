@@ -912,6 +912,7 @@ pkv_status pkv_quant_decode_attention(const pkv_quant_kv* kv, const void* q, int
     return fail(PKV_ERR_INVALID_ARG, f + ": max_seq_len, max_blocks must be > 0");
   if ((int64_t)max_blocks * kSupportedBlockSize < max_seq_len)
     return fail(PKV_ERR_INVALID_ARG, f + ": max_seq_len exceeds max_blocks * block_size");
+  if (max_seq_len > (1 << 30)) return fail(PKV_ERR_INVALID_ARG, f + ": max_seq_len above 2^30");
   if (!(scale > 0.f)) return fail(PKV_ERR_INVALID_ARG, f + ": scale <= 0");
   if ((int64_t)num_seqs * view.hkv > kMaxRowItems)
     return fail(PKV_ERR_INVALID_ARG, f + ": 2^22 sequences x kv heads or more");
@@ -970,6 +971,8 @@ pkv_status pkv_quant_prefill_attention(const pkv_quant_kv* kv, const void* q, in
                      num_seqs, total_new, max_new_len, max_total_len, scale, out, workspace,
                      workspace_bytes, &empty);
   if (st != PKV_OK || empty) return st;
+  if (max_total_len > (1 << 30))
+    return fail(PKV_ERR_INVALID_ARG, std::string(fn) + ": max_total_len above 2^30");
   const hipStream_t s = static_cast<hipStream_t>(stream);
   {
     const MetaCheck c = meta(kMetaPrefill, shape, block_tables, max_blocks, cached_lens, cu_new_lens,

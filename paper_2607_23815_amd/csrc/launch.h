@@ -188,8 +188,6 @@ struct PrefillSplit {
   int32_t nsplit;
   bool order;
 };
-// Sequences up to which every wave ranks them for itself (at most kRankSeqs).
-constexpr int32_t kPrefillRankSeqs = 16;
 PrefillSplit prefill_split_plan(int32_t num_seqs, int32_t hq, int32_t hkv, int32_t max_new_len,
                                 int32_t max_total_len);
 // Workspace of the plan (0 when it needs none): the sequence order when ordered, then when
@@ -204,12 +202,6 @@ hipError_t launch_prefill(const KvView& kv, const uint16_t* q, int32_t hq,
                           int32_t num_seqs, int32_t total_new, int32_t max_new_len,
                           int32_t max_total_len, float scale, uint16_t* out, float* lse,
                           void* workspace, hipStream_t stream);
-
-// The merge of a split prefill's partial results (prefill_split_plan has the split).
-hipError_t launch_prefill_merge(int32_t head_dim, const int32_t* cached_lens,
-                                const int32_t* cu_new_lens, int32_t num_seqs, int32_t hq,
-                                int32_t max_new_len, const PrefillSplit& sp, const float* ws_o,
-                                const float* ws_ml, uint16_t* out, float* lse, hipStream_t stream);
 
 size_t decode_workspace_bytes(int32_t num_seqs, int32_t hq, int32_t hkv, int32_t head_dim,
                               int32_t max_seq_len);

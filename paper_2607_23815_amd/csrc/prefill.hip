@@ -97,6 +97,7 @@ constexpr int32_t kMaxSplits = 64;
 // kernel and one more dependent load per workgroup): with documents up to 16k keys the
 // longest items would otherwise start anywhere in the launch and extend its end.
 constexpr int32_t kOrderKeys = 8192;
+constexpr int32_t kRankSeqsPrefill = 16;  // at most kRankSeqs
 
 PrefillSplit prefill_split_plan(int32_t num_seqs, int32_t hq, int32_t hkv, int32_t max_new_len,
                                 int32_t max_total_len) {
@@ -125,20 +126,6 @@ size_t prefill_workspace_bytes(int32_t num_seqs, int32_t total_new, int32_t hq, 
   return bytes;
 }
 
-hipError_t launch_prefill_merge(int32_t head_dim, const int32_t* cached_lens,
-                                const int32_t* cu_new_lens, int32_t num_seqs, int32_t hq,
-                                int32_t max_new_len, const PrefillSplit& sp, const float* ws_o,
-                                const float* ws_ml, uint16_t* out, float* lse, hipStream_t stream) {
-  const dim3 mgrid((unsigned)(((int64_t)max_new_len * hq + 3) / 4), (unsigned)num_seqs);
-  if (head_dim == 128)
-    hipLaunchKernelGGL(prefill_merge_kernel<128>, mgrid, dim3(256), 0, stream, cached_lens,
-                       cu_new_lens, hq, sp.split_keys, sp.nsplit, ws_o, ws_ml, out, lse);
-  else
-    hipLaunchKernelGGL(prefill_merge_kernel<64>, mgrid, dim3(256), 0, stream, cached_lens,
-                       cu_new_lens, hq, sp.split_keys, sp.nsplit, ws_o, ws_ml, out, lse);
-  return hipGetLastError();
-}
-
 hipError_t launch_prefill(const KvView& kv, const uint16_t* q, int32_t hq,
                           const int32_t* block_tables, int32_t max_blocks,
                           const int32_t* cached_lens, const int32_t* cu_new_lens,
@@ -156,7 +143,7 @@ hipError_t launch_prefill(const KvView& kv, const uint16_t* q, int32_t hq,
   // 9-20k keys 114.8 us against 117.2 with the ordering launch, 4 of 24-32k 342 against 343; at
   // 64 the ranking in every workgroup of a long launch costs more than the ordering launch (1708
   // us against 1686).
-  const bool by_rank = sp.order && num_seqs <= kPrefillRankSeqs;
+  const bool by_rank = sp.order && num_seqs <= kRankSeqsPrefill;
   if (by_rank) {
     ws += order_bytes(num_seqs);
   } else if (sp.order) {
@@ -183,8 +170,14 @@ hipError_t launch_prefill(const KvView& kv, const uint16_t* q, int32_t hq,
                      ws_ml, order, by_rank);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess || sp.nsplit <= 1) return err;
-  return launch_prefill_merge(kv.head_dim, cached_lens, cu_new_lens, num_seqs, hq, max_new_len, sp,
-                              ws_o, ws_ml, out, lse, stream);
+  const dim3 mgrid((unsigned)(((int64_t)max_new_len * hq + 3) / 4), (unsigned)num_seqs);
+  if (kv.head_dim == 128)
+    hipLaunchKernelGGL(prefill_merge_kernel<128>, mgrid, dim3(256), 0, stream, cached_lens,
+                       cu_new_lens, hq, sp.split_keys, sp.nsplit, ws_o, ws_ml, out, lse);
+  else
+    hipLaunchKernelGGL(prefill_merge_kernel<64>, mgrid, dim3(256), 0, stream, cached_lens,
+                       cu_new_lens, hq, sp.split_keys, sp.nsplit, ws_o, ws_ml, out, lse);
+  return hipGetLastError();
 }
 
 }  // namespace pkv

@@ -1,20 +1,24 @@
 // Prefix-reuse prefill attention over a cache held in 8 or 4 bits (gfx950): items, columns, tiles, lazy
-// softmax, key splits and their order as in the bf16 prefill (prefill_impl.h), on tiles that stay codes in LDS.
+// softmax, key splits and their order as in the bf16 prefill (prefill_impl.h), on tiles that arrive as codes.
 //
-// What bounds the bf16 kernel is LDS: four waves read 32 KB of a tile's keys and values each per step (128 dims),
-// which takes longer than the products. Here a tile is a half or a quarter of that, and a wave takes its
-// operands from codes: a lane reads 16 bytes of a key and has four products' operands of them (two with
-// 8 bits), converted two codes an instruction beside the products, exactly (quant.h). For this
-//   - the lane of half hh supplies dims 32 (2 (kk / 4) + hh) + 8 (kk % 4) .. + 7 to score product kk, which
-//     stand side by side in the slab and under one scale; the queries are loaded in the same order;
-//   - row r of output block db is dim 16 (D / 32 (r / 16) + db) + r % 16, so that a lane's codes of a quarter
-//     block for all output blocks stand side by side.
-// A value's scale multiplies the weight of its token. The product is one where 0 times anything is 0
-// (v_mul_legacy_f32): a masked token's weight is 0, whatever its scale, so that values that read back as NaN
+// What bounds the bf16 kernel is vector work beside the products, and codes that every wave converts for itself
+// are as much again (48 suffixes of 64-401 tokens over 500-3500, 4 bits, 32/8 heads of 128 dims: 483 us against
+// 440 in bf16). So
+//   - values become bf16 once a workgroup: a wave converts its block of a tile, two codes an instruction, from
+//     where it arrived in LDS to where all waves read it, beside the products of a step (418 us);
+//   - 4-bit keys are not converted: they and their groups' powers of two are operands of the matrix cores'
+//     4-bit products as they lie in the slab, and the queries are taken in three parts of 6 bits (quant.h). The
+//     three products take 3/4 of the bf16 ones' time, and come out as in 32 bits;
+//   - 8-bit keys have no such partner (products of 8-bit codes are off by 2^-11 of the largest one), and a wave
+//     converts its operands, exactly, a lane having dims 32 (2 (kk / 4) + hh) + 8 (kk % 4) .. of score product kk,
+//     which lie side by side and under one scale.
+// A value's scale multiplies the weight of its token, before its rounding to bf16. The product is one where 0
+// times anything is 0: a masked token's weight is 0 whatever its scale, so that values that read back as NaN
 // reach only the rows that see them, and slots past the sequence's end none.
-// Tiles and what is in flight at step kt: the score products of tile kt + 1, the softmax of tile kt and the value
-// products of tile kt - 1 are one block; K(kt + 2) with its tokens' value scales and V(kt) are loaded. The
-// scales outlive their keys by a step, so four buffers hold them.
+// Step kt: value products of tile kt - 1, the softmax of tile kt, score products of tile kt + 1 and the conversion
+// of V(kt) are one block; K(kt + 2) and the codes of V(kt + 1) are loaded. Of the case above the step's vector
+// work is 1.2 times the bf16 kernel's (32 products with scales), its time 415 us against 415-440 (928 TFLOP/s);
+// with 64 dims, where vector work weighs more, 1.16 times the bf16 kernel's.
 #include <math.h>
 
 #include <type_traits>
@@ -25,6 +29,8 @@
 
 namespace pkv {
 namespace {
+
+constexpr int32_t kMostRanked = 16;  // sequences up to which every wave ranks them for itself (seq_at_rank)
 
 using pre::kCols;
 using pre::kKeys;
@@ -50,8 +56,6 @@ struct QuantPrefillArgs {
   float scale_log2;
 };
 
-constexpr int kAhead = 4;  // fragments of values that are read ahead of their products
-
 // (the outputs leave through the values' space, after the last product)
 template <int D, int BITS>
 struct CodeSmem {
@@ -61,13 +65,16 @@ struct CodeSmem {
   uint16_t v[2][4][D * kBlockSize];  // values as bf16: [dim][16 slots], halves of odd eights of dims swapped
 };
 
-// x times s, 0 where either is 0. (By the compiler's own name for the instruction and not as assembly: one that
-// takes an exponential's result has a wait state to keep, which the compiler counts for what it knows.)
+// The lane index afresh where it is used, so that nothing made of it is kept in registers through the steps.
+__device__ __forceinline__ int lane_now() {
 #if __HIP_DEVICE_COMPILE__
-__device__ float mul_zero(float x, float s) __asm("llvm.amdgcn.fmul.legacy");
+  int lane;
+  asm volatile("v_and_b32 %0, 63, %1" : "=v"(lane) : "v"((int)threadIdx.x));
+  return lane;
 #else
-__device__ __forceinline__ float mul_zero(float x, float s) { return x * s; }
+  return 0;
 #endif
+}
 
 // kBytes bytes, 16 a lane, from a slab of kSlab bytes to LDS (at: 16 lane from where they begin).
 template <int kBytes, int kSlab>
@@ -130,6 +137,8 @@ __device__ __forceinline__ void quant_prefill_item(const QuantPrefillArgs& a, co
   using S = qnt::Slab<D, BITS>;
   constexpr int DB = D / 32;   // output blocks
   constexpr int kGroups = DB;  // groups that a tile's score products, and its value products, are issued in
+  constexpr int kAhead = D == 64 ? 4 : 3;  // fragments of values read ahead of their products
+  constexpr int kSums = D == 64 ? 4 : 2;  // partial sums of weights (as many as registers allow)
   constexpr int QOPS = Queries<D, BITS>::kProducts / kGroups, VOPS = 4;
   const int32_t* table = a.tables + (size_t)i * a.max_blocks;
   const int g = a.hq / a.hkv;
@@ -161,32 +170,28 @@ __device__ __forceinline__ void quant_prefill_item(const QuantPrefillArgs& a, co
   float m = -INFINITY, lpart = 0.f;
   Queries<D, BITS> qf;
 
-  // ---- the wave's blocks: lane l holds the address of the slab that the wave loads of tile kt0 + 64 c + l, where
-  // the sequence's first block (or block 0) stands in past the sequence, the table and outside the pool ----
+  // ---- the wave's blocks: lane l holds the one that the wave loads of tile kt0 + 64 c + l, where the sequence's
+  // first block (or block 0) stands in past the sequence, the table and outside the pool ----
   auto checked = [&](int e, int other) { return e >= 0 && e < a.num_blocks ? e : other; };
   const int first = checked(table[0], 0);
-  int slab_lo, slab_hi;
-  auto set_slabs = [&](int from) {
-    const int e = (from + lane) * 4 + wave;
-    const int block = e < a.max_blocks && e * kBlockSize < len ? checked(table[e], first) : first;
-    const size_t at = (size_t)a.cache + ((size_t)block * a.hkv + kvh) * S::kBytes;
-    slab_lo = (int)(uint32_t)at;
-    slab_hi = (int)(uint32_t)(at >> 32);
+  auto blocks_from = [&](int kt) {
+    const int e = (kt + lane_now()) * 4 + wave;
+    return e < a.max_blocks && e * kBlockSize < len ? checked(table[e], first) : first;
   };
-  set_slabs(kt0);
+  int blocks = blocks_from(kt0);
   const uint8_t* slab;  // of the newest tile whose keys are loaded or on their way
   auto next_slab = [&](int kt) {
     const int at = (kt - kt0) & 63;
-    if (at == 0 && kt != kt0) set_slabs(kt);
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane(slab_lo, at);
-    const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane(slab_hi, at);
-    slab = reinterpret_cast<const uint8_t*>((size_t)hi << 32 | lo);
+    if (at == 0 && kt != kt0) blocks = blocks_from(kt);
+    slab = a.cache + ((size_t)__builtin_amdgcn_readlane(blocks, at) * a.hkv + kvh) * S::kBytes;
   };
   auto issue_k = [&](auto buf) {
-    load_codes<S::kCodes + D / 2, S::kBytes>(slab, lane * 16, sm.k[buf][wave], lane);
+    const int ln = D == 64 ? lane : lane_now();  // (128 dims leave no register for it)
+    load_codes<S::kCodes + D / 2, S::kBytes>(slab, ln * 16, sm.k[buf][wave], ln);
   };
   auto issue_v = [&](auto buf) {
-    load_codes<S::kCodes + 4 * kBlockSize, S::kBytes>(slab, S::kValues + lane * 16, sm.vc[buf][wave], lane);
+    const int ln = D == 64 ? lane : lane_now();
+    load_codes<S::kCodes + 4 * kBlockSize, S::kBytes>(slab, S::kValues + ln * 16, sm.vc[buf][wave], ln);
   };
 
   // ---- values: the wave's own block of a tile, from codes to bf16 ----
@@ -239,7 +244,7 @@ __device__ __forceinline__ void quant_prefill_item(const QuantPrefillArgs& a, co
 #pragma unroll
     for (int beta = 0; beta < 2; ++beta) {
       const uint8_t* at = &sm.k[buf][2 * beta + blk][S::kCodes + slot * (D / 32)];
-      if constexpr (D == 128) ks[beta] = *reinterpret_cast<const uint32_t*>(at) >> (8 * hh);
+      if constexpr (D == 128) ks[beta] = *reinterpret_cast<const uint32_t*>(at) >> (lane_now() >> 2 & 8);
       else ks[beta] = at[hh];
     }
   };
@@ -247,8 +252,8 @@ __device__ __forceinline__ void quant_prefill_item(const QuantPrefillArgs& a, co
   auto key_codes = [&](int buf, int beta, int u, int i) {
     return ld16(&sm.k[buf][2 * beta + blk][((2 * u + hh) * (BITS / 4) + i) * 256 + slot * 16]);
   };
-  // The score products of group kG: 4 bits take half of a half-tile's parts for each of two half-tiles in turn, 8 bits
-  // two fragments of 16 dims for each. kc holds the codes, read a group ahead.
+  // The score products of group kG of kGroups. 4 bits: product t takes dims 64 (t / 6) .., part t / 2 % 3 of the
+  // queries, half-tile t % 2; 8 bits: dims 16 of kk = 2 kG + t / 2, half-tile t % 2. kc: codes, read ahead.
   u32x4 kc[2][2];
   auto read_first_codes = [&](int buf) {
     kc[0][0] = key_codes(buf, 0, 0, 0);
@@ -300,20 +305,21 @@ __device__ __forceinline__ void quant_prefill_item(const QuantPrefillArgs& a, co
   auto read_scales = [&](int buf, int b, int e2) {
     return ld16(&sm.vc[buf][b][S::kCodes + 4 * (8 * hh + 4 * e2)]);
   };
-  auto weight_pair = [&](const f32x16 (&sc)[2], int b, int e, const u32x4& s, float neg_m, float (&sum)[4]) {
+  auto weight_pair = [&](const f32x16 (&sc)[2], int b, int e, const u32x4& s, float neg_m, float (&sum)[kSums]) {
     const int beta = b >> 1, u = b & 1;
     const float x = fast_exp2(__builtin_fmaf(sc[beta][8 * u + 2 * e], a.scale_log2, neg_m));
     const float y = fast_exp2(__builtin_fmaf(sc[beta][8 * u + 2 * e + 1], a.scale_log2, neg_m));
-    sum[2 * (e & 1)] += x;
-    sum[2 * (e & 1) + 1] += y;
-    return pack_bf16x2(mul_zero(x, __uint_as_float(s[2 * (e & 1)])),
-                       mul_zero(y, __uint_as_float(s[2 * (e & 1) + 1])));
+    sum[2 * e % kSums] += x;
+    sum[(2 * e + 1) % kSums] += y;
+    return pack_bf16x2(qnt::mul_zero(x, __uint_as_float(s[2 * (e & 1)])),
+                       qnt::mul_zero(y, __uint_as_float(s[2 * (e & 1) + 1])));
   };
-  auto total = [](const float (&sum)[4]) {
-    return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  auto total = [&](const float (&sum)[kSums]) {
+    if constexpr (kSums == 2) return sum[0] + sum[1];
+    else return (sum[0] + sum[1]) + (sum[2] + sum[3]);
   };
   auto weights = [&](int buf, f32x16 (&sc)[2], bf16x8 (&pw)[2][2]) {
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    float sum[kSums] = {};
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
       u32x4 w;
@@ -332,7 +338,7 @@ __device__ __forceinline__ void quant_prefill_item(const QuantPrefillArgs& a, co
   // products of the keys of tile kt + 1 (QK), which take the registers that pw leaves; beside them the sixteen slices of the softmax of cur (SM)
   // and the landing of the wave's block of V(kt) (LAND; last: kt is the item's last tile).
   auto block = [&](auto qk, auto pv, auto smx, auto landing, auto last, int kt, auto buf, f32x16 (&sc)[2],
-                   const bf16x8 (&pw)[2][2], const f32x16 (&cur)[2], bf16x8 (&pcur)[2][2], float (&sum)[4]) {
+                   const bf16x8 (&pw)[2][2], const f32x16 (&cur)[2], bf16x8 (&pcur)[2][2], float (&sum)[kSums]) {
     constexpr bool QK = decltype(qk)::value, PV = decltype(pv)::value, SM = decltype(smx)::value;
     constexpr bool LAND = decltype(landing)::value;
     constexpr int GV = PV ? kGroups : 0, NG = GV + (QK ? kGroups : 0);
@@ -456,7 +462,7 @@ __device__ __forceinline__ void quant_prefill_item(const QuantPrefillArgs& a, co
     if (key0 + kKeys - 1 > p + wj_lo) mask_tile(key0, cur);
     __builtin_amdgcn_s_setprio(2);
     float lnew = 0.f;
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    float sum[kSums] = {};
     if constexpr (HN) zero_scores(nxt);
     if constexpr (HP) {
       block(has_next, yes_t(), yes_t(), yes_t(), last_t(), kt, buf, nxt, pprev, cur, pcur, sum);
@@ -517,7 +523,7 @@ __device__ __forceinline__ void quant_prefill_item(const QuantPrefillArgs& a, co
   f32x16 sa[2], sb[2];
   bf16x8 pa[2][2], pb[2][2];
   if (wave_live) {
-    float sum[4];
+    float sum[kSums];
     zero_scores(sa);
     block(yes_t(), no_t(), no_t(), no_t(), no_t(), kt0 - 1, odd_t(), sa, pa, sb, pb, sum);
   }
@@ -540,7 +546,7 @@ __device__ __forceinline__ void quant_prefill_item(const QuantPrefillArgs& a, co
   // value products of the last tile
   __syncthreads();
   if (wave_live) {
-    float sum[4];
+    float sum[kSums];
     if (nt & 1) block(no_t(), yes_t(), no_t(), no_t(), no_t(), kt_end, odd_t(), sa, pa, sb, pb, sum);
     else block(no_t(), yes_t(), no_t(), no_t(), no_t(), kt_end, even_t(), sa, pb, sb, pa, sum);
   }
@@ -551,8 +557,7 @@ __device__ __forceinline__ void quant_prefill_item(const QuantPrefillArgs& a, co
   constexpr int CH = D / 8;     // 16-byte units per row
   constexpr int RPI = 64 / CH;  // rows per store
   uint16_t* tile = &sm.v[0][0][0] + wave * 32 * D;
-  int ln;  // (the lane index afresh, so that nothing derived from it is kept through the steps)
-  asm volatile("v_and_b32 %0, 63, %1" : "=v"(ln) : "v"((int)threadIdx.x));
+  const int ln = lane_now();
   const int lcl = ln & 31, hhl = ln >> 5;
   // registers 4 r .. 4 r + 3 of output block db: dims 32 db + 8 r + 4 hhl ..
   auto unit = [&](int db, int r) { return 4 * db + r; };
@@ -622,6 +627,37 @@ void quant_prefill_kernel(const QuantPrefillArgs a) {
   quant_prefill_item<D, BITS>(a, i, kvh, qt, p, row0, n, split, sm);
 }
 
+// The splits' partial results of a row that reaches past split 0 (sequence blockIdx.y, one wave per query head)
+// by their log-sum-exp weights.
+template <int D>
+__global__ __launch_bounds__(kThreads) void quant_prefill_merge_kernel(const QuantPrefillArgs a) {
+  constexpr int PER = D / 64;
+  const int i = blockIdx.y, lane = threadIdx.x & 63;
+  const int r = (int)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row0 = a.cu_new_lens[i], n = a.cu_new_lens[i + 1] - row0;
+  const int j = r / a.hq;
+  if (j >= n) return;
+  const int splits = (a.cached_lens[i] + j) / a.split_keys + 1;  // that the row reaches
+  if (splits == 1) return;                                       // (written already)
+  const size_t row = (size_t)(row0 + j) * a.hq + r % a.hq, at = row * a.nsplit;
+  const float m = lane < splits ? a.ws_ml[(at + lane) * 2] : -INFINITY;
+  const float l = lane < splits ? a.ws_ml[(at + lane) * 2 + 1] : 0.f;
+  const float top = wave_all(m, Max());
+  const float w = lane < splits ? fast_exp2(m - top) : 0.f;
+  const float den = wave_all(w * l, Add());
+  float o[PER];
+#pragma unroll
+  for (int e = 0; e < PER; ++e) o[e] = 0.f;
+  const float* src = a.ws_o + at * D + lane * PER;
+  for (int s = 0; s < splits; s += 8) add_partials<D>(src, w, s, splits, o);
+  const float inv = 1.f / den;
+  uint16_t* to = a.out + row * D + lane * PER;
+  const uint32_t pair = pack_bf16x2(o[0] * inv, o[PER - 1] * inv);
+  if constexpr (PER == 2) *reinterpret_cast<uint32_t*>(to) = pair;
+  else *to = (uint16_t)pair;
+  if (a.lse != nullptr && lane == 0) a.lse[row] = (top + log2f(den)) * kLn2;
+}
+
 }  // namespace
 
 hipError_t launch_quant_prefill(const uint8_t* cache, int32_t num_blocks, int32_t hkv, int32_t head_dim,
@@ -643,7 +679,7 @@ hipError_t launch_quant_prefill(const uint8_t* cache, int32_t num_blocks, int32_
   a.out = out;
   a.lse = lse;
   char* ws = static_cast<char*>(workspace);
-  a.by_rank = sp.order && num_seqs <= kPrefillRankSeqs;
+  a.by_rank = sp.order && num_seqs <= kMostRanked;
   if (sp.order) {
     if (!a.by_rank) {
       int32_t* order = reinterpret_cast<int32_t*>(ws);
@@ -673,8 +709,10 @@ hipError_t launch_quant_prefill(const uint8_t* cache, int32_t num_blocks, int32_
   hipLaunchKernelGGL(kern, dim3((unsigned)pg.items), dim3(kThreads), 0, stream, a);
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess || sp.nsplit <= 1) return err;
-  return launch_prefill_merge(head_dim, cached_lens, cu_new_lens, num_seqs, hq, max_new_len, sp, a.ws_o,
-                              a.ws_ml, out, lse, stream);
+  hipLaunchKernelGGL((head_dim == 128 ? quant_prefill_merge_kernel<128> : quant_prefill_merge_kernel<64>),
+                     dim3((unsigned)(((int64_t)max_new_len * hq + kWaves - 1) / kWaves), (unsigned)num_seqs),
+                     dim3(kThreads), 0, stream, a);
+  return hipGetLastError();
 }
 
 }  // namespace pkv

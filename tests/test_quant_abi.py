@@ -124,6 +124,7 @@ def test_decode_refuses(lib):
                 dict(max_len=1025), dict(scale=0.0), dict(scale=float("nan")), dict(scale=-1.0),
                 dict(num_seqs=2**21 + 1)):
         refused(lib, arg, _decode(lib, **bad), "pkv_quant_decode_attention")
+    refused(lib, arg, _decode(lib, num_seqs=1, max_len=2**30 + 1, max_blocks=2**27), "2^30")
     for bad in (dict(hq=7), dict(hq=0), dict(hq=34)):
         refused(lib, shape, _decode(lib, **bad), "num_q_heads")
     need = lib.pkv_quant_decode_workspace_bytes(1, 8, 2, 128, 4, 2**20)
@@ -142,6 +143,7 @@ def test_prefill_refuses(lib):
                 dict(max_total=19), dict(max_blocks=62), dict(scale=0.0), dict(num_seqs=65536)):
         refused(lib, arg, _prefill(lib, **bad), "pkv_quant_prefill_attention")
     refused(lib, shape, _prefill(lib, hq=7), "num_q_heads")
+    refused(lib, arg, _prefill(lib, max_total=2**30 + 1, max_blocks=2**27), "2^30")
     long = dict(num_seqs=1, max_total=16000)
     need = lib.pkv_quant_prefill_workspace_bytes(1, 50, 8, 2, 128, 4, 20, 16000)
     assert need == lib.pkv_prefill_workspace_bytes(1, 50, 8, 2, 128, 20, 16000) > 0
