@@ -56,6 +56,10 @@ struct QuantPrefillArgs {
   float scale_log2;
 };
 
+// What a column's weights are relative to is kept this many powers of two above the largest score seen when it was
+// set, and moved when a score passes it: weights are at most 1, and sums of large finite values have as much room.
+constexpr float kSlack = 8.f;
+
 // (the outputs leave through the values' space, after the last product)
 template <int D, int BITS>
 struct CodeSmem {
@@ -480,7 +484,7 @@ __device__ __forceinline__ void quant_prefill_item(const QuantPrefillArgs& a, co
                  "v"(__builtin_bit_cast(u32x4, pcur[1][1])), "v"(lnew));
     __builtin_amdgcn_s_setprio(0);
     bool check = true;
-    if constexpr (HP) check = __builtin_amdgcn_ballot_w64(!(lnew <= pre::kRescaleLimit)) != 0;
+    if constexpr (HP) check = __builtin_amdgcn_ballot_w64(!(lnew <= 1.f)) != 0;
     if (check) {
       float mx = -INFINITY;
 #pragma unroll
@@ -488,9 +492,9 @@ __device__ __forceinline__ void quant_prefill_item(const QuantPrefillArgs& a, co
 #pragma unroll
         for (int r = 0; r < 16; ++r) mx = fmaxf(mx, cur[beta][r]);
       mx = fmaxf(mx, pre::swap_halves(mx)) * a.scale_log2;
-      const bool grow = mx > m + pre::kRescaleThreshold;
+      const bool grow = mx > m;
       if (__builtin_amdgcn_ballot_w64(grow)) {
-        const float m_new = grow ? mx : m;
+        const float m_new = grow ? mx + kSlack : m;
         const float alpha = fast_exp2(m - m_new);
         m = m_new;
         lpart *= alpha;

@@ -333,3 +333,29 @@ def test_prefill_queries_that_are_not_finite(gpu_lib):
                                     i32([0, new]), new, cached + new, 0.1, out)
     bad = torch.isnan(out).any(2).cpu().numpy()
     assert bad[3, 1] and bad[80, 6] and bad.sum() == 2
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+def test_prefill_extreme_scales(gpu_lib, bits):
+    """Values near the largest and the least, and scores far apart: no sum leaves the 32-bit range. (A weight times
+    a scale near 2^-98 may lose the bits below 2^-133, the least bf16: 300 keys' codes of 448 at most, which is less
+    than 2^-115.)"""
+    import torch
+    lib = gpu_lib
+    rng = np.random.default_rng(9)
+    hq, hkv, d, n, new = 4, 1, 128, 300, 40
+    for power, spread in ((126.0, 1.0), (-95.0, 1.0), (0.0, 300.0)):
+        x = np.clip(bf16_to_f64(rand_bf16(rng, (2, 19, hkv, BS, d))), -3.9, 3.9)
+        slabs = Q.blocks(x[0] * spread, np.clip(x[1], -1.9, 1.9) * 2.0**power, d, bits)
+        tables = rng.permutation(19)[None].astype(np.int32)
+        q = rand_bf16(rng, (new, hq, d))
+        out = torch.empty((new, hq, d), dtype=torch.bfloat16, device="cuda")
+        lib.pkv_quant_prefill_attention(torch.from_numpy(slabs).cuda(), to_dev_bits(q), i32(tables), i32([n - new]),
+                                        i32([0, new]), new, n, 0.09, out)
+        got = bf16_to_f64(to_host_bits(out))
+        k, v = (y.copy() for y in sequence(slabs, tables[0], n, d, bits))
+        for j in (0, new // 2, new - 1):
+            at = n - new + j + 1
+            y = bf16_to_f64(q[j])
+            o, _, tol, _ = rows_of(y, k[0, :at], v[0, :at], 0.09, 2.0**-8, parts_off(y, bits))
+            assert np.isfinite(got[j]).all() and (np.abs(got[j] - o) <= tol + 2.0**-115).all(), (power, spread, j)

@@ -250,3 +250,53 @@ def test_a_parked_prefix(gpu_lib, bits):
     assert torch.equal(k.view(torch.int16), k2.view(torch.int16))
     off = (v.double() - v2.double()).abs()
     assert (off <= (0 if bits == 4 else 2.0**-4 * v2.double().abs() + top * 2.0**-18)).all()
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+def test_padded_batch(gpu_lib, bits):
+    """Rows behind the last sequence: none is appended, and outputs there stay as they were."""
+    import torch
+    lib = gpu_lib
+    hq, hkv, d = 8, 2, 128
+    loop = Loop(lib, (hq, hkv, d), bits, 2, 100, 3)
+    loop.prompts([40, 7])
+    cached, cu = i32(loop.lens), i32([0, 5, 6])
+    fused = to_dev_bits(loop.rows(16, hq + 2 * hkv))
+    k, v, q = fused[:, :hkv], fused[:, hkv:2 * hkv], fused[:, 2 * hkv:].contiguous()
+    exact = loop.cache.clone()
+    lib.pkv_quant_append(exact, k[:6], v[:6], loop.tables, cached, cu, 5)
+    lib.pkv_quant_append(loop.cache, k, v, loop.tables, cached, cu, 16)  # (a bound above every length, too)
+    assert torch.equal(loop.cache, exact)
+    outs = []
+    for rows, most in ((6, 5), (16, 16)):
+        out, lse = torch.full((rows, hq, d), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((rows, hq), 7.0,
+                                                                                                   device="cuda")
+        lib.pkv_quant_prefill_attention(loop.cache, q[:rows], loop.tables, cached, cu, most, 40 + most, 0.1, out, lse=lse)
+        outs.append((out, lse))
+    (a, za), (b, zb) = outs
+    assert torch.equal(a.view(torch.int16), b[:6].view(torch.int16)) and torch.equal(za, zb[:6])
+    assert (b[6:] == 7).all() and (zb[6:] == 7).all()
+
+
+def test_two_streams_without_workspaces(gpu_lib):
+    """Decodes on two streams at once, each with the binding's own workspace of its stream."""
+    import torch
+    lib = gpu_lib
+    hq, hkv, d, bits = 8, 2, 128, 4
+    loop = Loop(lib, (hq, hkv, d), bits, 2, 6000, 4)
+    loop.prompts([5900, 2000])
+    lens = i32(loop.lens)
+    qs = [to_dev_bits(loop.rows(2, hq)) for _ in range(2)]
+    outs = [[torch.empty_like(q) for _ in range(6)] for q in qs]
+    want = []
+    for q, o in zip(qs, outs):
+        lib.pkv_quant_decode_attention(loop.cache, q, loop.tables, lens, 6000, 0.1, o[0])
+        want.append(o[0].clone())
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for n in range(6):
+        for s, q, o in zip(streams, qs, outs):
+            lib.pkv_quant_decode_attention(loop.cache, q, loop.tables, lens, 6000, 0.1, o[n], stream=s)
+    torch.cuda.synchronize()
+    for o, w in zip(outs, want):
+        assert all(torch.equal(x.view(torch.int16), w.view(torch.int16)) for x in o)
