@@ -585,7 +585,9 @@ size_t pkv_quant_decode_workspace_bytes(int32_t num_seqs, int32_t num_q_heads, i
                                         int32_t head_dim, int32_t bits, int32_t max_seq_len);
 
 /* Prefix-reuse prefill attention over the quantised cache, the new tokens appended before: with
- * pkv_prefill_attention's arguments, optional workspace and plan, over what the codes stand for. 32-bit sums; a
+ * pkv_prefill_attention's arguments over what the codes stand for. The workspace (optional, at least
+ * pkv_quant_prefill_workspace_bytes, 16-byte aligned, not shared by calls that overlap) lets the call take its sequences
+ * longest first and split their keys; without one it does neither. 32-bit sums; a
  * weight times its token's value scale is rounded to bf16 once. Beside 4-bit keys a query is exact where it is at
  * least 2^-6 of the largest of its 32 dims, and within 2^-14 of the largest otherwise. A key or value that reads
  * back as NaN makes NaN of the rows that see it, and of no other. max_total_len is at most 2^30. */

@@ -950,9 +950,9 @@ pkv_status pkv_quant_decode_attention(const pkv_quant_kv* kv, const void* q, int
 size_t pkv_quant_prefill_workspace_bytes(int32_t num_seqs, int32_t total_new, int32_t num_q_heads,
                                          int32_t num_kv_heads, int32_t head_dim, int32_t bits,
                                          int32_t max_new_len, int32_t max_total_len) {
-  if (bits != 4 && bits != 8) return 0;
-  return pkv_prefill_workspace_bytes(num_seqs, total_new, num_q_heads, num_kv_heads, head_dim,
-                                     max_new_len, max_total_len);
+  if ((bits != 4 && bits != 8) || (head_dim != 64 && head_dim != 128) || max_total_len <= 0) return 0;
+  return quant_prefill_workspace_bytes(num_seqs, total_new, num_q_heads, num_kv_heads, head_dim,
+                                       max_new_len, max_total_len);
 }
 
 pkv_status pkv_quant_prefill_attention(const pkv_quant_kv* kv, const void* q, int32_t num_q_heads,
@@ -968,9 +968,14 @@ pkv_status pkv_quant_prefill_attention(const pkv_quant_kv* kv, const void* q, in
   const KvView shape = shape_of(view);
   bool empty = false;
   st = check_prefill(shape, fn, q, num_q_heads, block_tables, max_blocks, cached_lens, cu_new_lens,
-                     num_seqs, total_new, max_new_len, max_total_len, scale, out, workspace,
-                     workspace_bytes, &empty);
+                     num_seqs, total_new, max_new_len, max_total_len, scale, out, nullptr, 0, &empty);
   if (st != PKV_OK || empty) return st;
+  const size_t need = quant_prefill_workspace_bytes(num_seqs, total_new, num_q_heads, view.hkv,
+                                                    view.head_dim, max_new_len, max_total_len);
+  if (need > 0 && workspace != nullptr && (workspace_bytes < need || !aligned16(workspace)))
+    return fail(PKV_ERR_INVALID_ARG,
+                std::string(fn) + ": workspace too small or not 16-byte aligned (see "
+                                  "pkv_quant_prefill_workspace_bytes; NULL runs without the plan)");
   if (max_total_len > (1 << 30))
     return fail(PKV_ERR_INVALID_ARG, std::string(fn) + ": max_total_len above 2^30");
   const hipStream_t s = static_cast<hipStream_t>(stream);
@@ -979,9 +984,7 @@ pkv_status pkv_quant_prefill_attention(const pkv_quant_kv* kv, const void* q, in
                              num_seqs, total_new, max_new_len, max_total_len);
     if ((st = check_metadata(fn, &c, 1, s)) != PKV_OK) return st;
   }
-  const bool plan = workspace != nullptr &&
-                    prefill_workspace_bytes(num_seqs, total_new, num_q_heads, view.hkv,
-                                            view.head_dim, max_new_len, max_total_len) > 0;
+  const bool plan = workspace != nullptr && need > 0;
   return launched(launch_quant_prefill(view.cache, view.num_blocks, view.hkv, view.head_dim,
                                        view.bits, static_cast<const uint16_t*>(q), num_q_heads,
                                        block_tables, max_blocks, cached_lens, cu_new_lens, num_seqs,

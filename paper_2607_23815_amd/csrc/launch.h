@@ -166,7 +166,9 @@ size_t quant_decode_workspace_bytes(int32_t num_seqs, int32_t hq, int32_t hkv, i
                                     int32_t bits, int32_t max_len);
 hipError_t launch_quant_decode(QuantDecodeArgs a, int head_dim, int bits, void* workspace,
                                hipStream_t stream);
-// As launch_prefill, over the cache.
+// As launch_prefill, over the cache, with a plan of its own.
+size_t quant_prefill_workspace_bytes(int32_t num_seqs, int32_t total_new, int32_t hq, int32_t hkv,
+                                     int32_t head_dim, int32_t max_new_len, int32_t max_total_len);
 hipError_t launch_quant_prefill(const uint8_t* cache, int32_t num_blocks, int32_t hkv, int32_t head_dim,
                                 int32_t bits, const uint16_t* q, int32_t hq,
                                 const int32_t* block_tables, int32_t max_blocks,

@@ -1,5 +1,5 @@
-// Prefix-reuse prefill attention over a cache held in 8 or 4 bits (gfx950): items, columns, tiles, lazy
-// softmax, key splits and their order as in the bf16 prefill (prefill_impl.h), on tiles that arrive as codes.
+// Prefix-reuse prefill attention over a cache held in 8 or 4 bits (gfx950): items, columns, tiles and
+// lazy softmax as in the bf16 prefill (prefill_impl.h), on tiles that arrive as codes.
 //
 // What bounds the bf16 kernel is vector work beside the products, and codes that every wave converts for itself
 // are as much again (48 suffixes of 64-401 tokens over 500-3500, 4 bits, 32/8 heads of 128 dims: 483 us against
@@ -17,10 +17,11 @@
 // reach only the rows that see them, and slots past the sequence's end none.
 // Step kt: value products of tile kt - 1, the softmax of tile kt, score products of tile kt + 1 and the conversion
 // of V(kt) are one block; K(kt + 2) and the codes of V(kt + 1) are loaded. Of the case above the step's vector
-// work is 1.2 times the bf16 kernel's (32 products with scales), its time 415 us against 415-440 (928 TFLOP/s);
-// with 64 dims, where vector work weighs more, 1.16 times the bf16 kernel's.
+// work is 1.2 times the bf16 kernel's (32 products with scales), its time 415 us against 415-440, and 395 (980
+// TFLOP/s) with the plan below; with 64 dims, where vector work weighs more, 1.16 times the bf16 kernel's.
 #include <math.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "launch.h"
@@ -30,6 +31,7 @@
 namespace pkv {
 namespace {
 
+constexpr int32_t kMostSplits = 64;  // (a lane each in the merge)
 constexpr int32_t kMostRanked = 16;  // sequences up to which every wave ranks them for itself (seq_at_rank)
 
 using pre::kCols;
@@ -662,7 +664,49 @@ __global__ __launch_bounds__(kThreads) void quant_prefill_merge_kernel(const Qua
   if (a.lse != nullptr && lane == 0) a.lse[row] = (top + log2f(den)) * kLn2;
 }
 
+// How a call is cut, by host arithmetic on its sizes: about `tiles` work items (kv head, 128 columns) on 512 places.
+// Measured with 4 bits, lengths spread evenly, us, `none` and splits of that many keys:
+//   - items that fill the chip are not split, but sequences taken longest first (a split costs 4 bytes per output dim
+//     written and read: 24 suffixes of 50-300 tokens over 500-4000, 32/8 heads of 128, 201 without order, 185 with it,
+//     211 with 3008; 128 single rows over 500-16000 316, and 388; but 450 items and more of one column tile each end
+//     with the longest: 64 rows over 4000-60000 986, and 699);
+//   - a few items are cut so that they fill it once (one of 400 over 16000, 32/8 heads of 128: 120 with 4096, 140 with
+//     3328, 127 with 2048, 144 with 1024; one of 64 over 60000 77 with 2048, 91 with 1024), into 32 splits and of 768 keys at least
+//     (one of 100 over 4000 27 with 768, 28 with 512, 30 with 1024);
+//   - between these, splits of 3008 keys even out the lengths (40 of 30-100 over 2000-20000, 16/4 heads of 64: 209, 217
+//     with 1536, 211 with 4096; 3 of 101-509 over 4096-16384, 32/8 of 128, 183, 193 and 208), or of 1536 for the
+//     fewer of 64 dims (the same 3 101, 97 and 119; 32 of 1-8 over 4000-30000 96, 91.5 and 111).
+PrefillSplit quant_prefill_plan(int32_t num_seqs, int32_t total_new, int32_t hq, int32_t hkv, int32_t head_dim,
+                                int32_t max_new_len, int32_t max_total_len) {
+  PrefillSplit sp{0, 1, false};
+  if (num_seqs <= 0 || total_new <= 0 || hkv <= 0 || hq <= 0 || hq % hkv != 0 || max_new_len <= 0) return sp;
+  const int64_t columns = (int64_t)total_new * (hq / hkv);
+  const int64_t most = ((int64_t)max_new_len * (hq / hkv) + kCols - 1) / kCols;  // column tiles of a sequence
+  const int64_t tiles = hkv * std::clamp<int64_t>((columns + num_seqs * (kCols / 2) + kCols - 1) / kCols, num_seqs,
+                                                  num_seqs * most);
+  // (the order is a launch of its own above kMostRanked sequences)
+  sp.order = num_seqs > 1 && (num_seqs <= kMostRanked || (max_total_len >= 2048 && tiles >= 100));
+  if (tiles >= 640 || (tiles >= 450 && columns >= (int64_t)num_seqs * 2 * kCols)) return sp;
+  int64_t keys = head_dim == 64 && tiles < 250 ? 1536 : 3008;
+  if (tiles <= 110) keys = std::max<int64_t>(768, max_total_len / std::min<int64_t>(32, 512 / tiles) + kKeys);
+  else keys = std::max<int64_t>(keys, max_total_len / (4096 / tiles) + kKeys);
+  keys = std::max<int64_t>(keys, max_total_len / kMostSplits + kKeys) / kKeys * kKeys;
+  if (keys > 4096 && keys < 4500) keys = 4096;  // (the tiles whose blocks a wave holds: 120 against 128 with 4160)
+  if (max_total_len <= keys) return sp;
+  sp.split_keys = (int32_t)keys;
+  sp.nsplit = (int32_t)((max_total_len + keys - 1) / keys);
+  return sp;
+}
+
 }  // namespace
+
+size_t quant_prefill_workspace_bytes(int32_t num_seqs, int32_t total_new, int32_t hq, int32_t hkv,
+                                     int32_t head_dim, int32_t max_new_len, int32_t max_total_len) {
+  const PrefillSplit sp = quant_prefill_plan(num_seqs, total_new, hq, hkv, head_dim, max_new_len, max_total_len);
+  size_t bytes = sp.order ? order_bytes(num_seqs) : 0;
+  if (sp.nsplit > 1) bytes += (size_t)total_new * hq * sp.nsplit * (head_dim + 2) * sizeof(float);
+  return bytes;
+}
 
 hipError_t launch_quant_prefill(const uint8_t* cache, int32_t num_blocks, int32_t hkv, int32_t head_dim,
                                 int32_t bits, const uint16_t* q, int32_t hq,
@@ -673,7 +717,7 @@ hipError_t launch_quant_prefill(const uint8_t* cache, int32_t num_blocks, int32_
                                 void* workspace, hipStream_t stream) {
   PrefillSplit sp{0, 1, false};
   if (workspace != nullptr)
-    sp = prefill_split_plan(num_seqs, hq, hkv, max_new_len, max_total_len);
+    sp = quant_prefill_plan(num_seqs, total_new, hq, hkv, head_dim, max_new_len, max_total_len);
   QuantPrefillArgs a{};
   a.cache = cache;
   a.q = q;

@@ -291,6 +291,23 @@ def test_prefill_many_items(gpu_lib):
 
 
 @pytest.mark.parametrize("bits", [4, 8])
+def test_prefill_plans(gpu_lib, bits):
+    """The sides of the plan: a few items cut to fill the chip, cuts of 3008 keys behind an ordering launch, items that
+    fill the chip in order, and one sequence alone; lengths of none and one among them."""
+    rng = np.random.default_rng(20 + bits)
+    lib = gpu_lib
+    sizes = lambda b, *a: lib.pkv_quant_prefill_workspace_bytes(b, *a)
+    check_prefill(lib, rng, [3000], [64], 8, 2, 64, bits)
+    check_prefill(lib, rng, rng.integers(0, 700, 17).tolist() + [3900, 0], [1, 0] + rng.integers(1, 9, 17).tolist(), 8, 8,
+                  64, bits)
+    assert sizes(19, 90, 8, 8, 64, bits, 8, 3908) > 90 * 8 * 2 * 66 * 4  # (split in two)
+    cached, new = rng.integers(0, 300, 20), rng.integers(60, 140, 20)
+    cached[3] = 2500
+    check_prefill(lib, rng, cached, new, 32, 8, 64, bits)
+    assert 0 < sizes(20, int(new.sum()), 32, 8, 64, bits, int(new.max()), 2640) < 4096  # (an order alone)
+
+
+@pytest.mark.parametrize("bits", [4, 8])
 @pytest.mark.parametrize("d", [64, 128])
 def test_prefill_nan_reaches_the_rows_that_see_it(gpu_lib, bits, d):
     """A token that reads back as NaN, key or value: rows before it keep their bits, rows from it on are NaN, and so
