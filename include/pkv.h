@@ -586,11 +586,12 @@ size_t pkv_quant_decode_workspace_bytes(int32_t num_seqs, int32_t num_q_heads, i
 
 /* Prefix-reuse prefill attention over the quantised cache, the new tokens appended before: with
  * pkv_prefill_attention's arguments over what the codes stand for. The workspace (optional, at least
- * pkv_quant_prefill_workspace_bytes, 16-byte aligned, not shared by calls that overlap) lets the call take its sequences
- * longest first and split their keys; without one it does neither. 32-bit sums; a
- * weight times its token's value scale is rounded to bf16 once. Beside 4-bit keys a query is exact where it is at
- * least 2^-6 of the largest of its 32 dims, and within 2^-14 of the largest otherwise. A key or value that reads
- * back as NaN makes NaN of the rows that see it, and of no other. max_total_len is at most 2^30. */
+ * pkv_quant_prefill_workspace_bytes, 16-byte aligned, not shared by calls that overlap) lets the call take its
+ * sequences longest first and split their keys; without one it does neither. Its size is for the call's own
+ * sizes: fewer rows can need more, being split further. 32-bit sums; a weight times its token's value scale is
+ * rounded to bf16 once. Beside 4-bit keys a query is exact where it is at least 2^-6 of the largest of its 32
+ * dims, and within 2^-14 of the largest otherwise. A key or value that reads back as NaN makes NaN of the rows
+ * that see it, and of no other. max_total_len is at most 2^30. */
 pkv_status pkv_quant_prefill_attention(const pkv_quant_kv* kv, const void* q, int32_t num_q_heads,
                                        const int32_t* block_tables, int32_t max_blocks,
                                        const int32_t* cached_lens, const int32_t* cu_new_lens,

@@ -1025,7 +1025,7 @@ def pkv_quant_prefill_attention(cache, q, block_tables, cached_lens, cu_new_lens
                                 max_total_len: int, scale: float, out, lse=None, workspace=None,
                                 stream=None) -> None:
     """Suffix rows q [total_new][Hq][D] over their sequences' cached and new keys in cache (the new
-    ones appended before). Without a workspace the keys are not split."""
+    ones appended before). Without a workspace the keys are not split and the sequences not ordered."""
     dev, hip_stream = _launch_on(stream)
     kv, hkv, d, _ = _quant_kv_on(cache, dev)
     b = cached_lens.numel()
