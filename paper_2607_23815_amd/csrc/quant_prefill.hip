@@ -341,8 +341,9 @@ __device__ __forceinline__ void quant_prefill_item(const QuantPrefillArgs& a, co
   };
 
   // The matrix-core work of a step, in groups: value products of tile kt - 1 with the weights pw (PV), then score
-  // products of the keys of tile kt + 1 (QK), which take the registers that pw leaves; beside them the sixteen slices of the softmax of cur (SM)
-  // and the landing of the wave's block of V(kt) (LAND; last: kt is the item's last tile).
+  // products of the keys of tile kt + 1 (QK), which take the registers that pw leaves; beside them the sixteen
+  // slices of the softmax of cur (SM) and the landing of the wave's block of V(kt) (LAND; last: kt is the item's
+  // last tile).
   auto block = [&](auto qk, auto pv, auto smx, auto landing, auto last, int kt, auto buf, f32x16 (&sc)[2],
                    const bf16x8 (&pw)[2][2], const f32x16 (&cur)[2], bf16x8 (&pcur)[2][2], float (&sum)[kSums]) {
     constexpr bool QK = decltype(qk)::value, PV = decltype(pv)::value, SM = decltype(smx)::value;
@@ -671,8 +672,8 @@ __global__ __launch_bounds__(kThreads) void quant_prefill_merge_kernel(const Qua
 //     211 with 3008; 128 single rows over 500-16000 316, and 388; but 450 items and more of one column tile each end
 //     with the longest: 64 rows over 4000-60000 986, and 699);
 //   - a few items are cut so that they fill it once (one of 400 over 16000, 32/8 heads of 128: 120 with 4096, 140 with
-//     3328, 127 with 2048, 144 with 1024; one of 64 over 60000 77 with 2048, 91 with 1024), into 32 splits and of 768 keys at least
-//     (one of 100 over 4000 27 with 768, 28 with 512, 30 with 1024);
+//     3328, 127 with 2048, 144 with 1024; one of 64 over 60000 77 with 2048, 91 with 1024), into 32 splits at most
+//     and of 768 keys at least (one of 100 over 4000 27 with 768, 28 with 512, 30 with 1024);
 //   - between these, splits of 3008 keys even out the lengths (40 of 30-100 over 2000-20000, 16/4 heads of 64: 209, 217
 //     with 1536, 211 with 4096; 3 of 101-509 over 4096-16384, 32/8 of 128, 183, 193 and 208), or of 1536 for the
 //     fewer of 64 dims (the same 3 101, 97 and 119; 32 of 1-8 over 4000-30000 96, 91.5 and 111).
