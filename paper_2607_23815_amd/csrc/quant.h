@@ -73,14 +73,6 @@ __device__ __forceinline__ u32x2 four_bf16(const uint32_t* w) {
     return u32x2{two_bf16_of_8<0>(w[kA], 1.f), two_bf16_of_8<1>(w[kA], 1.f)};
 }
 
-// x times s, 0 where either is 0. (By the compiler's own name for the instruction and not as assembly: one that
-// takes an exponential's result has a wait state to keep, which the compiler counts for what it knows.)
-#if __HIP_DEVICE_COMPILE__
-__device__ float mul_zero(float x, float s) __asm("llvm.amdgcn.fmul.legacy");
-#else
-__device__ inline float mul_zero(float x, float s) { return x * s; }
-#endif
-
 // The four slots' codes of a lane's dim 16 kA + b times the slots' scales, as bf16 (exact).
 template <int BITS, int kA>
 __device__ __forceinline__ u32x2 four_scaled(const uint32_t* w, const u32x4 scale) {
