@@ -562,7 +562,7 @@ pkv_status pkv_quant_append(const pkv_quant_kv* kv, const void* k_new, int64_t k
  * 16 slots of block pairs[2k] of `from`, for every kv head, go to block pairs[2k+1] of `to` (pairs: int32
  * device memory [num_pairs][2]). Slots that hold no token are converted like the others. The blocks
  * written must differ from one another; a pair naming a block outside either pool is skipped. Both pools
- * have the same num_kv_heads and head_dim. num_pairs * num_kv_heads stays below 2^26. */
+ * have the same num_kv_heads and head_dim. num_pairs * num_kv_heads is at most 2^26 - 4. */
 pkv_status pkv_quant_blocks(const pkv_paged_kv* from, const pkv_quant_kv* to, const int32_t* pairs,
                             int32_t num_pairs, void* stream);
 pkv_status pkv_dequant_blocks(const pkv_quant_kv* from, const pkv_paged_kv* to, const int32_t* pairs,

@@ -278,8 +278,8 @@ pkv_status convert_blocks(const char* fn, const pkv_paged_kv* kv, const pkv_quan
   if (num_pairs < 0) return fail(PKV_ERR_INVALID_ARG, f + ": negative size");
   if (num_pairs == 0) return ok();
   if (pairs == nullptr) return fail(PKV_ERR_INVALID_ARG, f + ": NULL pointer");
-  if ((int64_t)num_pairs * view.hkv >= (1 << 26))  // (waves of a launch)
-    return fail(PKV_ERR_INVALID_ARG, f + ": 2^26 pairs x kv heads or more");
+  if ((int64_t)num_pairs * view.hkv > (1 << 26) - 4)  // (waves of a launch, four a workgroup, below 2^32 threads)
+    return fail(PKV_ERR_INVALID_ARG, f + ": more than 2^26 - 4 pairs x kv heads");
   const QuantBlocksArgs a{view.cache, pool.k, pool.v, pairs, num_pairs, view.hkv, view.num_blocks,
                           pool.num_blocks};
   return launched(launch_quant_blocks(a, back, view.head_dim, view.bits,
