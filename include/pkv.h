@@ -574,8 +574,10 @@ pkv_status pkv_dequant_blocks(const pkv_quant_kv* from, const pkv_paged_kv* to, 
  * weights reach the value product within 2^-16 of themselves; bf16 output. A key or value that reads
  * back as NaN makes NaN of the heads that see it. workspace: at least pkv_quant_decode_workspace_bytes (0
  * where there are items enough to fill the chip), 16-byte aligned, owned by the caller, not read
- * back; calls that share one must not overlap. num_seqs * num_kv_heads stays below 2^22, max_seq_len at
- * most 2^30. */
+ * back; calls that share one must not overlap. Its size is for the call's own sizes: fewer sequences, or a
+ * smaller max_seq_len, can need more, being split further (8 kv heads and 4096 keys: none for 128 sequences,
+ * some for 127), so one workspace for several sizes is as large as the largest of theirs. num_seqs *
+ * num_kv_heads stays below 2^22, max_seq_len at most 2^30. */
 pkv_status pkv_quant_decode_attention(const pkv_quant_kv* kv, const void* q, int32_t num_q_heads,
                                       const int32_t* block_tables, int32_t max_blocks,
                                       const int32_t* seq_lens, int32_t num_seqs,

@@ -991,6 +991,7 @@ def _attended_sizes(q, out, lse, block_tables, seqs, d):
 
 def pkv_quant_decode_workspace_bytes(num_seqs, num_q_heads, num_kv_heads, head_dim, bits,
                                      max_seq_len) -> int:
+    """For a call of these sizes; fewer sequences or a smaller max_seq_len can need more."""
     return int(_lib.pkv_quant_decode_workspace_bytes(num_seqs, num_q_heads, num_kv_heads, head_dim,
                                                      bits, max_seq_len))
 
@@ -1017,6 +1018,7 @@ def pkv_quant_decode_attention(cache, q, block_tables, seq_lens, max_seq_len: in
 
 def pkv_quant_prefill_workspace_bytes(num_seqs, total_new, num_q_heads, num_kv_heads, head_dim, bits,
                                       max_new_len, max_total_len) -> int:
+    """For a call of these sizes; fewer rows can need more."""
     return int(_lib.pkv_quant_prefill_workspace_bytes(num_seqs, total_new, num_q_heads, num_kv_heads,
                                                       head_dim, bits, max_new_len, max_total_len))
 

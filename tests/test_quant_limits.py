@@ -3,7 +3,7 @@ here: a call that passes its checks ends at the launch)."""
 
 import pytest
 
-from tests.test_quant_abi import _append, _blocks, _decode, _kv, _pool, lib, refused  # noqa: F401
+from tests.test_quant_abi import FAKE, _append, _blocks, _decode, _kv, _pool, lib, refused  # noqa: F401
 
 
 def passes(lib, call, *args, **kw):  # noqa: F811
@@ -41,3 +41,20 @@ def test_blocks_of_an_append(lib):  # noqa: F811
         a = dict(ks=1024, vs=1024, max_blocks=2**30, num_seqs=65535)
         passes(lib, _append, _kv(lib, hkv=heads), max_new=most, **a)
         refused(lib, lib.PKV_ERR_INVALID_ARG, _append(lib, _kv(lib, hkv=heads), max_new=most + 1, **a), "2^24")
+
+
+def test_a_decode_workspace_is_for_the_calls_own_sizes(lib):  # noqa: F811
+    """Smaller calls can need more than larger ones. One that is given too little is refused, and the largest of
+    several sizes' needs serves each of them."""
+    size = lambda n, longest: lib.pkv_quant_decode_workspace_bytes(n, 32, 8, 128, 4, longest)
+    call = lambda n, longest, ws, nbytes: _decode(lib, _kv(lib, hkv=8), hq=32, num_seqs=n, max_len=longest,
+                                                  max_blocks=1024, ws=ws, ws_bytes=nbytes)
+    assert size(128, 4096) == 0 < size(127, 4096)
+    assert 0 < size(64, 9000) < size(64, 8192)
+    for n, longest, given in ((127, 4096, 0), (64, 8192, size(64, 9000))):
+        for ws in (None, FAKE):
+            refused(lib, lib.PKV_ERR_INVALID_ARG, call(n, longest, ws, given), "workspace", "pkv_quant_decode_workspace_bytes")
+    sizes = [(n, longest) for n in (1, 2, 7, 64, 127, 128, 300) for longest in (100, 2048, 2049, 8192, 9000, 16000)]
+    most = max(size(*x) for x in sizes)
+    for x in sizes:
+        passes(lib, lambda lib: call(*x, FAKE, most))
