@@ -571,10 +571,10 @@ pkv_status pkv_dequant_blocks(const pkv_quant_kv* from, const pkv_paged_kv* to, 
 /* Decode attention over the quantised cache: pkv_decode_attention on what its codes stand for, with its
  * arguments, a length above max_seq_len being cut to it. Here a length may be 0 (a padding sequence): its
  * output is zeros and its LSE -infinity, as for a row whose scores are all -infinity. 32-bit sums;
- * weights reach the value product within 2^-16 of themselves; bf16 output. A key or value that reads
- * back as NaN makes NaN of the heads that see it. workspace: at least pkv_quant_decode_workspace_bytes (0
- * where there are items enough to fill the chip), 16-byte aligned, owned by the caller, not read
- * back; calls that share one must not overlap. Its size is for the call's own sizes: fewer sequences, or a
+ * a weight times its token's value scale reaches the value product within 2^-16 of itself (or 2^-126, where
+ * that is more); bf16 output. A key or value that reads back as NaN makes NaN of the heads that see it.
+ * workspace: at least pkv_quant_decode_workspace_bytes (0 where there are items enough to fill the chip),
+ * 16-byte aligned, owned by the caller, not read back; calls that share one must not overlap. Its size is for the call's own sizes: fewer sequences, or a
  * smaller max_seq_len, can need more, being split further (8 kv heads and 4096 keys: none for 128 sequences,
  * some for 127), so one workspace for several sizes is as large as the largest of theirs. num_seqs *
  * num_kv_heads stays below 2^22, max_seq_len at most 2^30. */
@@ -591,9 +591,10 @@ size_t pkv_quant_decode_workspace_bytes(int32_t num_seqs, int32_t num_q_heads, i
  * pkv_quant_prefill_workspace_bytes, 16-byte aligned, not shared by calls that overlap) lets the call take its
  * sequences longest first and split their keys; without one it does neither. Its size is for the call's own
  * sizes: fewer rows can need more, being split further. 32-bit sums; a weight times its token's value scale is
- * rounded to bf16 once. Beside 4-bit keys a query is exact where it is at least 2^-6 of the largest of its 32
- * dims, and within 2^-14 of the largest otherwise. A key or value that reads back as NaN makes NaN of the rows
- * that see it, and of no other. max_total_len is at most 2^30. */
+ * rounded to bf16 once (the decode takes it in two parts). Beside 4-bit keys a query is exact where it is at
+ * least 2^-6 of the largest of its 32 dims, and within 2^-14 of the largest otherwise (all of them within 2^-130
+ * where the largest is below 2^-116); beside 8-bit keys it is exact. A key or value that reads back as NaN makes
+ * NaN of the rows that see it, however small its weight, and of no other. max_total_len is at most 2^30. */
 pkv_status pkv_quant_prefill_attention(const pkv_quant_kv* kv, const void* q, int32_t num_q_heads,
                                        const int32_t* block_tables, int32_t max_blocks,
                                        const int32_t* cached_lens, const int32_t* cu_new_lens,

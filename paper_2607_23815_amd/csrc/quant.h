@@ -158,7 +158,8 @@ constexpr int kParts = 3;
 // A group of 32 queries (16 words of bf16) in kParts parts of e2m3 and their scale bytes (byte i: part i's). The
 // group's largest magnitude is brought to 4 .. 8 by a power of two; a part is the nearest code to what the
 // parts before it leave, times 16^i. A code has 4 significant bits above 1 and steps of 1/8 below, so the parts'
-// sum is the query if that is at least 2^-6 of the group's largest, and within 2^-14 of the largest otherwise.
+// sum is the query if that is at least 2^-6 of the group's largest, and within 2^-14 of the largest otherwise. (Scales
+// end at 2^-118: of a group whose largest is below 2^-116 every query is within 2^-130.)
 // Where a query is not finite the bytes are 255, which makes the products NaN.
 __device__ __forceinline__ uint32_t query_parts(u32x16 x, i32x8 (&part)[kParts]) {
 #if __HIP_DEVICE_COMPILE__

@@ -116,9 +116,10 @@ __device__ __forceinline__ void value_products(const BlockCodes<D, BITS>& even,
 
 // Where slabs are small (all but 8 bits and 128 dims) a wave's slabs come through LDS, loaded straight there, keys'
 // and values' halves apart: the next step's are on their way from when this step's have been read. The registers
-// that codes in flight would take are free for more waves: 128 sequences of 4000-32000 keys, 4 bits, 16/4 heads
-// of 64 dims 141 us against 162 with registers, 512 of 1-300 keys, 32/8 heads of 128, 23.8 and 24.7. (Two steps
-// ahead, which leaves two waves a SIMD unit with 128 dims: 26.1 there, elsewhere within 2%.)
+// that codes in flight would take are free for more waves: 128 sequences of 4000-32000 keys, 16/4 heads of 64 dims,
+// 4 bits 129 us against 137 with registers (8 bits 225 both), 256 of 512-4096 41.5 and 46.7 (8 bits 69 and 75), 512 of
+// 1-300 keys, 32/8 heads of 128, 4 bits 23.6 and 24.9. (Two steps ahead, which leaves two waves a SIMD unit with 128
+// dims: 26.1 there, elsewhere within 2%.)
 template <int D, int BITS>
 struct Ring {
   using S = Slab<D, BITS>;
