@@ -36,31 +36,6 @@ constexpr float kSlack = 8.f;  // (base 2)
 constexpr int kMergeWaves = 4;
 constexpr int kMaxSplits = 128;  // (two a lane in the merge)
 
-template <int kCtrl>
-__device__ __forceinline__ float dpp_f(float x) {
-  return __uint_as_float(dpp<kCtrl>(__float_as_uint(x)));
-}
-constexpr int kRor4 = 0x124, kRor8 = 0x128;  // rotations within 16 lanes
-
-// Sum (or maximum) over the ways, the columns that hold the same head.
-template <int kWays>
-__device__ __forceinline__ float ways_sum(float x) {
-  if constexpr (kWays >= 2) x += dpp_f<kRor8>(x);
-  if constexpr (kWays >= 4) x += dpp_f<kRor4>(x);
-  return x;
-}
-template <int kWays>
-__device__ __forceinline__ float ways_max(float x) {
-  if constexpr (kWays >= 2) x = fmaxf(x, dpp_f<kRor8>(x));
-  if constexpr (kWays >= 4) x = fmaxf(x, dpp_f<kRor4>(x));
-  return x;
-}
-// Two floats as two bf16 each, their sum off by 2^-16 of the float at most.
-__device__ __forceinline__ void two_parts(float x, float y, uint32_t& first, uint32_t& second) {
-  first = pack_bf16x2(x, y);
-  second = pack_bf16x2(x - __uint_as_float(first << 16), y - __uint_as_float(first & 0xFFFF0000u));
-}
-
 // A lane's codes of a block: of the keys (slot col, dims D / 4 * grp ..), and of the values (slots
 // 4 grp .., dims 16 a + col).
 template <int D, int BITS>

@@ -44,12 +44,6 @@ constexpr int kMergeWaves = 4;
 constexpr int kParts = 4;        // waves that share an item where items are few
 constexpr int kXcds = 8;         // workgroups go to the chip's XCDs in turn
 
-template <int kCtrl>
-__device__ __forceinline__ float dpp_f(float x) {
-  return __uint_as_float(dpp<kCtrl>(__float_as_uint(x)));
-}
-constexpr int kRor4 = 0x124, kRor8 = 0x128;  // rotations within 16 lanes
-
 // Odd rows (of 16 lanes) of a and even rows of b change places.
 __device__ __forceinline__ u32x2 swap_rows(uint32_t a, uint32_t b) {
 #if __HIP_DEVICE_COMPILE__
@@ -58,27 +52,6 @@ __device__ __forceinline__ u32x2 swap_rows(uint32_t a, uint32_t b) {
 #else
   return u32x2{a, b};
 #endif
-}
-
-// Sum (or maximum) over the ways, the columns that hold the same head.
-template <int kWays>
-__device__ __forceinline__ float ways_sum(float x) {
-  if constexpr (kWays >= 2) x += dpp_f<kRor8>(x);
-  if constexpr (kWays >= 4) x += dpp_f<kRor4>(x);
-  return x;
-}
-template <int kWays>
-__device__ __forceinline__ float ways_max(float x) {
-  if constexpr (kWays >= 2) x = fmaxf(x, dpp_f<kRor8>(x));
-  if constexpr (kWays >= 4) x = fmaxf(x, dpp_f<kRor4>(x));
-  return x;
-}
-
-// Two floats as two bf16 each, their sum off by 2^-16 of the float at most (its second part is exact in
-// 32 bits, then rounded).
-__device__ __forceinline__ void two_parts(float x, float y, uint32_t& first, uint32_t& second) {
-  first = pack_bf16x2(x, y);
-  second = pack_bf16x2(x - __uint_as_float(first << 16), y - __uint_as_float(first & 0xFFFF0000u));
 }
 
 // One wave's share: entries [e0, e1) of a list. Leaves, summed over the ways, the unnormalised output

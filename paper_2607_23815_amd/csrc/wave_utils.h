@@ -11,6 +11,33 @@ template <int kCtrl>
 __device__ __forceinline__ uint32_t dpp(uint32_t x) {
   return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, kCtrl, 0xF, 0xF, true);
 }
+template <int kCtrl>
+__device__ __forceinline__ float dpp_f(float x) {
+  return __uint_as_float(dpp<kCtrl>(__float_as_uint(x)));
+}
+constexpr int kRor4 = 0x124, kRor8 = 0x128;  // rotations within 16 lanes
+
+// Sum (or maximum) over the kWays columns of a product that hold the same head (16 / kWays columns apart).
+template <int kWays>
+__device__ __forceinline__ float ways_sum(float x) {
+  if constexpr (kWays >= 2) x += dpp_f<kRor8>(x);
+  if constexpr (kWays >= 4) x += dpp_f<kRor4>(x);
+  return x;
+}
+template <int kWays>
+__device__ __forceinline__ float ways_max(float x) {
+  if constexpr (kWays >= 2) x = fmaxf(x, dpp_f<kRor8>(x));
+  if constexpr (kWays >= 4) x = fmaxf(x, dpp_f<kRor4>(x));
+  return x;
+}
+
+// Two floats as two bf16 each, their sum off by 2^-16 of the float at most (its second part is exact in
+// 32 bits, then rounded).
+__device__ __forceinline__ void two_parts(float x, float y, uint32_t& first, uint32_t& second) {
+  first = pack_bf16x2(x, y);
+  second = pack_bf16x2(x - __uint_as_float(first << 16), y - __uint_as_float(first & 0xFFFF0000u));
+}
+
 // x and its value in the lane 16 (or 32) away, in some order.
 __device__ __forceinline__ u32x2 with_row(uint32_t x) {
 #if __HIP_DEVICE_COMPILE__
