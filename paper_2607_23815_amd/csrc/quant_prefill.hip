@@ -12,11 +12,12 @@
 //   - 8-bit keys have no such partner (products of 8-bit codes are off by 2^-11 of the largest one), and a wave
 //     converts its operands, exactly (460 us with 8 bits for the case above), a lane having dims
 //     32 (2 (kk / 4) + hh) + 8 (kk % 4) .. of score product kk, which lie side by side and under one scale.
-// A value's scale multiplies the weight of its token, before its rounding to bf16. A token whose scale is NaN makes NaN
-// of all columns where all see it, however small its weight. In the last tiles, which some columns see only in part,
-// the columns that see such a token are noted and its scale is cleared for the others, whose weight for it is 0; so are
-// scales of slots past the sequence's end. (Noting in every tile, beside products where 0 times NaN is 0, took 0.5-2%
-// longer.)
+// A value's scale multiplies the weight of its token, before its rounding to bf16, which is one, as in the bf16 prefill:
+// a second part of the weights, as the decode takes it, would be as many value products again, half as much matrix
+// work more. A token whose scale is NaN makes NaN of all columns where all see it, however small its weight. In the
+// last tiles, which some columns see only in part, the columns that see such a token are noted and its scale is cleared
+// for the others, whose weight for it is 0; so are scales of slots past the sequence's end. (Noting in every tile,
+// beside products where 0 times NaN is 0, took 0.5-2% longer.)
 // Step kt: value products of tile kt - 1, the softmax of tile kt, score products of tile kt + 1 and the conversion
 // of V(kt) are one block; K(kt + 2) and the codes of V(kt + 1) are loaded. Of the case above the step's vector
 // work is 1.2 times the bf16 kernel's (32 products with scales), its time 415 us against 415-440, and 395 (980
